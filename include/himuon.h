@@ -478,6 +478,160 @@ int himuon_plan_chunks(int64_t n_mats, const int64_t* rows, const int64_t* cols,
  */
 int himuon_select_compute(int dtype, int compute, int K, float a, float b, float c);
 
+/*
+ * The operators of a training step around the optimizer: the token table's lookup
+ * and gradient, the per-head norms of queries and keys with the position rotation,
+ * and activations held in 8 bits with the weight gradient that reads them.
+ *
+ * They follow the rules of the calls above: device pointers (the scalars and
+ * sizes by value), one storage type per call, work enqueued on `stream`, errors
+ * detected before anything is enqueued, no allocation and no synchronisation.
+ * They use no host staging, so they may be captured into a HIP graph. Sums,
+ * norms and products are held in fp32; a result is rounded once, on store. Every
+ * result is the same, bit for bit, from call to call (no order of atomics).
+ * Leading dimensions and strides count elements. Empty batches (no token) are
+ * valid; sizes above INT32_MAX rows or columns are HIMUON_ERR_UNSUPPORTED.
+ */
+
+/* Integer type of token and position arrays. */
+typedef enum himuon_index {
+    HIMUON_I32 = 0,
+    HIMUON_I64 = 1
+} himuon_index_t;
+
+/*
+ * out[i, :] = scale * table[tokens[i], :], i = 0 .. n_tokens-1.
+ *
+ * tokens      n_tokens integers of type `index`. A token outside [0, n_rows)
+ *             (such as -1 for padding) gives a row of zeros.
+ * table, out  n_rows x dim and n_tokens x dim, storage `dtype`; ld >= dim.
+ *             They must not overlap.
+ * Errors: HIMUON_ERR_INVALID_ARG, HIMUON_ERR_UNSUPPORTED, HIMUON_ERR_HIP.
+ */
+int himuon_embed(int64_t n_tokens, const void* tokens, int index, int64_t n_rows, int64_t dim,
+                 const void* table, int64_t ld_table, void* out, int64_t ld_out, float scale, int dtype, void* stream);
+
+/*
+ * The table's gradient: dtable[v, :] = scale * sum of grad[i, :] over the i with
+ * tokens[i] = v, added to dtable[v, :] if accumulate != 0 (rows of tokens that
+ * do not occur are then untouched, otherwise they become zero).
+ *
+ * The tokens are sorted on the device (stable), and every row is summed in fp32
+ * in an order that depends on the tokens alone. Tokens outside [0, n_rows) give nothing.
+ * grad        n_tokens x dim, storage `dtype`.
+ * dtable      n_rows x dim, storage `out_dtype`; must not overlap grad.
+ * workspace   himuon_embed_grad_workspace_size(n_tokens, n_rows, dim) bytes (0:
+ *             invalid sizes), 16-byte aligned.
+ */
+size_t himuon_embed_grad_workspace_size(int64_t n_tokens, int64_t n_rows, int64_t dim);
+
+int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index, int64_t n_rows, int64_t dim,
+                      const void* grad, int64_t ld_grad, int dtype, void* dtable, int64_t ld_dtable, int out_dtype,
+                      float scale, int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Largest head of the calls below. */
+#define HIMUON_MAX_HEAD_DIM 512
+
+/*
+ * What himuon_qk_norm_rope and its gradient share. Queries, keys and their
+ * gradients are [batch, seq, heads, dim] arrays in which the elements of a head
+ * are adjacent; the strides of batch, seq and head are the caller's (slices of a
+ * fused projection, heads before tokens).
+ */
+typedef struct himuon_heads {
+    void* ptr;
+    int64_t stride_batch, stride_seq, stride_head;
+} himuon_heads_t;
+
+typedef struct himuon_qk {
+    int64_t batch, seq;
+    int32_t q_heads, k_heads;  /* >= 1                                            */
+    int32_t head_dim;          /* even, 2 .. HIMUON_MAX_HEAD_DIM                  */
+    int32_t rot_dim;           /* even, 0 .. head_dim: elements that are rotated  */
+    int32_t interleaved;       /* pairs (2i, 2i+1) instead of (i, i + rot_dim/2)  */
+    int32_t dtype;             /* storage of queries, keys and their gradients    */
+    int32_t gain_dtype;        /* storage of the gains and of their gradients     */
+    int32_t index;             /* himuon_index_t of `positions`                   */
+    const void* q_gain;        /* head_dim                                        */
+    const void* k_gain;
+    const float* cos_table;    /* table_rows x rot_dim/2, contiguous: cosine and  */
+    const float* sin_table;    /* sine of position p's angles in row p            */
+    int64_t table_rows;
+    const void* positions;     /* batch x seq, contiguous; NULL: s for token (b, s) */
+    float eps;                 /* >= 0                                            */
+} himuon_qk_t;
+
+/*
+ * Every head's vector x of queries and keys becomes
+ *     y = R(p) (x * gain / sqrt(mean(x^2) + eps)),
+ * R(p) the rotation of the pairs (u, v) by the angles of the token's position:
+ * u' = u cos - v sin, v' = v cos + u sin. Outputs may be the inputs (same
+ * strides). A token whose position lies outside the table is one that is not in
+ * use: its outputs are zeros, and it gives no gradient.
+ */
+int himuon_qk_norm_rope(const himuon_qk_t* args, const himuon_heads_t* q, const himuon_heads_t* k,
+                        const himuon_heads_t* q_out, const himuon_heads_t* k_out, void* stream);
+
+/*
+ * Its backward pass. g_q, g_k: gradients of the outputs; q, k: the inputs of the
+ * forward call (the norms are computed again from them, nothing else is kept);
+ * dq, dk: gradients of the inputs (may be g_q, g_k with the same strides);
+ * dq_gain, dk_gain: head_dim each, summed over tokens and heads, overwritten.
+ * workspace: himuon_qk_norm_rope_grad_workspace_size(batch, seq, head_dim) bytes,
+ * 16-byte aligned.
+ */
+size_t himuon_qk_norm_rope_grad_workspace_size(int64_t batch, int64_t seq, int64_t head_dim);
+
+int himuon_qk_norm_rope_grad(const himuon_qk_t* args, const himuon_heads_t* g_q, const himuon_heads_t* g_k,
+                             const himuon_heads_t* q, const himuon_heads_t* k,
+                             const himuon_heads_t* dq, const himuon_heads_t* dk, void* dq_gain, void* dk_gain,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Tokens of one column that share an exponent in an 8-bit activation. */
+#define HIMUON_ACT_GROUP 32
+
+/*
+ * Activations in 8 bits, for the backward pass: an n_tokens x cols matrix becomes
+ *   codes      [ceil(n_tokens / 32)][cols][32] bytes, 8-bit floats (4 exponent
+ *              bits, 3 mantissa bits, no infinity; 0x7f is NaN), and
+ *   exponents  [ceil(n_tokens / 32)][cols] bytes c,
+ * standing for code * 2^(c - 127). 32 tokens of a column share an exponent: the
+ * least e with max |x| <= 448 * 2^e, within -100 .. 119; codes round to nearest
+ * even. The tokens that fill the last group up are zeros. Infinities and NaN
+ * become NaN and do not count towards the maximum.
+ *
+ * A weight gradient sums over tokens, so a group lies along its sum and a column's
+ * outliers do not cost the others precision. Values held so are exact in bf16.
+ *
+ * codes: 16-byte aligned. x (n_tokens x cols, ld >= cols): storage `dtype`.
+ */
+int himuon_act_pack(int64_t n_tokens, int64_t cols, const void* x, int64_t ld, int dtype,
+                    void* codes, void* exponents, void* stream);
+
+/* The values of an activation in 8 bits, as storage `dtype` (exact). */
+int himuon_act_unpack(int64_t n_tokens, int64_t cols, const void* codes, const void* exponents,
+                      void* x, int64_t ld, int dtype, void* stream);
+
+/*
+ * The gradient of an out x cols weight matrix from the gradient of its outputs and
+ * its inputs held in 8 bits:
+ *     dweight[o, i] (+)= sum over tokens t of grad[t, o] * x[t, i],
+ * added to dweight if accumulate != 0. bf16 gradients are exact operands of the
+ * matrix cores; fp32 ones are taken as three bf16 terms, which hold all 24 bits.
+ * Products are exact and accumulated in fp32.
+ *
+ * grad       n_tokens x out, storage `dtype`, ld_grad >= out.
+ * dweight    out x cols, storage `out_dtype`, ld_dweight >= cols; may be what
+ *            himuon_step takes as a gradient.
+ * workspace  himuon_weight_grad_workspace_size(...) bytes (0: invalid sizes),
+ *            256-byte aligned.
+ */
+size_t himuon_weight_grad_workspace_size(int64_t n_tokens, int64_t out, int64_t cols, int dtype);
+
+int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, const void* grad, int64_t ld_grad, int dtype,
+                       const void* codes, const void* exponents, void* dweight, int64_t ld_dweight, int out_dtype,
+                       int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static English text for a status code. */
 const char* himuon_status_string(int status);
 

@@ -9,7 +9,10 @@ there is no fallback implementation.
 Low-level names mirror the C ABI (``himuon_ns_tiled``, ``himuon_plan_chunks``,
 ``himuon_ns_tiled_workspace_size``, ``himuon_select_compute``,
 ``himuon_status_string``, ``himuon_last_hip_error``, ``himuon_version``);
-``ns_tiled`` is the tensor-level convenience wrapper.
+``ns_tiled`` is the tensor-level convenience wrapper. The operators of a training
+step around the optimizer (``embed``, ``embed_grad``, ``qk_norm_rope``,
+``qk_norm_rope_grad``, ``act_pack``, ``act_unpack``, ``weight_grad``) are in
+``train_ops``.
 """
 from __future__ import annotations
 
@@ -115,6 +118,7 @@ def lib():
         L.himuon_version.restype = ctypes.c_int
         L.himuon_calib_mfma.argtypes = [ctypes.c_int, vp, vp, ctypes.c_int, ctypes.c_int, vp]
         L.himuon_calib_mfma.restype = ctypes.c_int
+        train_ops.declare(L)
         _lib = L
     return _lib
 
@@ -765,3 +769,8 @@ class HiMuon:
             _keep_alive([self._workspace] + self.moms, stream, self._workspace.device)
             self._streams.add(stream)
         return self.params
+
+
+from . import train_ops  # noqa: E402  (takes the error type and the checks above)
+from .train_ops import (act_pack, act_unpack, embed, embed_grad, qk_norm_rope,  # noqa: E402,F401
+                        qk_norm_rope_grad, weight_grad)

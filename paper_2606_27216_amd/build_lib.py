@@ -38,6 +38,9 @@ SOURCES = [
     ("ns_gemm_kernels.hip", []),
     ("ns_block_gemm.hip", []),
     ("optim_kernels.hip", []),
+    ("embed_ops.hip", []),
+    ("qk_norm_rope.hip", []),
+    ("act8_ops.hip", []),
     ("himuon_api.cpp", []),
     ("ns_gemm_path.cpp", []),
     ("himuon_step.cpp", []),

@@ -1,0 +1,479 @@
+// Per-head norms of queries and keys with the position rotation, and the backward
+// pass (himuon_qk_norm_rope, himuon_qk_norm_rope_grad).
+//
+// For a head's vector x of D elements, r = (mean x^2 + eps)^(-1/2), gain w:
+//     z = r x w,  y = R z           R turns the pairs of the position's angles
+//     dz = R^T dy,  dw = sum over tokens and heads of dz r x,
+//     dx = r (dz w - x r^2 mean(dz w x))
+// so one pass over x (and dy) is all there is to read: both sums over a head are
+// taken at once, and r is computed again in the backward pass.
+//
+// A head is 8 pairs to a lane: L lanes hold it, a wave 64 / L heads of one token. The
+// two elements of a pair sit in one lane, so the rotation needs no exchange, and a
+// token's cosines and sines and the gains stay in registers while the wave walks
+// over its heads. Memory bounds it.
+#include "elementwise8.h"
+#include "train_ops.h"
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+namespace himuon {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+struct Strided {
+    uint8_t* ptr;
+    int64_t sb, ss, sh;
+};
+
+struct QkArgs {
+    Strided q, k, qo, ko, gq, gk;  // forward: inputs, outputs; backward: inputs, their gradients, the outputs' gradients
+    const void *wq, *wk;
+    const float *cs, *sn;
+    const void* positions;
+    float* part;                   // backward: [blocks][2][D]
+    int64_t tokens, seq, table_rows, units;
+    int32_t hq, hk, dim, rot, wide, parts, gain_bf16;
+    float eps, inv_dim;
+};
+
+// Sum over the L lanes of a head (L consecutive lanes, a power of two).
+template <int L> __device__ __forceinline__ float head_sum(float v)
+{
+    auto dpp = [](float x, auto ctrl) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    if constexpr (L >= 2) v += dpp(v, std::integral_constant<int, 0xB1>{});   // lane ^ 1
+    if constexpr (L >= 4) v += dpp(v, std::integral_constant<int, 0x4E>{});   // lane ^ 2
+    if constexpr (L >= 8) v += dpp(v, std::integral_constant<int, 0x141>{});  // the other four of eight
+    if constexpr (L >= 16) v += dpp(v, std::integral_constant<int, 0x140>{}); // the other eight of sixteen
+    if constexpr (L >= 32) v += __shfl_xor(v, 16);
+    return v;
+}
+
+// Where the eight pairs of a lane lie in a head: first elements a, a + 1, .., second
+// ones b, b + 1, ..; or (INTER) 16 elements from a on, pairs side by side.
+struct Place {
+    int a, b, pair, n;  // n: pairs that exist
+};
+
+template <bool INTER> __device__ __forceinline__ Place place(int pair, int dim, int rot)
+{
+    Place w;
+    w.pair = pair;
+    w.n = max(0, min(8, dim / 2 - pair));
+    if (INTER) {
+        w.a = 2 * pair;
+        w.b = 2 * pair + 1;
+    } else if (pair < rot / 2) {
+        w.a = pair;
+        w.b = rot / 2 + pair;
+    } else {
+        w.a = rot + (pair - rot / 2);
+        w.b = w.a + (dim - rot) / 2;
+    }
+    return w;
+}
+
+// A lane's eight pairs: first and second elements.
+struct Pairs {
+    f32x8 u, v;
+};
+
+// The lane's pairs of the vector at base + i. (VEC: eight whole pairs in runs of
+// elements; lanes past the head read its first pairs and get zeros.)
+template <GemmStore ST, bool INTER, bool VEC>
+__device__ __forceinline__ Pairs load_pairs(const void* base, int64_t i, const Place& w, int dim, int rot)
+{
+    Pairs x;
+    if constexpr (VEC) {
+        const bool on = w.n > 0;
+        if constexpr (INTER) {
+            const int a = on ? w.a : 0;
+            const f32x8 lo = get8<ST>(base, i + a), hi = get8<ST>(base, i + a + 8);
+            x.u = f32x8{lo[0], lo[2], lo[4], lo[6], hi[0], hi[2], hi[4], hi[6]};
+            x.v = f32x8{lo[1], lo[3], lo[5], lo[7], hi[1], hi[3], hi[5], hi[7]};
+        } else {
+            x.u = get8<ST>(base, i + (on ? w.a : 0));
+            x.v = get8<ST>(base, i + (on ? w.b : 0));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x.u[e] = on ? x.u[e] : 0.f;
+            x.v[e] = on ? x.v[e] : 0.f;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool on = e < w.n;
+            const Place q = place<INTER>(on ? w.pair + e : 0, dim, rot);
+            const float a = get1<ST>(base, i + q.a), b = get1<ST>(base, i + q.b);
+            x.u[e] = on ? a : 0.f;
+            x.v[e] = on ? b : 0.f;
+        }
+    }
+    return x;
+}
+
+template <GemmStore ST, bool INTER, bool VEC>
+__device__ __forceinline__ void store_pairs(void* base, int64_t i, const Place& w, int dim, int rot, const Pairs& x)
+{
+    if constexpr (VEC) {
+        if (w.n == 0) return;
+        if constexpr (INTER) {
+            put8<ST>(base, i + w.a, f32x8{x.u[0], x.v[0], x.u[1], x.v[1], x.u[2], x.v[2], x.u[3], x.v[3]});
+            put8<ST>(base, i + w.a + 8, f32x8{x.u[4], x.v[4], x.u[5], x.v[5], x.u[6], x.v[6], x.u[7], x.v[7]});
+        } else {
+            put8<ST>(base, i + w.a, x.u);
+            put8<ST>(base, i + w.b, x.v);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (e < w.n) {
+                const Place q = place<INTER>(w.pair + e, dim, rot);
+                put1<ST>(base, i + q.a, x.u[e]);
+                put1<ST>(base, i + q.b, x.v[e]);
+            }
+        }
+    }
+}
+
+template <bool INTER, bool VEC> __device__ __forceinline__ Pairs load_gains(const QkArgs& p, const void* gain, const Place& w)
+{
+    if (p.gain_bf16) return load_pairs<GemmStore::BF16, INTER, VEC>(gain, 0, w, p.dim, p.rot);
+    return load_pairs<GemmStore::F32, INTER, VEC>(gain, 0, w, p.dim, p.rot);
+}
+
+// The lane's cosines (u) and sines (v) of position t: 1 and 0 for what is not rotated.
+__device__ __forceinline__ Pairs load_turn(const QkArgs& p, int64_t t, const Place& w)
+{
+    const int half = p.rot / 2;
+    const int64_t i = t * half + w.pair;
+    Pairs x;
+    x.u = f32x8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    x.v = f32x8{};
+    if (w.pair + 8 <= half) {
+        x.u = get8<GemmStore::F32>(p.cs, i);
+        x.v = get8<GemmStore::F32>(p.sn, i);
+    } else if (w.pair < half) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (w.pair + e < half) {
+                x.u[e] = p.cs[i + e];
+                x.v[e] = p.sn[i + e];
+            }
+        }
+    }
+    return x;
+}
+
+// The position of a token; false if it lies outside the table.
+__device__ __forceinline__ bool token_position(const QkArgs& p, int64_t token, int64_t s, int64_t& t)
+{
+    t = p.positions ? load_index(p.positions, token, p.wide != 0) : s;
+    const bool in = t >= 0 && t < p.table_rows;
+    if (!in) t = 0;
+    return in;
+}
+
+// x -> R (r x w) for the heads of one token that fall to this wave.
+template <GemmStore ST, bool INTER, bool VEC, int L>
+__device__ __forceinline__ void forward_heads(const QkArgs& p, const Strided& in, const Strided& out, const void* gain, int heads,
+                                              int part, int64_t b, int64_t s, bool used, const Place& w, const Pairs& turn)
+{
+    constexpr int G = 64 / L;
+    const int lane = threadIdx.x & 63;
+    const Pairs g = load_gains<INTER, VEC>(p, gain, w);
+    const int64_t bi = b * in.sb + s * in.ss, bo = b * out.sb + s * out.ss;
+    for (int h = part * G + lane / L; h < heads; h += p.parts * G) {
+        Pairs x = load_pairs<ST, INTER, VEC>(in.ptr, bi + h * in.sh, w, p.dim, p.rot);
+        float sq = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sq += x.u[e] * x.u[e] + x.v[e] * x.v[e];
+        const float r = rsqrtf(head_sum<L>(sq) * p.inv_dim + p.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float z0 = x.u[e] * r * g.u[e], z1 = x.v[e] * r * g.v[e];
+            x.u[e] = used ? z0 * turn.u[e] - z1 * turn.v[e] : 0.f;
+            x.v[e] = used ? z1 * turn.u[e] + z0 * turn.v[e] : 0.f;
+        }
+        store_pairs<ST, INTER, VEC>(out.ptr, bo + h * out.sh, w, p.dim, p.rot, x);
+    }
+}
+
+template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bounds__(kThreads) qk_forward(const QkArgs p)
+{
+    const int64_t unit = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (unit >= p.units) return;
+    const int64_t token = unit / p.parts;
+    const int part = (int)(unit - token * p.parts);
+    const int64_t b = token / p.seq, s = token - b * p.seq;
+    const Place w = place<INTER>(8 * (threadIdx.x & (L - 1)), p.dim, p.rot);
+    int64_t t;
+    const bool used = token_position(p, token, s, t);
+    Pairs turn{};
+    if (used) turn = load_turn(p, t, w);
+    forward_heads<ST, INTER, VEC, L>(p, p.q, p.qo, p.wq, p.hq, part, b, s, used, w, turn);
+    forward_heads<ST, INTER, VEC, L>(p, p.k, p.ko, p.wk, p.hk, part, b, s, used, w, turn);
+}
+
+template <GemmStore ST, bool INTER, bool VEC, int L>
+__device__ __forceinline__ void backward_heads(const QkArgs& p, const Strided& in, const Strided& grad, const Strided& out,
+                                               const Pairs& g, int heads, int64_t b, int64_t s, bool used, const Place& w,
+                                               const Pairs& turn, Pairs& d)
+{
+    constexpr int G = 64 / L;
+    const int lane = threadIdx.x & 63;
+    const int64_t bi = b * in.sb + s * in.ss, bg = b * grad.sb + s * grad.ss, bo = b * out.sb + s * out.ss;
+    for (int h = lane / L; h < heads; h += G) {
+        Pairs x = load_pairs<ST, INTER, VEC>(in.ptr, bi + h * in.sh, w, p.dim, p.rot);
+        Pairs y = load_pairs<ST, INTER, VEC>(grad.ptr, bg + h * grad.sh, w, p.dim, p.rot);
+        float sq = 0.f, dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float a = y.u[e] * turn.u[e] + y.v[e] * turn.v[e], c = y.v[e] * turn.u[e] - y.u[e] * turn.v[e];
+            y.u[e] = a;  // dz
+            y.v[e] = c;
+            sq += x.u[e] * x.u[e] + x.v[e] * x.v[e];
+            dot += a * g.u[e] * x.u[e] + c * g.v[e] * x.v[e];
+        }
+        sq = head_sum<L>(sq);
+        dot = head_sum<L>(dot);
+        const float r = rsqrtf(sq * p.inv_dim + p.eps);
+        const float m = r * r * (dot * p.inv_dim);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            d.u[e] += used ? y.u[e] * (x.u[e] * r) : 0.f;
+            d.v[e] += used ? y.v[e] * (x.v[e] * r) : 0.f;
+            x.u[e] = used ? r * (y.u[e] * g.u[e] - x.u[e] * m) : 0.f;
+            x.v[e] = used ? r * (y.v[e] * g.v[e] - x.v[e] * m) : 0.f;
+        }
+        store_pairs<ST, INTER, VEC>(out.ptr, bo + h * out.sh, w, p.dim, p.rot, x);
+    }
+}
+
+// A wave takes tokens `units` apart; its sums for the gains stay in registers until
+// the end, when the block adds its own up in LDS and leaves one row of partial sums.
+template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bounds__(kThreads) qk_backward(const QkArgs p)
+{
+    __shared__ float sums[kWaves][2][L * 16];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place w = place<INTER>(8 * (threadIdx.x & (L - 1)), p.dim, p.rot);
+    const Pairs gq = load_gains<INTER, VEC>(p, p.wq, w), gk = load_gains<INTER, VEC>(p, p.wk, w);
+    Pairs dq{}, dk{};
+    for (int64_t token = (int64_t)blockIdx.x * kWaves + wave; token < p.tokens; token += p.units) {
+        const int64_t b = token / p.seq, s = token - b * p.seq;
+        int64_t t;
+        const bool used = token_position(p, token, s, t);
+        Pairs turn{};
+        if (used) turn = load_turn(p, t, w);
+        backward_heads<ST, INTER, VEC, L>(p, p.q, p.gq, p.qo, gq, p.hq, b, s, used, w, turn, dq);
+        backward_heads<ST, INTER, VEC, L>(p, p.k, p.gk, p.ko, gk, p.hk, b, s, used, w, turn, dk);
+    }
+    const int l = lane & (L - 1);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float v[4] = {dq.u[e], dq.v[e], dk.u[e], dk.v[e]};
+#pragma unroll
+        for (int o = L; o < 64; o <<= 1) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v[x] += __shfl_xor(v[x], o);
+        }
+        if (lane < L) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) sums[wave][x >> 1][16 * l + 2 * e + (x & 1)] = v[x];
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * p.dim; i += kThreads) {
+        const int which = i >= p.dim, x = i - which * p.dim;  // element x of the pairs' order
+        float v = 0.f;
+#pragma unroll
+        for (int wv = 0; wv < kWaves; ++wv) v += sums[wv][which][x];
+        const Place q = place<INTER>(x >> 1, p.dim, p.rot);
+        p.part[(int64_t)blockIdx.x * 2 * p.dim + which * p.dim + (x & 1 ? q.b : q.a)] = v;
+    }
+}
+
+// Sums of the blocks' rows for 64 of the 2 D columns, the rows shared out over the waves.
+constexpr int kSumThreads = 1024;
+template <GemmStore GT> __global__ void __launch_bounds__(kSumThreads) gain_sums(const float* part, int rows, int dim, void* dq, void* dk)
+{
+    constexpr int W = kSumThreads / 64;
+    __shared__ float sums[W][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = blockIdx.x * 64 + lane;
+    float v[4] = {};
+    if (col < 2 * dim) {
+        int r = wave;
+        for (; r + 3 * W < rows; r += 4 * W) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += part[(int64_t)(r + j * W) * 2 * dim + col];
+        }
+        for (; r < rows; r += W) v[0] += part[(int64_t)r * 2 * dim + col];
+    }
+    sums[wave][lane] = (v[0] + v[1]) + (v[2] + v[3]);
+    __syncthreads();
+    if (wave > 0 || col >= 2 * dim) return;
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) t += sums[w][lane];
+    if (col < dim) put1<GT>(dq, col, t);
+    else put1<GT>(dk, col - dim, t);
+}
+
+// ---------------------------------------------------------------- host side
+
+// Blocks of the backward pass, and rows of partial sums.
+int64_t grad_blocks(int64_t tokens) { return std::max<int64_t>(1, std::min<int64_t>(ceil_div(tokens, kWaves), 1024)); }
+
+template <bool BWD, GemmStore ST, bool INTER, bool VEC, int L> int launch_l(QkArgs p, hipStream_t stream)
+{
+    if constexpr (BWD) {
+        const int64_t blocks = grad_blocks(p.tokens);
+        p.units = blocks * kWaves;
+        hipLaunchKernelGGL((qk_backward<ST, INTER, VEC, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
+    } else {
+        // few tokens: a token's heads are shared out over several waves
+        const int64_t groups = ceil_div(std::max(p.hq, p.hk), 64 / L);
+        p.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(groups, 4096 / std::max<int64_t>(1, p.tokens)));
+        p.units = p.tokens * p.parts;
+        const int64_t blocks = ceil_div(p.units, kWaves);
+        if (blocks > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+        hipLaunchKernelGGL((qk_forward<ST, INTER, VEC, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
+    }
+    return launch_status();
+}
+
+template <bool BWD, GemmStore ST, bool INTER, bool VEC> int launch_vec(const QkArgs& p, hipStream_t stream)
+{
+    if (p.dim <= 64) return launch_l<BWD, ST, INTER, VEC, 4>(p, stream);
+    if (p.dim <= 128) return launch_l<BWD, ST, INTER, VEC, 8>(p, stream);
+    if (p.dim <= 256) return launch_l<BWD, ST, INTER, VEC, 16>(p, stream);
+    return launch_l<BWD, ST, INTER, VEC, 32>(p, stream);
+}
+
+template <bool BWD, GemmStore ST> int launch_st(const QkArgs& p, bool inter, hipStream_t stream)
+{
+    // whole groups of eight pairs in every lane, on one side of the rotated part
+    const bool vec = p.dim % 16 == 0 && (inter || p.rot % 16 == 0);
+    if (inter) return vec ? launch_vec<BWD, ST, true, true>(p, stream) : launch_vec<BWD, ST, true, false>(p, stream);
+    return vec ? launch_vec<BWD, ST, false, true>(p, stream) : launch_vec<BWD, ST, false, false>(p, stream);
+}
+
+template <bool BWD> int launch_qk(const QkArgs& p, const himuon_qk_t* a, hipStream_t stream)
+{
+    const bool inter = a->interleaved != 0;
+    return a->dtype == HIMUON_BF16 ? launch_st<BWD, GemmStore::BF16>(p, inter, stream)
+                                   : launch_st<BWD, GemmStore::F32>(p, inter, stream);
+}
+
+int check_args(const himuon_qk_t* a)
+{
+    if (!a || a->batch < 0 || a->seq < 0 || a->q_heads < 1 || a->k_heads < 1) return HIMUON_ERR_INVALID_ARG;
+    if (a->head_dim < 2 || a->head_dim % 2 || a->rot_dim < 0 || a->rot_dim % 2 || a->rot_dim > a->head_dim)
+        return HIMUON_ERR_INVALID_ARG;
+    if (!known_dtype(a->dtype) || !known_dtype(a->gain_dtype) || !known_index(a->index)) return HIMUON_ERR_INVALID_ARG;
+    if (!a->q_gain || !a->k_gain || a->table_rows < 0 || !(a->eps >= 0.f) || !std::isfinite(a->eps))
+        return HIMUON_ERR_INVALID_ARG;
+    if (a->rot_dim > 0 && a->table_rows > 0 && (!a->cos_table || !a->sin_table)) return HIMUON_ERR_INVALID_ARG;
+    if (a->head_dim > HIMUON_MAX_HEAD_DIM) return HIMUON_ERR_UNSUPPORTED;
+    if (a->batch > INT32_MAX || a->seq > INT32_MAX || a->table_rows > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    if (a->batch * a->seq > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    return HIMUON_OK;
+}
+
+bool set(Strided& s, const himuon_heads_t* h)
+{
+    if (!h || !h->ptr) return false;
+    s.ptr = static_cast<uint8_t*>(h->ptr);
+    s.sb = h->stride_batch;
+    s.ss = h->stride_seq;
+    s.sh = h->stride_head;
+    return true;
+}
+
+QkArgs common(const himuon_qk_t* a)
+{
+    QkArgs p{};
+    p.wq = a->q_gain;
+    p.wk = a->k_gain;
+    p.cs = a->cos_table;
+    p.sn = a->sin_table;
+    p.positions = a->positions;
+    p.tokens = a->batch * a->seq;
+    p.seq = a->seq;
+    p.table_rows = a->table_rows;
+    p.hq = a->q_heads;
+    p.hk = a->k_heads;
+    p.dim = a->head_dim;
+    p.rot = a->rot_dim;
+    p.wide = a->index == HIMUON_I64;
+    p.gain_bf16 = a->gain_dtype == HIMUON_BF16;
+    p.parts = 1;
+    p.eps = a->eps;
+    p.inv_dim = 1.f / (float)a->head_dim;
+    return p;
+}
+
+}  // namespace
+}  // namespace himuon
+
+extern "C" int himuon_qk_norm_rope(const himuon_qk_t* args, const himuon_heads_t* q, const himuon_heads_t* k,
+                                   const himuon_heads_t* q_out, const himuon_heads_t* k_out, void* stream)
+{
+    using namespace himuon;
+    const int st = check_args(args);
+    if (st != HIMUON_OK) return st;
+    if (args->batch == 0 || args->seq == 0) return HIMUON_OK;
+    QkArgs p = common(args);
+    if (!set(p.q, q) || !set(p.k, k) || !set(p.qo, q_out) || !set(p.ko, k_out)) return HIMUON_ERR_INVALID_ARG;
+    StreamDevice on(stream);
+    if (on.status != HIMUON_OK) return on.status;
+    return launch_qk<false>(p, args, static_cast<hipStream_t>(stream));
+}
+
+extern "C" size_t himuon_qk_norm_rope_grad_workspace_size(int64_t batch, int64_t seq, int64_t head_dim)
+{
+    using namespace himuon;
+    if (batch < 0 || seq < 0 || head_dim < 2 || head_dim > HIMUON_MAX_HEAD_DIM) return 0;
+    if (batch > INT32_MAX || seq > INT32_MAX || batch * seq > INT32_MAX) return 0;
+    return round_up((size_t)grad_blocks(batch * seq) * 2 * (size_t)head_dim * sizeof(float), 256);
+}
+
+extern "C" int himuon_qk_norm_rope_grad(const himuon_qk_t* args, const himuon_heads_t* g_q, const himuon_heads_t* g_k,
+                                        const himuon_heads_t* q, const himuon_heads_t* k, const himuon_heads_t* dq,
+                                        const himuon_heads_t* dk, void* dq_gain, void* dk_gain, void* workspace,
+                                        size_t workspace_bytes, void* stream)
+{
+    using namespace himuon;
+    int st = check_args(args);
+    if (st != HIMUON_OK) return st;
+    if (!dq_gain || !dk_gain) return HIMUON_ERR_INVALID_ARG;
+    QkArgs p = common(args);
+    // (without a token there is nothing to read: the gains' gradients become zero)
+    if (p.tokens > 0 && (!set(p.gq, g_q) || !set(p.gk, g_k) || !set(p.q, q) || !set(p.k, k) || !set(p.qo, dq) || !set(p.ko, dk)))
+        return HIMUON_ERR_INVALID_ARG;
+    if (!workspace || ((uintptr_t)workspace & 15) ||
+        workspace_bytes < himuon_qk_norm_rope_grad_workspace_size(args->batch, args->seq, args->head_dim))
+        return HIMUON_ERR_WORKSPACE;
+    p.part = static_cast<float*>(workspace);
+    StreamDevice on(stream);
+    if (on.status != HIMUON_OK) return on.status;
+    const hipStream_t hs = static_cast<hipStream_t>(stream);
+    st = launch_qk<true>(p, args, hs);
+    if (st != HIMUON_OK) return st;
+    const int rows = (int)grad_blocks(p.tokens);
+    const dim3 grid((unsigned)ceil_div(2 * p.dim, 64));
+    if (args->gain_dtype == HIMUON_BF16)
+        hipLaunchKernelGGL(gain_sums<GemmStore::BF16>, grid, dim3(kSumThreads), 0, hs, p.part, rows, p.dim, dq_gain, dk_gain);
+    else
+        hipLaunchKernelGGL(gain_sums<GemmStore::F32>, grid, dim3(kSumThreads), 0, hs, p.part, rows, p.dim, dq_gain, dk_gain);
+    return launch_status();
+}

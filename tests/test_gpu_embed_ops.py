@@ -1,0 +1,238 @@
+"""embed and embed_grad against their definition in 64 bits.
+
+Bounds, u = 2^-24: the lookup is one fp32 product and one rounding to the type; a
+gradient row is a sum of k terms in fp32, k u sum|term| at most whatever the order,
+one product, one addition (accumulate) and one rounding to the type (bf16, of 8
+significant bits: 2^-8 of the value)."""
+import pytest
+
+import paper_2606_27216_amd as hm
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+ROUND = {"f32": 2 * U, "bf16": 2.0 ** -8 + 2 * U}
+
+
+def _dt(name):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16}[name]
+
+
+def _rand(shape, dtype, seed, scale=1.0):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return (scale * torch.randn(*shape, generator=gen, device="cuda")).to(_dt(dtype))
+
+
+def _ids(n, rows, seed, kind="mixed", index="i64"):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    t = torch.randint(0, rows, (n,), generator=gen, device="cuda")
+    if kind == "mixed":  # many repeats, some outside the table
+        t = torch.where(torch.rand(n, generator=gen, device="cuda") < 0.4, t % 3, t)
+        t = torch.where(torch.rand(n, generator=gen, device="cuda") < 0.1, -1 - t, t)
+        t = torch.where(torch.rand(n, generator=gen, device="cuda") < 0.05, rows + t, t)
+    elif kind == "one":
+        t = torch.full_like(t, rows // 2)
+    elif kind == "none":
+        t = torch.full_like(t, -1)
+    return t.to(torch.int32 if index == "i32" else torch.int64)
+
+
+def _exact_grad(tokens, grad, rows, scale):
+    """(the sum in 64 bits, the sum of the terms' sizes, the number of terms) of each row"""
+    import torch
+    t = tokens.long()
+    ok = (t >= 0) & (t < rows)
+    g = grad.double()[ok] * scale
+    out = torch.zeros(2, rows, grad.shape[1], dtype=torch.float64, device="cuda")
+    out[0].index_put_((t[ok],), g, accumulate=True)
+    out[1].index_put_((t[ok],), g.abs(), accumulate=True)
+    return out[0], out[1], torch.bincount(t[ok], minlength=rows).double()[:, None]
+
+
+def _check_grad(got, tokens, grad, rows, scale, dtype, base=None):
+    s, a, k = _exact_grad(tokens, grad, rows, scale)
+    if base is not None:
+        s, a = s + base.double(), a + base.double().abs()
+    bound = (k + 3) * U * a + ROUND[dtype] * s.abs()
+    err = (got.double() - s).abs()
+    assert bool((err <= bound).all()), float((err - bound).max())
+
+
+@pytest.mark.parametrize("n,rows,width", [(1, 1, 1), (5, 7, 3), (33, 50, 64), (257, 1000, 100), (64, 300, 513), (3, 11, 4096),
+                                          (5000, 400, 2560), (1, 32000, 4099)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_lookup(n, rows, width, dtype):
+    import torch
+    table = _rand((rows, width), dtype, 1)
+    for index, scale in (("i64", 1.0), ("i32", 45.25)):
+        tokens = _ids(n, rows, 2, index=index)
+        print(f"[gpu-case] embed {n} {rows} {width} {dtype} {index}", flush=True)
+        got = hm.embed(tokens, table, scale=scale)
+        ok = (tokens >= 0) & (tokens < rows)
+        want = torch.where(ok[:, None], table.double()[tokens.long().clamp(0, rows - 1)] * scale, 0.0)
+        assert bool(((got.double() - want).abs() <= ROUND[dtype] * want.abs()).all())
+        if scale == 1.0:
+            assert torch.equal(got.double(), want)
+
+
+def test_lookup_strides_shapes_and_no_tokens():
+    import torch
+    wide = _rand((40, 101), "bf16", 3)
+    table = wide[:, 1:98]  # rows at odd addresses
+    tokens = _ids(12, 40, 4, "plain").view(3, 4)
+    got = hm.embed(tokens, table)
+    assert got.shape == (3, 4, 97) and torch.equal(got, table[tokens])
+    space = torch.full((12, 130), 7.0, dtype=torch.bfloat16, device="cuda")
+    hm.embed(tokens, table, out=space[:, 3:100])
+    assert torch.equal(space[:, 3:100], table[tokens.view(-1)])
+    assert bool((space[:, :3] == 7).all()) and bool((space[:, 100:] == 7).all())
+    assert hm.embed(tokens[:0], table).shape == (0, 4, 97)
+
+
+def test_lookup_past_32_bits():
+    """Rows whose elements lie beyond 2^31."""
+    import torch
+    rows, width = 540000, 4096
+    table = torch.empty(rows, width, dtype=torch.bfloat16, device="cuda")
+    pick = torch.tensor([0, rows - 1, 524288, 524287, rows // 2], device="cuda")
+    table[pick] = _rand((5, width), "bf16", 5)
+    assert torch.equal(hm.embed(pick, table), table[pick])
+
+
+@pytest.mark.parametrize("n,rows,width", [(1, 1, 1), (2, 2, 8), (100, 37, 3), (1500, 5003, 103), (1025, 1023, 64), (1024, 1024, 512),
+                                          (9000, 70000, 520), (3000, (1 << 20) + 3, 17), (20000, 300, 1032)])
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+def test_gradient(n, rows, width, dtype, out):
+    tokens = _ids(n, rows, 6, index="i32" if n % 2 else "i64")
+    grad = _rand((n, width), dtype, 7)
+    print(f"[gpu-case] embed_grad {n} {rows} {width} {dtype} {out}", flush=True)
+    got = hm.embed_grad(tokens, grad, rows, scale=1.5, dtype=_dt(out))
+    _check_grad(got, tokens, grad, rows, 1.5, out)
+
+
+@pytest.mark.parametrize("kind", ["one", "none", "mixed"])
+@pytest.mark.parametrize("n", [31, 4097, 40000])
+def test_gradient_of_extreme_batches(kind, n):
+    """A batch of one token alone (a sum over every chunk), and one of padding alone,
+    whose rows, infinities and NaN must not be seen."""
+    import torch
+    rows, width = 129, 260
+    tokens, grad = _ids(n, rows, 8, kind), _rand((n, width), "bf16", 9)
+    if kind == "none":
+        grad[0] = float("nan")
+        grad[-1] = float("inf")
+    got = hm.embed_grad(tokens, grad, rows, dtype=torch.float32)
+    if kind == "none":
+        assert bool((got == 0).all())
+    else:
+        _check_grad(got, tokens, grad, rows, 1.0, "f32")
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_gradient_accumulates_into_strided_rows(out):
+    import torch
+    n, rows, width = 700, 90, 75
+    tokens, grad = _ids(n, rows, 10), _rand((n, width + 6), "bf16", 11)[:, 5:5 + width]
+    space = _rand((rows, width + 4), out, 12)
+    before = space.clone()
+    hm.embed_grad(tokens, grad, rows, out=space[:, 1:1 + width], accumulate=True)
+    assert torch.equal(space[:, 0], before[:, 0]) and torch.equal(space[:, 1 + width:], before[:, 1 + width:])
+    _check_grad(space[:, 1:1 + width], tokens, grad, rows, 1.0, out, base=before[:, 1:1 + width])
+    hm.embed_grad(tokens, grad, rows, out=space[:, 1:1 + width])  # overwritten, not added to
+    _check_grad(space[:, 1:1 + width], tokens, grad, rows, 1.0, out)
+
+
+def test_gradient_of_no_tokens():
+    import torch
+    t = torch.empty(0, dtype=torch.int64, device="cuda")
+    g = torch.empty(0, 33, device="cuda")
+    out = torch.ones(10, 33, device="cuda")
+    hm.embed_grad(t, g, 10, out=out, accumulate=True)
+    assert bool((out == 1).all())
+    hm.embed_grad(t, g, 10, out=out)
+    assert bool((out == 0).all())
+
+
+def test_gradient_is_the_same_from_call_to_call_and_nan_stays_in_its_row():
+    import torch
+    n, rows, width = 30000, 500, 300
+    tokens, grad = _ids(n, rows, 13), _rand((n, width), "bf16", 14)
+    first = hm.embed_grad(tokens, grad, rows, dtype=torch.float32)
+    for _ in range(3):
+        assert torch.equal(first, hm.embed_grad(tokens, grad, rows, dtype=torch.float32))
+    i = int((tokens == 77).nonzero()[0])
+    grad[i, 5] = float("nan")
+    got = hm.embed_grad(tokens, grad, rows, dtype=torch.float32)
+    bad = torch.isnan(got)
+    assert int(bad.sum()) == 1 and bool(bad[77, 5])
+    assert torch.equal(torch.where(bad, first, got), first)
+
+
+def test_gradient_against_differences():
+    """The lookup is linear: its change along a direction is the gradient's product with it."""
+    import torch
+    rows, width, n = 300, 130, 2000
+    tokens = _ids(n, rows, 15)
+    d, g = _rand((rows, width), "f32", 16), _rand((n, width), "f32", 17)
+    along = (hm.embed(tokens, d, scale=3.0).double() * g.double()).sum()
+    terms = (hm.embed(tokens, d, scale=3.0).double() * g.double()).abs().sum()
+    inner = (hm.embed_grad(tokens, g, rows, scale=3.0).double() * d.double()).sum()
+    assert abs(float(along - inner)) <= float(terms) * U * (n + 8)
+
+
+def test_streams_and_graph_replay():
+    """Sort, sums and zero rows inside a captured graph, replayed on new contents with
+    other work in between, and on a stream of its own."""
+    import torch
+    n, rows, width = 6000, 777, 264
+    tokens, grad = _ids(n, rows, 18), _rand((n, width), "bf16", 19)
+    out = torch.empty(rows, width, device="cuda")
+    ws = torch.empty(int(hm.lib().himuon_embed_grad_workspace_size(n, rows, width)), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    want = hm.embed_grad(tokens, grad, rows, dtype=torch.float32)
+    got = hm.embed_grad(tokens, grad, rows, dtype=torch.float32, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(want, got)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hm.embed_grad(tokens, grad, rows, out=out, workspace=ws)
+    for k in range(4):
+        tokens.copy_(_ids(n, rows, 30 + k))
+        grad.copy_(_rand((n, width), "bf16", 40 + k))
+        out.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, hm.embed_grad(tokens, grad, rows, dtype=torch.float32))
+
+
+def test_refusals():
+    import torch
+    table, tokens = _rand((10, 8), "f32", 20), torch.zeros(4, dtype=torch.int64, device="cuda")
+    with pytest.raises(ValueError):
+        hm.embed(tokens.cpu(), table)
+    with pytest.raises(ValueError):
+        hm.embed(torch.zeros(8, dtype=torch.int64, device="cuda")[::2], table)
+    with pytest.raises(ValueError):
+        hm.embed(tokens, table.t())
+    with pytest.raises(TypeError):
+        hm.embed(tokens.float(), table)
+    with pytest.raises(TypeError):
+        hm.embed(tokens, table.double())
+    with pytest.raises(ValueError):
+        hm.embed(tokens, table, out=torch.empty(3, 8, device="cuda"))
+    g = _rand((4, 8), "f32", 21)
+    with pytest.raises(ValueError):
+        hm.embed_grad(tokens, g[:3], 10)
+    with pytest.raises(ValueError):
+        hm.embed_grad(tokens, g, 10, accumulate=True)
+    with pytest.raises(ValueError):
+        hm.embed_grad(tokens, g, 10, out=torch.empty(9, 8, device="cuda"))
+    with pytest.raises(hm.HimuonError):
+        hm.embed_grad(tokens, g, 0)
+    with pytest.raises(hm.HimuonError) as e:
+        hm.embed_grad(tokens, g, 10, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == hm.ERR_WORKSPACE
