@@ -624,9 +624,11 @@ int himuon_act_unpack(int64_t n_tokens, int64_t cols, const void* codes, const v
  * dweight    out x cols, storage `out_dtype`, ld_dweight >= cols; may be what
  *            himuon_step takes as a gradient.
  * workspace  himuon_weight_grad_workspace_size(...) bytes (0: invalid sizes),
- *            256-byte aligned.
+ *            256-byte aligned. The size depends on grad's type, leading dimension
+ *            and address (16-byte aligned rows of bf16 are read in place).
  */
-size_t himuon_weight_grad_workspace_size(int64_t n_tokens, int64_t out, int64_t cols, int dtype);
+size_t himuon_weight_grad_workspace_size(int64_t n_tokens, int64_t out, int64_t cols, const void* grad, int64_t ld_grad,
+                                         int dtype);
 
 int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, const void* grad, int64_t ld_grad, int dtype,
                        const void* codes, const void* exponents, void* dweight, int64_t ld_dweight, int out_dtype,

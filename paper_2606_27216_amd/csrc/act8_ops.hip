@@ -5,10 +5,12 @@
 // are 8-bit floats with 3 mantissa bits, so code * 2^e has 4 significant bits and is exact
 // in bf16. A group lies along the weight gradient's sum, and a column's 32 codes are
 // adjacent: they are the operand of 32 consecutive terms as they stand in memory.
+#include "lds_dma.h"
 #include "ns_device.h"
 #include "train_ops.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace himuon {
 namespace {
@@ -173,96 +175,410 @@ __global__ void __launch_bounds__(kThreads) act_unpack(const uint8_t* codes, con
 
 // ------------------------------------------------------------ weight gradient
 
+// dweight = grad^T x: tokens are the sum's index. A workgroup owns a BM x BN tile of the
+// result and walks over the tokens in slices of 32, one group of codes. Both operands go
+// to LDS as they lie in memory, by DMA (global_load_lds) into a ring of NS slices with
+// one barrier a slice:
+//   - the gradient, 32 rows of BM bf16, in panels of 64 columns; ds_read_b64_tr_b16
+//     turns 4 tokens x 16 columns on the way to the registers, so no pass transposes it;
+//   - the codes, a column's 32 bytes, 16 of them to a lane: no transposition at all;
+//   - the exponents, a byte a column.
+// A wave widens codes to bf16 between the products, two to an instruction and the
+// exponent applied by the same one; that is exact. The k index of a product is permuted
+// alike in both operands: lane half h has tokens 16 h .. 16 h + 15 of the slice.
+//
+// An fp32 gradient, or one whose rows do not start on 16 bytes, is first laid out in the
+// workspace as slices of bf16 rows, fp32 as three terms that follow each other (the
+// codes' slice is then read three times in a row, from cache).
 struct WgradArgs {
-    const void* grad;
+    const uint16_t* a;           // gradient, or its terms in the workspace
     const uint8_t *codes, *exps;
     void* out;
-    int64_t tokens, ld_grad, ld_out;
-    int32_t rows, cols, accumulate;
+    float* part;                 // [splits][rows][part_pitch] partial sums (splits > 1)
+    int64_t lda, lde, ld_out, part_pitch;
+    int32_t rows, cols;
+    int32_t a_cols;              // columns of `a`, a multiple of 8
+    int32_t slices, terms;       // slices in all; consecutive ones that share their codes
+    int32_t tail;                // rows of the last slice, if fewer than 32 (else 0)
+    int32_t splits, ti, tj, accumulate;
 };
 
-// 64 x 64 tiles, 32 tokens at a time through LDS: the gradient's columns turned so that
-// tokens are adjacent (fp32: three bf16 terms of eight bits each), the codes widened.
-template <GemmStore ST, GemmStore OT> __global__ void __launch_bounds__(kThreads) wgrad_tile(const WgradArgs p)
+// Four consecutive results from column j on, of which n exist.
+template <GemmStore OT> HM_DEV void put_result(void* out, int64_t i, int n, bool accumulate, f32x4 v)
+{
+    if (accumulate) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n) v[e] += get1<OT>(out, i + e);
+    }
+    if (n == 4) {
+        if constexpr (OT == GemmStore::BF16)
+            *reinterpret_cast<u32x2_any16*>(static_cast<uint16_t*>(out) + i) =
+                u32x2{pack2<Operand::BF16>(v[0], v[1]), pack2<Operand::BF16>(v[2], v[3])};
+        else
+            *reinterpret_cast<f32x4_any32*>(static_cast<float*>(out) + i) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) put1<OT>(out, i + e, v[e]);
+    }
+}
+
+template <GemmStore OT, int BM, int BN, int WGM, int WGN, int NS, int MINW>
+__global__ void __launch_bounds__(64 * WGM * WGN, MINW) wgrad_blocks(const WgradArgs p)
+{
+    constexpr int W = WGM * WGN;
+    constexpr int RB = BM / 32 / WGM, CB = BN / 32 / WGN;  // 32-blocks of a wave
+    static_assert(RB % 2 == 0, "whole panels to a wave");
+    constexpr int ABYTES = BM * 64, BBYTES = BN * 32;
+    constexpr int STAGE = ABYTES + BBYTES + W * 256;
+    constexpr int AI = BM / 16 / W, BI = BN / 32 / W, NI = AI + BI + 1;  // DMA instructions per wave and slice
+    static_assert(AI * 16 * W == BM && BI * 32 * W == BN, "whole DMA instructions");
+    static_assert((NS - 2) * NI < 64, "the wait's counter");
+    constexpr int PITCH = CB * 128 + 16;  // bytes of a row of results in LDS
+    constexpr int OUT = W * 32 * PITCH;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGE * NS > OUT ? STAGE * NS : OUT];
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 31, lh = lane >> 5, g16 = lane >> 4;
+    const int wi = (wave / WGN) * RB * 32, wj = (wave % WGN) * CB * 32;
+
+    // Workgroups go to the eight XCDs in turn; each XCD gets a contiguous run of tiles, in
+    // bands of four tile rows, so that its tiles share operands in its L2.
+    int split, i0, j0;
+    {
+        const int tiles = p.ti * p.tj, total = tiles * p.splits;
+        const int b = blockIdx.x, x = b & 7, per = total >> 3, rem = total & 7;
+        const int t = x * per + min(x, rem) + (b >> 3);
+        split = t / tiles;
+        int r = t - split * tiles;
+        const int band = r / (4 * p.tj), h = min(4, p.ti - 4 * band);
+        r -= band * 4 * p.tj;
+        const int tj = r / h;
+        i0 = (4 * band + (r - tj * h)) * BM;
+        j0 = tj * BN;
+    }
+    const int s0 = (int)((int64_t)p.slices * split / p.splits), s1 = (int)((int64_t)p.slices * (split + 1) / p.splits);
+    const bool tail = p.tail != 0 && s1 == p.slices;
+    const int nk = s1 - s0 - (tail ? 1 : 0);  // whole slices
+
+    // DMA sources. Gradient: instruction q of a wave fills 8 rows of a panel (128 bytes
+    // each); the 64-byte halves of rows 2, 3, 6, 7, .. change places, so that a
+    // transposing read's four rows lie in different banks. Columns past the last read
+    // the last ones (their results are not stored).
+    uint32_t va[AI], vb[BI];
+    auto a_offset = [&](int q, int rows) -> uint32_t {
+        const int u = q * W + wave;
+        const int row = 8 * (u & 3) + (lane >> 3);
+        const int col = 64 * (u >> 2) + 8 * ((lane & 7) ^ (4 * ((row >> 1) & 1)));
+        return (uint32_t)min(row, rows - 1) * (uint32_t)(p.lda * 2) + 2u * (uint32_t)min(col, p.a_cols - 8 - i0);
+    };
+#pragma unroll
+    for (int q = 0; q < AI; ++q) va[q] = a_offset(q, kGroup);
+#pragma unroll
+    for (int q = 0; q < BI; ++q) {
+        const int col = 32 * (q * W + wave) + li;
+        vb[q] = 32u * (uint32_t)min(col, p.cols - 1 - j0) + 16u * lh;
+    }
+    const int e0 = min(j0 + wj, (int)p.lde - 4);
+    const uint32_t ve = (uint32_t)min(4 * lane, (int)p.lde - 4 - e0);
+    const uint16_t* a_base = p.a + (int64_t)s0 * kGroup * p.lda + i0;
+    const uint8_t* b_base = p.codes + ((int64_t)(s0 / p.terms) * p.cols + j0) * kGroup;
+    const uint8_t* e_base = p.exps + (int64_t)(s0 / p.terms) * p.lde + e0;
+    int term = s0 % p.terms;
+    const uint32_t lds0 = lds_offset(lds);
+    // DMA instruction q of the next slice, into ring buffer `buf`
+    auto issue1 = [&](int buf, int q) {
+        const uint32_t d = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE);
+        if (q < AI) dma16(d + (q * W + wave) * 1024, va[q < AI ? q : 0], uniform_address(a_base));
+        else if (q < AI + BI) dma16(d + ABYTES + ((q - AI) * W + wave) * 1024, vb[q < AI || q >= AI + BI ? 0 : q - AI], uniform_address(b_base));
+        else dma4(d + ABYTES + BBYTES + wave * 256, ve, uniform_address(e_base));
+    };
+    auto advance = [&]() {
+        a_base += (int64_t)kGroup * p.lda;
+        if (++term == p.terms) {
+            term = 0;
+            b_base += (int64_t)p.cols * kGroup;
+            e_base += p.lde;
+        }
+    };
+
+    f32x16 acc[RB][CB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j) acc[i][j] = f32x16{};
+
+    // A slice is two steps of 16 tokens. The operands of a step are read while the step
+    // before it is multiplied.
+    u32x4 fa[2][RB], fb[2][CB], raw[CB];
+    uint32_t scale[CB];
+    const int arow = (16 * lh + ((lane & 15) >> 2)) * 128, acol = 32 * (g16 & 1) + 8 * (lane & 3), aswap = 64 * ((lane >> 3) & 1);
+    const int ra[2] = {arow + (acol ^ aswap), arow + ((acol + 64) ^ aswap)};
+    auto load_a = [&](const uint8_t* ta, int s, int i) __attribute__((always_inline)) {
+        const uint8_t* const t = ta + ((wi >> 6) + (i >> 1)) * 4096 + 1024 * s + ra[i & 1];
+        const u32x2 lo = tr_read(t), hi = tr_read(t + 512);
+        fa[s][i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    };
+    auto load_b = [&](const uint8_t* ta, int j) __attribute__((always_inline)) {
+        raw[j] = *reinterpret_cast<const u32x4*>(ta + ABYTES + (wj / 32 + j) * 1024 + lane * 16);
+        scale[j] = ta[ABYTES + BBYTES + wave * 256 + 32 * j + li];
+    };
+    auto widen = [&](int s, int j) __attribute__((always_inline)) {
+        const float f = __uint_as_float(scale[j] << 23);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t w = raw[j][2 * s + e];
+            fb[s][j][2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, false));
+            fb[s][j][2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, true));
+        }
+    };
+    constexpr int PROD = RB * CB;
+    // the products of step 0 beside the operands of step 1
+    auto first = [&](const uint8_t* ta) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < PROD; ++e) {
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+                if (i * PROD / RB == e) load_a(ta, 1, i);
+#pragma unroll
+            for (int j = 0; j < CB; ++j)
+                if (j * PROD / CB == e) widen(1, j);
+            acc[e / CB][e % CB] = mma1<Operand::BF16>(fb[0][e % CB], fa[0][e / CB], acc[e / CB][e % CB]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // the products of step 1 beside the next slice's operands (more) and the DMA into the
+    // buffer that has become free (refill)
+    auto second = [&](const uint8_t* ta, auto more, auto refill, int dst) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < PROD; ++e) {
+            if constexpr (decltype(more)::value) {
+#pragma unroll
+                for (int j = 0; j < CB; ++j)
+                    if (j * (PROD / 2) / CB == e) load_b(ta, j);
+#pragma unroll
+                for (int i = 0; i < RB; ++i)
+                    if (i * (PROD / 2) / RB == e) load_a(ta, 0, i);
+#pragma unroll
+                for (int j = 0; j < CB; ++j)
+                    if (PROD / 2 + j * (PROD / 2) / CB == e) widen(0, j);
+            }
+            acc[e / CB][e % CB] = mma1<Operand::BF16>(fb[1][e % CB], fa[1][e / CB], acc[e / CB][e % CB]);
+            if constexpr (decltype(refill)::value) {
+#pragma unroll
+                for (int q = 0; q < NI; ++q)
+                    if (q * PROD / NI == e) issue1(dst, q);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (decltype(refill)::value) advance();
+    };
+    auto load_first = [&](const uint8_t* ta) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < CB; ++j) load_b(ta, j);
+#pragma unroll
+        for (int i = 0; i < RB; ++i) load_a(ta, 0, i);
+#pragma unroll
+        for (int j = 0; j < CB; ++j) widen(0, j);
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+
+    if (nk > 0) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            if (s < nk) {
+#pragma unroll
+                for (int q = 0; q < NI; ++q) issue1(s, q);
+                advance();
+            }
+        }
+        if (nk >= NS) dma_wait_barrier<(NS - 1) * NI < 63 ? (NS - 1) * NI : 63>();
+        else dma_wait_barrier<0>();
+        load_first(lds);
+        int buf = 0, k = 0;
+        auto slice = [&](auto more, auto refill) __attribute__((always_inline)) {
+            const int nbuf = buf + 1 == NS ? 0 : buf + 1;
+            first(lds + buf * STAGE);
+            // slice k + 1 has landed; every wave has read slice k
+            if constexpr (decltype(more)::value) dma_wait_barrier<decltype(refill)::value ? (NS - 2) * NI : 0>();
+            second(lds + nbuf * STAGE, more, refill, buf);
+            buf = nbuf;
+        };
+        for (; k < nk - NS; ++k) slice(yes, yes);
+        for (; k < nk - 1; ++k) slice(yes, no);
+        slice(no, no);
+    }
+    if (tail) {  // the last slice is cut: rows past the last token become zeros in LDS
+        dma_wait_barrier<0>();
+#pragma unroll
+        for (int q = 0; q < AI; ++q) va[q] = a_offset(q, p.tail);
+#pragma unroll
+        for (int q = 0; q < NI; ++q) issue1(0, q);
+        dma_wait_barrier<0>();
+        for (int x = threadIdx.x; x < BM / 64 * (kGroup - p.tail) * 8; x += 64 * W) {
+            const int c = x & 7, r = p.tail + (x >> 3) % (kGroup - p.tail), panel = (x >> 3) / (kGroup - p.tail);
+            *reinterpret_cast<u32x4*>(lds + panel * 4096 + r * 128 + c * 16) = u32x4{};
+        }
+        __syncthreads();
+        load_first(lds);
+        first(lds);
+        second(lds, no, no, 0);
+    }
+
+    // Results through LDS, 32 rows of a wave at a time, so that stores are whole rows.
+    dma_wait_barrier<0>();
+    uint8_t* const mine = lds + wave * 32 * PITCH;
+    constexpr int LR = CB * 8;  // lanes to a row
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4*>(mine + li * PITCH + (32 * j + 8 * g + 4 * lh) * 4) =
+                    f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+        for (int r = lane / LR; r < 32; r += 64 / LR) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(mine + r * PITCH + (lane % LR) * 16);
+            const int o = i0 + wi + 32 * i + r, j = j0 + wj + 4 * (lane % LR);
+            if (o >= p.rows || j >= p.cols) continue;
+            if (p.splits > 1)  // (rows of whole 16 bytes)
+                *reinterpret_cast<f32x4*>(p.part + ((int64_t)split * p.rows + o) * p.part_pitch + j) = v;
+            else
+                put_result<OT>(p.out, (int64_t)o * p.ld_out + j, min(4, p.cols - j), p.accumulate != 0, v);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Adds the splits' partial sums up in order.
+template <GemmStore OT> __global__ void __launch_bounds__(kThreads) wgrad_join(const WgradArgs p)
+{
+    const int64_t per = p.part_pitch / 4, n = per * p.rows;
+    for (int64_t x = (int64_t)blockIdx.x * kThreads + threadIdx.x; x < n; x += (int64_t)gridDim.x * kThreads) {
+        const int64_t o = x / per;
+        const int j = (int)(x - o * per) * 4;
+        const float* const src = p.part + o * p.part_pitch + j;
+        f32x4 v = *reinterpret_cast<const f32x4*>(src);
+        for (int s = 1; s < p.splits; ++s) {
+            const f32x4 w = *reinterpret_cast<const f32x4*>(src + (int64_t)s * p.rows * p.part_pitch);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += w[e];
+        }
+        put_result<OT>(p.out, o * p.ld_out + j, min(4, p.cols - j), p.accumulate != 0, v);
+    }
+}
+
+// The gradient as slices of bf16 rows: [slice][32][pitch], fp32 as three terms of 8 bits
+// each (x = h + m + l, cut, not rounded: all 24 bits; infinities and NaN in the first
+// alone). Rows past the last token and columns past the last are zeros.
+template <GemmStore ST>
+__global__ void __launch_bounds__(kThreads) stage_grad(const void* grad, int64_t ld, int64_t tokens, int32_t rows, int32_t pitch,
+                                                       int64_t chunks, uint16_t* dst)
 {
     constexpr int TERMS = ST == GemmStore::F32 ? 3 : 1;
-    constexpr int PITCH = 40;
-    __shared__ __attribute__((aligned(16))) uint16_t sa[TERMS][64][PITCH];
-    __shared__ __attribute__((aligned(16))) uint16_t sb[64][PITCH];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 31, lh = lane >> 5;
-    const int wi = (wave >> 1) * 32, wj = (wave & 1) * 32;
-    const int64_t o0 = (int64_t)blockIdx.y * 64, j0 = (int64_t)blockIdx.x * 64;
-    f32x16 acc = {};
-    for (int64_t t0 = 0; t0 < p.tokens; t0 += kGroup) {
-        {
-            const int t = tid >> 3, o = (tid & 7) * 8;
+    const int per = pitch / 8;
+    for (int64_t x = (int64_t)blockIdx.x * kThreads + threadIdx.x; x < chunks; x += (int64_t)gridDim.x * kThreads) {
+        const int64_t t = x / per;
+        const int o = (int)(x - t * per) * 8;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+        if (t < tokens) load8<ST>(grad, t * ld + o, min(8, rows - o), false, v);
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) {
+            uint32_t h[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const bool on = t0 + t < p.tokens && o0 + o + e < p.rows;
-                float v = on ? get1<ST>(p.grad, (t0 + t) * p.ld_grad + o0 + o + e) : 0.f;
-#pragma unroll
-                for (int k = 0; k < TERMS; ++k) {
-                    const uint32_t top = __float_as_uint(v) & 0xffff0000u;
-                    sa[k][o + e][t] = (uint16_t)(top >> 16);
-                    v = (top & kInf) == kInf ? 0.f : v - __uint_as_float(top);
-                }
+                uint32_t top = __float_as_uint(v[e]) & 0xffff0000u;
+                if (v[e] != v[e]) top = 0x7fc00000u;
+                h[e] = top >> 16;
+                v[e] = (top & kInf) == kInf ? 0.f : v[e] - __uint_as_float(top);
             }
+            const int64_t row = ((t / kGroup) * TERMS + k) * kGroup + t % kGroup;
+            *reinterpret_cast<u32x4*>(dst + row * pitch + o) =
+                u32x4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
         }
-        {
-            const int j = tid >> 2, part = (tid & 3) * 8;
-            const int64_t g = (t0 / kGroup) * p.cols + min(j0 + j, (int64_t)p.cols - 1);
-            const u32x2 w = *reinterpret_cast<const u32x2*>(p.codes + g * kGroup + part);
-            const float unit = __uint_as_float((uint32_t)p.exps[g] << 23);
-            u32x4 h;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d = (int)w[e >> 1];
-                const f32x2 f = (e & 1) ? __builtin_amdgcn_cvt_pk_f32_fp8(d, true) : __builtin_amdgcn_cvt_pk_f32_fp8(d, false);
-                h[e] = __float_as_uint(f[0] * unit) >> 16 | (__float_as_uint(f[1] * unit) & 0xffff0000u);
-            }
-            *reinterpret_cast<u32x4*>(&sb[j][part]) = h;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const u32x4 b = *reinterpret_cast<const u32x4*>(&sb[wj + li][16 * s + 8 * lh]);
-#pragma unroll
-            for (int k = 0; k < TERMS; ++k)
-                acc = mma1<Operand::BF16>(b, *reinterpret_cast<const u32x4*>(&sa[k][wi + li][16 * s + 8 * lh]), acc);
-        }
-        __syncthreads();
     }
-    const int64_t o = o0 + wi + li;
-    if (o >= p.rows) return;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        const int64_t j = j0 + wj + 8 * (v >> 2) + 4 * lh + (v & 3);
-        if (j >= p.cols) continue;
-        const int64_t i = o * p.ld_out + j;
-        put1<OT>(p.out, i, p.accumulate ? acc[v] + get1<OT>(p.out, i) : acc[v]);
+}
+
+// The exponents in rows of whole 4 bytes.
+__global__ void __launch_bounds__(kThreads) stage_exps(const uint8_t* exps, int32_t cols, int32_t pitch, int64_t n, uint8_t* dst)
+{
+    for (int64_t x = (int64_t)blockIdx.x * kThreads + threadIdx.x; x < n; x += (int64_t)gridDim.x * kThreads) {
+        const int64_t r = x / pitch;
+        const int c = (int)(x - r * pitch);
+        dst[x] = exps[r * cols + min(c, cols - 1)];
     }
 }
 
 int act_sizes(int64_t tokens, int64_t cols)
 {
     if (tokens < 0 || cols < 1) return HIMUON_ERR_INVALID_ARG;
-    if (tokens > INT32_MAX - 1024 || cols > INT32_MAX - 4096) return HIMUON_ERR_UNSUPPORTED;
+    if (tokens > INT32_MAX / 4 || cols > (INT32_MAX >> 5) - 4096) return HIMUON_ERR_UNSUPPORTED;
     return HIMUON_OK;
 }
 
 int wgrad_sizes(int64_t tokens, int64_t out, int64_t cols)
 {
     if (out < 1) return HIMUON_ERR_INVALID_ARG;
-    if (out > INT32_MAX - 4096) return HIMUON_ERR_UNSUPPORTED;
+    if (out >= (INT32_MAX >> 5) - 4096) return HIMUON_ERR_UNSUPPORTED;
     return act_sizes(tokens, cols);
 }
 
-template <GemmStore ST, GemmStore OT> int launch_wgrad(const WgradArgs& p, hipStream_t stream)
+// How a call runs: tile, splits of the tokens, what is laid out first.
+struct WgradPlan {
+    bool stage;
+    int terms, tile, splits;
+    int64_t pitch, exp_pitch, groups, part_pitch;
+    size_t exps_at, part_at, total;
+};
+
+WgradPlan plan_wgrad(int64_t tokens, int64_t out, int64_t cols, const void* grad, int64_t ld, int dtype)
 {
-    const int64_t gy = ceil_div(p.rows, 64);
-    if (gy > 65535) return HIMUON_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((wgrad_tile<ST, OT>), dim3((unsigned)ceil_div(p.cols, 64), (unsigned)gy), dim3(kThreads), 0, stream, p);
+    WgradPlan g;
+    g.groups = ceil_div(tokens, kGroup);
+    g.terms = dtype == HIMUON_F32 ? 3 : 1;
+    g.stage = dtype == HIMUON_F32 || out % 8 || ld % 8 || ((uintptr_t)grad & 15) || ld >= (INT64_C(1) << 26);
+    g.pitch = (int64_t)round_up((size_t)out, 8);
+    g.exp_pitch = (int64_t)round_up((size_t)cols, 4);
+    g.part_pitch = g.exp_pitch;
+    const int64_t slices = g.groups * g.terms;
+    g.tile = ceil_div(out, 256) * ceil_div(cols, 256) >= 128 ? 256 : 128;
+    const int64_t tiles = ceil_div(out, g.tile) * ceil_div(cols, g.tile);
+    const int64_t slots = g.tile == 256 ? 256 : 512;  // workgroups that the chip takes at once
+    g.splits = (int)std::max<int64_t>(1, std::min<int64_t>(slots / tiles, slices / 8));
+    size_t at = g.stage ? round_up((size_t)slices * kGroup * (size_t)g.pitch * 2, 256) : 0;
+    g.exps_at = at;
+    at += round_up((size_t)g.groups * (size_t)g.exp_pitch, 256);
+    g.part_at = at;
+    if (g.splits > 1) at += round_up((size_t)g.splits * (size_t)out * (size_t)g.part_pitch * 4, 256);
+    g.total = std::max<size_t>(at, 256);
+    return g;
+}
+
+template <GemmStore OT, int BM, int BN, int WGM, int WGN, int NS, int MINW> int launch_tiles(WgradArgs p, hipStream_t stream)
+{
+    p.ti = (int32_t)ceil_div(p.rows, BM);
+    p.tj = (int32_t)ceil_div(p.cols, BN);
+    const int64_t total = (int64_t)p.ti * p.tj * p.splits;
+    if (total > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((wgrad_blocks<OT, BM, BN, WGM, WGN, NS, MINW>), dim3((unsigned)total), dim3(64 * WGM * WGN), 0, stream, p);
+    int st = launch_status();
+    if (st != HIMUON_OK || p.splits == 1) return st;
+    const int64_t blocks = std::min<int64_t>(ceil_div(p.part_pitch / 4 * p.rows, kThreads), 8192);
+    hipLaunchKernelGGL(wgrad_join<OT>, dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
     return launch_status();
+}
+
+template <GemmStore OT> int launch_wgrad(const WgradArgs& p, int tile, hipStream_t stream)
+{
+    if (tile == 256) return launch_tiles<OT, 256, 256, 2, 2, 5, 1>(p, stream);
+    return launch_tiles<OT, 128, 128, 2, 2, 4, 2>(p, stream);
 }
 
 }  // namespace
@@ -320,11 +636,12 @@ extern "C" int himuon_act_unpack(int64_t n_tokens, int64_t cols, const void* cod
     return launch_status();
 }
 
-extern "C" size_t himuon_weight_grad_workspace_size(int64_t n_tokens, int64_t out, int64_t cols, int dtype)
+extern "C" size_t himuon_weight_grad_workspace_size(int64_t n_tokens, int64_t out, int64_t cols, const void* grad,
+                                                    int64_t ld_grad, int dtype)
 {
     using namespace himuon;
-    if (wgrad_sizes(n_tokens, out, cols) != HIMUON_OK || !known_dtype(dtype)) return 0;
-    return 256;
+    if (wgrad_sizes(n_tokens, out, cols) != HIMUON_OK || !known_dtype(dtype) || ld_grad < out) return 0;
+    return plan_wgrad(n_tokens, out, cols, grad, ld_grad, dtype).total;
 }
 
 extern "C" int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, const void* grad, int64_t ld_grad, int dtype,
@@ -337,27 +654,56 @@ extern "C" int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, c
     if (!known_dtype(dtype) || !known_dtype(out_dtype) || ld_grad < out || ld_dweight < cols) return HIMUON_ERR_INVALID_ARG;
     if (!small_product(n_tokens, ld_grad) || !small_product(out, ld_dweight)) return HIMUON_ERR_INVALID_ARG;
     if (!dweight || (n_tokens && (!grad || !codes || !exponents || ((uintptr_t)codes & 15)))) return HIMUON_ERR_INVALID_ARG;
-    if (!workspace || ((uintptr_t)workspace & 255) ||
-        workspace_bytes < himuon_weight_grad_workspace_size(n_tokens, out, cols, dtype))
-        return HIMUON_ERR_WORKSPACE;
+    WgradPlan g = plan_wgrad(n_tokens, out, cols, grad, ld_grad, dtype);
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < g.total) return HIMUON_ERR_WORKSPACE;
     if (n_tokens == 0 && accumulate) return HIMUON_OK;
     StreamDevice on(stream);
     if (on.status != HIMUON_OK) return on.status;
     const hipStream_t hs = static_cast<hipStream_t>(stream);
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
     WgradArgs p{};
-    p.grad = grad;
+    p.a = static_cast<const uint16_t*>(grad);
+    p.lda = ld_grad;
+    p.a_cols = (int32_t)out;
+    p.tail = (int32_t)(n_tokens % kGroup);
+    if (g.stage) {
+        uint16_t* const dst = reinterpret_cast<uint16_t*>(ws);
+        const int64_t chunks = g.groups * kGroup * (g.pitch / 8);
+        const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(chunks, kThreads), 16384)));
+        if (dtype == HIMUON_BF16)
+            hipLaunchKernelGGL(stage_grad<GemmStore::BF16>, grid, dim3(kThreads), 0, hs, grad, ld_grad, n_tokens, (int32_t)out,
+                               (int32_t)g.pitch, chunks, dst);
+        else
+            hipLaunchKernelGGL(stage_grad<GemmStore::F32>, grid, dim3(kThreads), 0, hs, grad, ld_grad, n_tokens, (int32_t)out,
+                               (int32_t)g.pitch, chunks, dst);
+        const int st = launch_status();
+        if (st != HIMUON_OK) return st;
+        p.a = dst;
+        p.lda = g.pitch;
+        p.a_cols = (int32_t)g.pitch;
+        p.tail = 0;
+    }
     p.codes = static_cast<const uint8_t*>(codes);
     p.exps = static_cast<const uint8_t*>(exponents);
+    p.lde = cols;
+    if (cols % 4 || ((uintptr_t)exponents & 3)) {
+        const int64_t n = g.groups * g.exp_pitch;
+        hipLaunchKernelGGL(stage_exps, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(n, kThreads), 4096))),
+                           dim3(kThreads), 0, hs, p.exps, (int32_t)cols, (int32_t)g.exp_pitch, n, ws + g.exps_at);
+        const int st = launch_status();
+        if (st != HIMUON_OK) return st;
+        p.exps = ws + g.exps_at;
+        p.lde = g.exp_pitch;
+    }
     p.out = dweight;
-    p.tokens = n_tokens;
-    p.ld_grad = ld_grad;
+    p.part = reinterpret_cast<float*>(ws + g.part_at);
     p.ld_out = ld_dweight;
+    p.part_pitch = g.part_pitch;
     p.rows = (int32_t)out;
     p.cols = (int32_t)cols;
+    p.slices = (int32_t)(g.groups * g.terms);
+    p.terms = g.terms;
+    p.splits = g.splits;
     p.accumulate = accumulate != 0;
-    if (dtype == HIMUON_BF16)
-        return out_dtype == HIMUON_BF16 ? launch_wgrad<GemmStore::BF16, GemmStore::BF16>(p, hs)
-                                        : launch_wgrad<GemmStore::BF16, GemmStore::F32>(p, hs);
-    return out_dtype == HIMUON_BF16 ? launch_wgrad<GemmStore::F32, GemmStore::BF16>(p, hs)
-                                    : launch_wgrad<GemmStore::F32, GemmStore::F32>(p, hs);
+    return out_dtype == HIMUON_BF16 ? launch_wgrad<GemmStore::BF16>(p, g.tile, hs) : launch_wgrad<GemmStore::F32>(p, g.tile, hs);
 }

@@ -40,6 +40,7 @@
 // ring of five or of two 64-deep slices, row-major iterates or 256-tiles changed
 // nothing by 3%.
 #include "elementwise8.h"
+#include "lds_dma.h"
 #include "ns_device.h"
 
 #include <type_traits>
@@ -72,38 +73,6 @@ struct BlkArgs {
 
 // where APPLY's results go: the next iterate, the output matrices, the weights
 enum class Dest : int { ITERATE, OUT, WEIGHTS };
-
-HM_DEV uint32_t lds_offset(const void* p)
-{
-    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)(p);
-}
-
-// 64 lanes x 16 bytes from base + voff to LDS bytes dst .. dst + 1023, lane order.
-// (An asm statement without outputs: the compiler would otherwise order every
-// LDS read behind all DMA in flight. The waits are dma_wait_barrier's.)
-HM_DEV void dma16(uint32_t dst, uint32_t voff, uint64_t base)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(voff), "s"(base)
-                 : "m0", "memory");
-}
-
-// The same with 4 bytes a lane: LDS bytes dst .. dst + 255.
-HM_DEV void dma4(uint32_t dst, uint32_t voff, uint64_t base)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(voff), "s"(base)
-                 : "m0", "memory");
-}
-
-// Waits until at most N of this wave's DMA are in flight and its LDS reads
-// have returned, then for the other waves. (Builtins, so that the compiler
-// knows that earlier LDS reads need no further wait.)
-template <int N> HM_DEV void dma_wait_barrier()
-{
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4);
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
 
 // Value e of four operand values as fp32.
 template <Operand OP> HM_DEV float widen(const u32x2& w, int e)
@@ -195,16 +164,11 @@ __global__ void __launch_bounds__(64 * WGM * WGN, MINW) block_gemm(const BlkArgs
         }
     }
     const uint32_t lds0 = lds_offset(lds);
-    auto uniform = [](const void* q) -> uint64_t {
-        const uint64_t v = (uint64_t)(uintptr_t)q;
-        return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v) |
-               (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32)) << 32;
-    };
     // DMA instruction q of the next slice, into ring buffer `buf`
     auto issue1 = [&](int buf, int q) {
         const uint32_t d = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + wave * 1024);
-        if (q < AI) dma16(d + q * W * 1024, va[q < AI ? q : 0], uniform(a_base));
-        else dma16(d + ABYTES + (q - AI) * W * 1024, vb[q < AI ? 0 : q - AI], uniform(b_base));
+        if (q < AI) dma16(d + q * W * 1024, va[q < AI ? q : 0], uniform_address(a_base));
+        else dma16(d + ABYTES + (q - AI) * W * 1024, vb[q < AI ? 0 : q - AI], uniform_address(b_base));
     };
     auto advance = [&]() {
         a_base += panel;
@@ -303,7 +267,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN, MINW) block_gemm(const BlkArgs
     if constexpr (P == Product::APPLY) {  // (ahead of the slices: whoever waits for slice 0 waits for it too)
         if (wave < BM / 64)
             dma4(__builtin_amdgcn_readfirstlane(lds0 + STAGE * NS + wave * 256),
-                 4u * (uint32_t)min(64 * wave + lane, p.m - 1 - i0), uniform(p.d + (int64_t)prob * p.m + i0));
+                 4u * (uint32_t)min(64 * wave + lane, p.m - 1 - i0), uniform_address(p.d + (int64_t)prob * p.m + i0));
     }
 #pragma unroll
     for (int s = 0; s < NS; ++s) {

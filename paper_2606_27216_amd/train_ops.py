@@ -49,7 +49,7 @@ def declare(L):
     L.himuon_qk_norm_rope_grad.argtypes = [ctypes.POINTER(Qk)] + [heads] * 6 + [_vp, _vp, _vp, _sz, _vp]
     L.himuon_act_pack.argtypes = [_i64, _i64, _vp, _i64, _int, _vp, _vp, _vp]
     L.himuon_act_unpack.argtypes = [_i64, _i64, _vp, _vp, _vp, _i64, _int, _vp]
-    L.himuon_weight_grad_workspace_size.argtypes = [_i64, _i64, _i64, _int]
+    L.himuon_weight_grad_workspace_size.argtypes = [_i64, _i64, _i64, _vp, _i64, _int]
     L.himuon_weight_grad.argtypes = [_i64, _i64, _i64, _vp, _i64, _int, _vp, _vp, _vp, _i64, _int, _int, _vp, _sz, _vp]
     for name in ("embed", "embed_grad", "qk_norm_rope", "qk_norm_rope_grad", "act_pack", "act_unpack", "weight_grad"):
         getattr(L, "himuon_" + name).restype = _int
@@ -350,7 +350,7 @@ def weight_grad(grad, codes, exps, out=None, dtype=None, accumulate=False, works
         ld_out = _matrix(out, "out")
         _same_device(grad.device, codes, out)
         L = lib()
-        ws = call.workspace(L.himuon_weight_grad_workspace_size(n, rows, cols, code), workspace, "himuon_weight_grad")
+        ws = call.workspace(L.himuon_weight_grad_workspace_size(n, rows, cols, grad.data_ptr(), ld, code), workspace, "himuon_weight_grad")
         _done(L.himuon_weight_grad(n, rows, cols, grad.data_ptr(), ld, code, codes.data_ptr(), exps.data_ptr(), out.data_ptr(),
                                    ld_out, _dtype_code(out), int(bool(accumulate)), *ws, call.raw), "himuon_weight_grad")
     return out
