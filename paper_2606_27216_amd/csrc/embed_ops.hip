@@ -102,7 +102,7 @@ struct SortArgs {
     const uint32_t *key_in, *pos_in;
     uint32_t *key_out, *pos_out;
     uint32_t* hist;              // [tiles][bins]
-    uint8_t* named;              // rows that some token names (cleared and marked by the first digit)
+    uint8_t* named;              // rows that some token names, whole 16 bytes (cleared and marked by the first digit)
     int64_t rows;
     int32_t n, wide, tiles, shift, bits, first;
 };
@@ -121,8 +121,8 @@ __global__ void __launch_bounds__(kThreads) sort_count(const SortArgs p)
     const int bins = 1 << p.bits;
     for (int b = threadIdx.x; b < bins; b += kThreads) h[b] = 0;
     if (p.first) {
-        for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < p.rows; r += (int64_t)gridDim.x * kThreads)
-            p.named[r] = 0;
+        for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < (p.rows + 15) / 16; r += (int64_t)gridDim.x * kThreads)
+            reinterpret_cast<uint4*>(p.named)[r] = uint4{};
     }
     __syncthreads();
     if ((int)blockIdx.x >= p.tiles) return;
@@ -182,13 +182,20 @@ __global__ void __launch_bounds__(kThreads) sort_scatter(const SortArgs p)
     for (int j = 0; j < BPT; ++j) total[j] = before[j] = 0;
     const int b0 = tid * BPT;
     if (b0 < bins) {
-        for (int t = 0; t < p.tiles; ++t) {
+        const uint4* const row = reinterpret_cast<const uint4*>(p.hist) + tid;
+        const int step = bins / BPT;  // (eight rows at a time, all loads in flight)
+        for (int t0 = 0; t0 < p.tiles; t0 += 8) {
+            uint4 h[8];
 #pragma unroll
-            for (int j = 0; j < BPT; ++j) {
-                if (b0 + j < bins) {
-                    const uint32_t h = p.hist[(int64_t)t * bins + b0 + j];
-                    total[j] += h;
-                    if (t < (int)blockIdx.x) before[j] += h;
+            for (int k = 0; k < 8; ++k) h[k] = row[(int64_t)min(t0 + k, p.tiles - 1) * step];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t on = t0 + k < p.tiles ? ~0u : 0u, earlier = t0 + k < (int)blockIdx.x ? ~0u : 0u;
+                const uint32_t v[BPT] = {h[k].x, h[k].y, h[k].z, h[k].w};
+#pragma unroll
+                for (int j = 0; j < BPT; ++j) {
+                    total[j] += v[j] & on;
+                    before[j] += v[j] & earlier;
                 }
             }
         }
@@ -226,6 +233,104 @@ __global__ void __launch_bounds__(kThreads) sort_scatter(const SortArgs p)
         const uint32_t at = cnt[wave][(key[k] >> p.shift) & (uint32_t)(bins - 1)] + rank[k];
         p.key_out[at] = key[k];
         p.pos_out[at] = p.first ? (uint32_t)i : p.pos_in[i];
+    }
+}
+
+// All digits of a short list in one launch: a block of 1024 threads keeps keys and
+// positions in LDS (up to kSmall of them).
+constexpr int kSmallThreads = 1024;
+constexpr int kSmall = kSmallThreads * kIpt;
+
+__global__ void __launch_bounds__(kSmallThreads) sort_small(const SortArgs p, int digits)
+{
+    constexpr int W = kSmallThreads / kWave;
+    __shared__ uint32_t keys[kSmall], poss[kSmall];
+    __shared__ uint16_t cnt[W][kMaxBins];
+    __shared__ uint32_t wsum[W];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int bins = 1 << p.bits;
+    uint32_t key[kIpt], pos[kIpt], rank[kIpt];
+    const int base = wave * (kWave * kIpt);
+    if (p.named) {
+        for (int64_t r = tid; r < (p.rows + 15) / 16; r += kSmallThreads) reinterpret_cast<uint4*>(p.named)[r] = uint4{};
+    }
+#pragma unroll
+    for (int k = 0; k < kIpt; ++k) {
+        const int i = base + k * kWave + lane;
+        key[k] = i < p.n ? sort_key(p, i) : 0u;
+        pos[k] = (uint32_t)i;
+    }
+    volatile uint16_t* const mine = cnt[wave];
+    for (int d = 0; d < digits; ++d) {
+        const int shift = d * p.bits;
+        for (int b = tid; b < W * kMaxBins / 2; b += kSmallThreads) reinterpret_cast<uint32_t*>(&cnt[0][0])[b] = 0;
+        __syncthreads();
+        if (d == 0 && p.named) {
+#pragma unroll
+            for (int k = 0; k < kIpt; ++k)
+                if (base + k * kWave + lane < p.n && key[k] < (uint32_t)p.rows) p.named[key[k]] = 1;
+        }
+#pragma unroll
+        for (int k = 0; k < kIpt; ++k) {
+            const bool valid = base + k * kWave + lane < p.n;
+            const uint32_t g = (key[k] >> shift) & (uint32_t)(bins - 1);
+            uint64_t peers = __ballot(valid);
+            for (int b = 0; b < p.bits; ++b) {
+                const bool one = (g >> b) & 1;
+                const uint64_t m = __ballot(one);
+                peers &= one ? m : ~m;
+            }
+            const uint32_t below = (uint32_t)__popcll(peers & ((UINT64_C(1) << lane) - 1));
+            const uint32_t start = mine[g];
+            __builtin_amdgcn_wave_barrier();
+            rank[k] = start + below;
+            if (valid && below == 0) mine[g] = (uint16_t)(start + (uint32_t)__popcll(peers));
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+        uint32_t sum = 0;  // thread b: digit b
+#pragma unroll
+        for (int w = 0; w < W; ++w) sum += cnt[w][tid];
+        uint32_t scan = sum;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const uint32_t v = __shfl_up(scan, o);
+            if (lane >= o) scan += v;
+        }
+        if (lane == 63) wsum[wave] = scan;
+        __syncthreads();
+        uint32_t at = scan - sum;
+        for (int w = 0; w < wave; ++w) at += wsum[w];
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const uint32_t c = cnt[w][tid];
+            cnt[w][tid] = (uint16_t)at;
+            at += c;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kIpt; ++k) {
+            if (base + k * kWave + lane < p.n) {
+                const uint32_t to = cnt[wave][(key[k] >> shift) & (uint32_t)(bins - 1)] + rank[k];
+                keys[to] = key[k];
+                poss[to] = pos[k];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kIpt; ++k) {
+            const int i = base + k * kWave + lane;
+            key[k] = i < p.n ? keys[i] : 0u;
+            pos[k] = i < p.n ? poss[i] : 0u;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kIpt; ++k) {
+        const int i = base + k * kWave + lane;
+        if (i < p.n) {
+            p.key_out[i] = key[k];
+            p.pos_out[i] = pos[k];
+        }
     }
 }
 
@@ -338,15 +443,18 @@ template <GemmStore OT, int S> __global__ void __launch_bounds__(kJoinThreads) j
     const uint32_t key = p.key[after];
     if (key >= (uint32_t)p.rows || p.key[after - 1] != key) return;
     if (p.key[first] == key && first > 0 && p.key[first - 1] == key) return;  // began in an earlier chunk
-    // the end of the run
-    int64_t lo = after, hi = p.n;  // key[lo] == key, key[hi] != key
-    while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (p.key[mid] == key) lo = mid;
-        else hi = mid;
-    }
-    const int last = (int)(lo / S);  // chunks chunk + 1 .. last hold parts
     const int lane = threadIdx.x & 63;
+    // the last chunk that holds a part: 64 chunks' first entries are asked at once
+    int last = chunk + 1;
+    for (;;) {
+        const int64_t i = (int64_t)(last + 1 + lane) * S;
+        const uint64_t ends = __ballot(i >= p.n || p.key[min(i, (int64_t)p.n - 1)] != key);
+        if (ends) {
+            last += __ffsll((unsigned long long)ends) - 1;
+            break;
+        }
+        last += 64;
+    }
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = blockIdx.y * kSlab + lane * 8;
     const int nc = min(8, p.dim - c);
@@ -425,7 +533,7 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
     GradPlan g;
     const int kb = key_bits(rows);
     g.digits = (kb + 9) / 10;
-    g.bits = (kb + g.digits - 1) / g.digits;
+    g.bits = std::max(2, (kb + g.digits - 1) / g.digits);  // (bins in groups of four)
     g.tiles = (int)ceil_div(n, kTile);
     g.chunk = chunk_size(n, dim);
     size_t at = 0;
@@ -520,7 +628,17 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
     s.tiles = g.tiles;
     s.bits = g.bits;
     int from = 0;
-    for (int d = 0; d < (n_tokens ? g.digits : 1); ++d) {
+    const bool small = n_tokens > 0 && n_tokens <= kSmall;
+    if (small) {
+        s.first = 1;
+        if (accumulate) s.named = nullptr;
+        s.key_out = reinterpret_cast<uint32_t*>(ws + g.key[0]);
+        s.pos_out = reinterpret_cast<uint32_t*>(ws + g.pos[0]);
+        hipLaunchKernelGGL(sort_small, dim3(1), dim3(kSmallThreads), 0, hs, s, g.digits);
+        const int st = launch_status();
+        if (st != HIMUON_OK) return st;
+    }
+    for (int d = 0; !small && d < (n_tokens ? g.digits : 1); ++d) {
         s.first = d == 0;
         s.shift = d * g.bits;
         s.key_in = reinterpret_cast<const uint32_t*>(ws + g.key[from]);
@@ -528,7 +646,7 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
         s.key_out = reinterpret_cast<uint32_t*>(ws + g.key[from ^ 1]);
         s.pos_out = reinterpret_cast<uint32_t*>(ws + g.pos[from ^ 1]);
         from ^= 1;
-        const int clear = d == 0 ? (int)std::min<int64_t>(ceil_div(n_rows, kThreads), 256) : 1;
+        const int clear = d == 0 ? (int)std::min<int64_t>(ceil_div(n_rows, kThreads * 16), 256) : 1;
         hipLaunchKernelGGL(sort_count, dim3((unsigned)std::max(g.tiles, clear)), dim3(kThreads), 0, hs, s);
         int st = launch_status();
         if (st != HIMUON_OK) return st;

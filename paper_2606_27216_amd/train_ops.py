@@ -14,8 +14,9 @@ of the library raises HimuonError. Tensors are float32 or bfloat16.
 from __future__ import annotations
 
 import ctypes
+import struct
 
-from . import OK, HimuonError, _dtype_code, _keep_alive, lib
+from . import BF16, ERR_UNSUPPORTED, F32, OK, HimuonError, _dtype_code, _keep_alive, lib
 
 I32, I64 = 0, 1              # himuon_index_t
 MAX_HEAD_DIM = 512           # HIMUON_MAX_HEAD_DIM
@@ -24,29 +25,19 @@ ACT_GROUP = 32               # HIMUON_ACT_GROUP: tokens of a column that share a
 _i64, _vp, _sz, _f, _int = ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float, ctypes.c_int
 
 
-class Heads(ctypes.Structure):
-    """himuon_heads_t"""
-    _fields_ = [("ptr", _vp), ("stride_batch", _i64), ("stride_seq", _i64), ("stride_head", _i64)]
-
-
-class Qk(ctypes.Structure):
-    """himuon_qk_t"""
-    _fields_ = [("batch", _i64), ("seq", _i64), ("q_heads", ctypes.c_int32), ("k_heads", ctypes.c_int32),
-                ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
-                ("dtype", ctypes.c_int32), ("gain_dtype", ctypes.c_int32), ("index", ctypes.c_int32),
-                ("q_gain", _vp), ("k_gain", _vp), ("cos_table", _vp), ("sin_table", _vp), ("table_rows", _i64),
-                ("positions", _vp), ("eps", _f)]
+# himuon_heads_t and himuon_qk_t, as bytes (a call packs them in one go)
+_HEADS = struct.Struct("@P3q")
+_QK = struct.Struct("@2q8i4PqPf0q")
 
 
 def declare(L):
     """Argument types of the operators' entry points (called once, as the library is loaded)."""
-    heads = ctypes.POINTER(Heads)
     L.himuon_embed.argtypes = [_i64, _vp, _int, _i64, _i64, _vp, _i64, _vp, _i64, _f, _int, _vp]
     L.himuon_embed_grad_workspace_size.argtypes = [_i64, _i64, _i64]
     L.himuon_embed_grad.argtypes = [_i64, _vp, _int, _i64, _i64, _vp, _i64, _int, _vp, _i64, _int, _f, _int, _vp, _sz, _vp]
-    L.himuon_qk_norm_rope.argtypes = [ctypes.POINTER(Qk)] + [heads] * 4 + [_vp]
+    L.himuon_qk_norm_rope.argtypes = [_vp] * 6
     L.himuon_qk_norm_rope_grad_workspace_size.argtypes = [_i64, _i64, _i64]
-    L.himuon_qk_norm_rope_grad.argtypes = [ctypes.POINTER(Qk)] + [heads] * 6 + [_vp, _vp, _vp, _sz, _vp]
+    L.himuon_qk_norm_rope_grad.argtypes = [_vp] * 10 + [_sz, _vp]
     L.himuon_act_pack.argtypes = [_i64, _i64, _vp, _i64, _int, _vp, _vp, _vp]
     L.himuon_act_unpack.argtypes = [_i64, _i64, _vp, _vp, _vp, _i64, _int, _vp]
     L.himuon_weight_grad_workspace_size.argtypes = [_i64, _i64, _i64, _vp, _i64, _int]
@@ -58,14 +49,21 @@ def declare(L):
 
 
 # ------------------------------------------------------------------ shared checks
+#
+# (These run on every call: a small call's time is the host's. Tensors' properties are read
+# once, and the error messages are made only when something is wrong.)
 
-_INDEX = {}
+_INDEX, _TYPES = {}, {}
+_device = _raw_stream = None
 
 
 def _torch():
+    global _device, _raw_stream
     import torch
     if not _INDEX:
+        _TYPES.update({torch.float32: F32, torch.bfloat16: BF16})
         _INDEX.update({torch.int32: I32, torch.int64: I64})
+        _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     return torch
 
 
@@ -76,11 +74,18 @@ def _index_code(t):
     return code
 
 
+def _type_code(t):
+    code = _TYPES.get(t.dtype)
+    return _dtype_code(t) if code is None else code
+
+
 def _matrix(t, what):
-    """Checks a row-major CUDA matrix; its leading dimension."""
-    if t.dim() != 2 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1):
+    """Checks a row-major CUDA matrix; (rows, columns, leading dimension)."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or not t.is_cuda or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{what} must be a 2-D row-major CUDA tensor")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+    rows, cols = shape
+    return rows, cols, (stride[0] if rows > 1 else max(cols, 1))
 
 
 def _same_device(dev, *tensors):
@@ -89,44 +94,28 @@ def _same_device(dev, *tensors):
             raise ValueError("tensors must be on one device")
 
 
-class _Call:
-    """The stream of a call, its device made current, and the tensors allocated for it."""
+def _on(dev, f, *args):
+    """``f(*args)`` with ``dev`` the current device (the default stream has no handle
+    that names its device)."""
+    torch = _torch()
+    with torch.cuda.device(dev):
+        return f(*args)
 
-    __slots__ = ("dev", "stream", "raw", "fresh", "prev")
 
-    def __init__(self, dev, stream):
-        torch = _torch()
-        self.dev, self.stream, self.fresh = dev, stream, []
-        # the default stream has no handle that names its device
-        cur = torch._C._cuda_getDevice()
-        self.prev = cur if cur != dev.index else None
-        if self.prev is not None:
-            torch.cuda.set_device(dev)
-        self.raw = (torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream) or None
+def _stream_of(stream, index):
+    return (_raw_stream(index) if stream is None else stream.cuda_stream) or None
 
-    def __enter__(self):
-        return self
 
-    def __exit__(self, *exc):
-        if self.stream is not None:
-            _keep_alive(self.fresh, self.stream, self.dev)
-        if self.prev is not None:
-            _torch().cuda.set_device(self.prev)
-
-    def empty(self, shape, dtype):
-        t = _torch().empty(shape, dtype=dtype, device=self.dev)
-        self.fresh.append(t)
-        return t
-
-    def workspace(self, need, given, what):
-        """``given``, or a fresh one of ``need`` bytes (0: the sizes are not served)."""
-        if need == 0:
-            raise HimuonError(-2, what + "_workspace_size")
-        if given is None:
-            given = self.empty(need, _torch().uint8)
-        elif given.device != self.dev:
-            raise ValueError("the workspace must be on the tensors' device")
-        return given.data_ptr(), given.numel() * given.element_size()
+def _workspace(need, given, like, what):
+    """``given``, or a fresh one of ``need`` bytes (0: the sizes are not served)."""
+    torch = _torch()
+    if need == 0:
+        raise HimuonError(ERR_UNSUPPORTED, what + "_workspace_size")
+    if given is None:
+        return torch.empty(need, dtype=torch.uint8, device=like.device)
+    if given.device != like.device:
+        raise ValueError("the workspace must be on the tensors' device")
+    return given
 
 
 def _done(status, what):
@@ -142,24 +131,28 @@ def embed(tokens, table, scale=1.0, out=None, stream=None):
     outside the table (such as -1 for padding) gives zeros. Rows of ``table`` and
     of a 2-D ``out`` (one row per token) may be strided."""
     _torch()
-    ld = _matrix(table, "table")
+    rows, width, ld = _matrix(table, "table")
     if not tokens.is_cuda or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous CUDA tensor")
-    dev, code, index = table.device, _dtype_code(table), _index_code(tokens)
-    n, width = tokens.numel(), table.shape[1]
-    with _Call(dev, stream) as call:
-        if out is None:
-            out = call.empty((*tokens.shape, width), table.dtype)
-            ld_out = width
-        else:
-            if out.dtype != table.dtype or tuple(out.shape) not in ((n, width), (*tokens.shape, width)):
-                raise ValueError("out must hold one row of the table's type and width per token")
-            if out.dim() != 2 and not out.is_contiguous():
-                raise ValueError("out must be a 2-D row-major or a contiguous tensor")
-            ld_out = _matrix(out, "out") if out.dim() == 2 else width
+    dev, n, fresh = table.device, tokens.numel(), ()
+    if dev.index != _device():
+        return _on(dev, embed, tokens, table, scale, out, stream)
+    code, index = _type_code(table), _index_code(tokens)
+    if out is None:
+        out = table.new_empty((*tokens.shape, width))
+        fresh, ld_out = (out,), width
+        _same_device(dev, tokens)
+    else:
+        if out.dtype != table.dtype or tuple(out.shape) not in ((n, width), (*tokens.shape, width)):
+            raise ValueError("out must hold one row of the table's type and width per token")
+        if out.dim() != 2 and not out.is_contiguous():
+            raise ValueError("out must be a 2-D row-major or a contiguous tensor")
+        ld_out = _matrix(out, "out")[2] if out.dim() == 2 else width
         _same_device(dev, tokens, out)
-        _done(lib().himuon_embed(n, tokens.data_ptr(), index, table.shape[0], width, table.data_ptr(), ld, out.data_ptr(),
-                                 ld_out, float(scale), code, call.raw), "himuon_embed")
+    _done(lib().himuon_embed(n, tokens.data_ptr(), index, rows, width, table.data_ptr(), ld, out.data_ptr(), ld_out,
+                             scale, code, _stream_of(stream, dev.index)), "himuon_embed")
+    if stream is not None:
+        _keep_alive(fresh, stream, dev)
     return out
 
 
@@ -173,65 +166,88 @@ def embed_grad(tokens, grad, num_rows, scale=1.0, out=None, dtype=None, accumula
     torch = _torch()
     if not tokens.is_cuda or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous CUDA tensor")
-    n = tokens.numel()
+    n, fresh = tokens.numel(), []
     if grad.dim() != 2:
         if tuple(grad.shape[:-1]) != tuple(tokens.shape) or not grad.is_contiguous():
             raise ValueError("grad must have one row per token")
         grad = grad.view(n, grad.shape[-1])
-    ld = _matrix(grad, "grad")
-    if grad.shape[0] != n:
+    given, width, ld = _matrix(grad, "grad")
+    if given != n:
         raise ValueError("grad must have one row per token")
-    dev, code, index, width, rows = grad.device, _dtype_code(grad), _index_code(tokens), grad.shape[1], int(num_rows)
     if accumulate and out is None:
         raise ValueError("accumulate needs the tensor to add to")
-    with _Call(dev, stream) as call:
-        if out is None:
-            out = call.empty((rows, width), grad.dtype if dtype is None else dtype)
-        elif tuple(out.shape) != (rows, width) or (dtype is not None and out.dtype != dtype):
-            raise ValueError("out must be num_rows x width of the asked type")
-        ld_out = _matrix(out, "out")
-        _same_device(dev, tokens, out)
-        L = lib()
-        ws = call.workspace(L.himuon_embed_grad_workspace_size(n, rows, width), workspace, "himuon_embed_grad")
-        _done(L.himuon_embed_grad(n, tokens.data_ptr(), index, rows, width, grad.data_ptr(), ld, code, out.data_ptr(), ld_out,
-                                  _dtype_code(out), float(scale), int(bool(accumulate)), *ws, call.raw), "himuon_embed_grad")
+    dev, rows = grad.device, int(num_rows)
+    if dev.index != _device():
+        return _on(dev, embed_grad, tokens, grad, rows, scale, out, dtype, accumulate, workspace, stream)
+    code, index = _type_code(grad), _index_code(tokens)
+    L = lib()
+    workspace = _workspace(L.himuon_embed_grad_workspace_size(n, rows, width), workspace, grad, "himuon_embed_grad")
+    fresh.append(workspace)
+    if out is None:
+        out = torch.empty((rows, width), dtype=grad.dtype if dtype is None else dtype, device=dev)
+        fresh.append(out)
+    elif tuple(out.shape) != (rows, width) or (dtype is not None and out.dtype != dtype):
+        raise ValueError("out must be num_rows x width of the asked type")
+    ld_out = _matrix(out, "out")[2]
+    _same_device(dev, tokens, out)
+    _done(L.himuon_embed_grad(n, tokens.data_ptr(), index, rows, width, grad.data_ptr(), ld, code, out.data_ptr(), ld_out,
+                              _type_code(out), scale, bool(accumulate), workspace.data_ptr(),
+                              workspace.numel() * workspace.element_size(), _stream_of(stream, dev.index)),
+          "himuon_embed_grad")
+    if stream is not None:
+        _keep_alive(fresh, stream, dev)
     return out
 
 
 # --------------------------------------------------------------- queries and keys
 
-def _heads(t, what, like=None):
-    """A [batch, seq, heads, dim] or [tokens, heads, dim] tensor as himuon_heads_t."""
-    if t.dim() not in (3, 4) or not t.is_cuda or (t.stride(-1) != 1 and t.shape[-1] > 1):
+def _heads(t, what):
+    """A [batch, seq, heads, dim] or [tokens, heads, dim] tensor: its shape, and himuon_heads_t."""
+    shape, s = t.shape, t.stride()
+    n = len(shape)
+    if n == 4:
+        packed = _HEADS.pack(t.data_ptr(), s[0], s[1], s[2])
+    elif n == 3:
+        packed = _HEADS.pack(t.data_ptr(), 0, s[0], s[1])
+    else:
+        n = 0
+    if n == 0 or not t.is_cuda or (s[-1] != 1 and shape[-1] > 1):
         raise ValueError(f"{what} must be a [batch, seq, heads, dim] or [tokens, heads, dim] CUDA tensor with adjacent dim")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+    return shape, packed
+
+
+def _heads_like(t, what, shape, like):
+    got, packed = _heads(t, what)
+    if got != shape or t.dtype != like.dtype or t.device != like.device:
         raise ValueError(f"{what} must match the inputs' shape, type and device")
-    s = t.stride()
-    return Heads(t.data_ptr(), s[0] if len(s) == 4 else 0, s[-3], s[-2])
+    return packed
 
 
 def _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved):
+    """(shape of q, of k, himuon_qk_t, and q and k as himuon_heads_t), checked."""
     torch = _torch()
-    hq, hk = _heads(q, "q"), _heads(k, "k")
-    if q.dim() != k.dim() or q.shape[:-2] != k.shape[:-2] or q.shape[-1] != k.shape[-1] or q.dtype != k.dtype:
+    sq, hq = _heads(q, "q")
+    sk, hk = _heads(k, "k")
+    dim, dev, f32 = sq[-1], q.device, torch.float32
+    if sq[:-2] != sk[:-2] or dim != sk[-1] or q.dtype != k.dtype:
         raise ValueError("q and k must share tokens, head size and type")
-    dim = q.shape[-1]
-    for g in (q_gain, k_gain):
-        if tuple(g.shape) != (dim,) or g.dtype != q_gain.dtype or not g.is_contiguous():
-            raise ValueError("gains must be contiguous tensors of the head size and of one type")
-    if cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32 or \
-            not cos.is_contiguous() or not sin.is_contiguous():
+    gain = q_gain.dtype
+    if q_gain.shape != (dim,) or k_gain.shape != (dim,) or k_gain.dtype != gain or not q_gain.is_contiguous() or \
+            not k_gain.is_contiguous():
+        raise ValueError("gains must be contiguous tensors of the head size and of one type")
+    table = cos.shape
+    if len(table) != 2 or sin.shape != table or cos.dtype != f32 or sin.dtype != f32 or not cos.is_contiguous() or \
+            not sin.is_contiguous():
         raise ValueError("cos and sin must be contiguous float32 tensors, one row per position")
-    _same_device(q.device, k, q_gain, k_gain, cos, sin, positions)
-    index = I64
+    _same_device(dev, k, q_gain, k_gain, cos, sin, positions)
+    index, at = I64, 0
     if positions is not None:
-        index = _index_code(positions)
-        if positions.shape != q.shape[:-2] or not positions.is_contiguous():
+        index, at = _index_code(positions), positions.data_ptr()
+        if positions.shape != sq[:-2] or not positions.is_contiguous():
             raise ValueError("positions must be a contiguous tensor, one per token")
-    batch, seq = (q.shape[0], q.shape[1]) if q.dim() == 4 else (1, q.shape[0])
-    return Qk(batch, seq, q.shape[-2], k.shape[-2], dim, 2 * cos.shape[1], int(bool(interleaved)), _dtype_code(q),
-              _dtype_code(q_gain), index, q_gain.data_ptr(), k_gain.data_ptr(), cos.data_ptr(), sin.data_ptr(), cos.shape[0],
-              positions.data_ptr() if positions is not None else None, float(eps)), hq, hk
+    batch, seq = (sq[0], sq[1]) if len(sq) == 4 else (1, sq[0])
+    return sq, sk, _QK.pack(batch, seq, sq[-2], sk[-2], dim, 2 * table[1], bool(interleaved), _type_code(q), _type_code(q_gain),
+                            index, q_gain.data_ptr(), k_gain.data_ptr(), cos.data_ptr(), sin.data_ptr(), table[0], at, eps), hq, hk
 
 
 def qk_norm_rope(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, interleaved=False, out=None, stream=None):
@@ -247,13 +263,15 @@ def qk_norm_rope(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, inter
                     not in use: zeros come out.
     ``interleaved`` pairs (2i, 2i+1) instead of (i, i + width).
     ``out``         the two tensors to write (q and k themselves are allowed)."""
-    torch = _torch()
-    args, hq, hk = _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
-    with _Call(q.device, stream) as call:
-        oq, ok = out if out is not None else (call.empty(q.shape, q.dtype), call.empty(k.shape, k.dtype))
-        ref = ctypes.byref
-        ho, hp = _heads(oq, "out", q), _heads(ok, "out", k)
-        _done(lib().himuon_qk_norm_rope(ref(args), ref(hq), ref(hk), ref(ho), ref(hp), call.raw), "himuon_qk_norm_rope")
+    sq, sk, args, hq, hk = _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
+    dev = q.device
+    if dev.index != _device():
+        return _on(dev, qk_norm_rope, q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, out, stream)
+    oq, ok = out if out is not None else (q.new_empty(sq), q.new_empty(sk))
+    _done(lib().himuon_qk_norm_rope(args, hq, hk, _heads_like(oq, "out", sq, q), _heads_like(ok, "out", sk, k),
+                                    _stream_of(stream, dev.index)), "himuon_qk_norm_rope")
+    if stream is not None and out is None:
+        _keep_alive((oq, ok), stream, dev)
     return oq, ok
 
 
@@ -262,19 +280,24 @@ def qk_norm_rope_grad(g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions=None, 
     """The backward pass of ``qk_norm_rope``: from the gradients ``g_q``, ``g_k`` of its
     outputs and its inputs, (dq, dk, dq_gain, dk_gain). ``out``: the tensors for dq
     and dk (``g_q`` and ``g_k`` themselves are allowed)."""
-    torch = _torch()
-    args, hq, hk = _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
-    gq, gk = _heads(g_q, "g_q", q), _heads(g_k, "g_k", k)
-    with _Call(q.device, stream) as call:
-        oq, ok = out if out is not None else (call.empty(q.shape, q.dtype), call.empty(k.shape, k.dtype))
-        dwq, dwk = (call.empty(w.shape, w.dtype) for w in (q_gain, k_gain))
-        ref = ctypes.byref
-        ho, hp = _heads(oq, "out", q), _heads(ok, "out", k)
-        L = lib()
-        ws = call.workspace(L.himuon_qk_norm_rope_grad_workspace_size(args.batch, args.seq, args.head_dim), workspace,
-                            "himuon_qk_norm_rope_grad")
-        _done(L.himuon_qk_norm_rope_grad(ref(args), ref(gq), ref(gk), ref(hq), ref(hk), ref(ho), ref(hp), dwq.data_ptr(),
-                                         dwk.data_ptr(), *ws, call.raw), "himuon_qk_norm_rope_grad")
+    sq, sk, args, hq, hk = _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
+    dev = q.device
+    if dev.index != _device():
+        return _on(dev, qk_norm_rope_grad, g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, out,
+                   workspace, stream)
+    gq, gk = _heads_like(g_q, "g_q", sq, q), _heads_like(g_k, "g_k", sk, k)
+    L = lib()
+    batch, seq = (sq[0], sq[1]) if len(sq) == 4 else (1, sq[0])
+    workspace = _workspace(L.himuon_qk_norm_rope_grad_workspace_size(batch, seq, sq[-1]), workspace, q,
+                           "himuon_qk_norm_rope_grad")
+    oq, ok = out if out is not None else (q.new_empty(sq), q.new_empty(sk))
+    dwq, dwk = q_gain.new_empty(sq[-1]), k_gain.new_empty(sq[-1])
+    _done(L.himuon_qk_norm_rope_grad(args, gq, gk, hq, hk, _heads_like(oq, "out", sq, q), _heads_like(ok, "out", sk, k),
+                                     dwq.data_ptr(), dwk.data_ptr(), workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), _stream_of(stream, dev.index)),
+          "himuon_qk_norm_rope_grad")
+    if stream is not None:
+        _keep_alive((oq, ok, dwq, dwk, workspace), stream, dev)
     return oq, ok, dwq, dwk
 
 
@@ -282,12 +305,12 @@ def qk_norm_rope_grad(g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions=None, 
 
 def _packed(codes, exps):
     """Checks an activation in 8 bits; (groups, columns)."""
-    torch = _torch()
-    if codes.dtype != torch.uint8 or exps.dtype != torch.uint8 or codes.dim() != 3 or codes.shape[2] != ACT_GROUP or \
-            codes.shape[:2] != exps.shape or not codes.is_contiguous() or not exps.is_contiguous() or not codes.is_cuda:
+    u8, shape = _torch().uint8, codes.shape
+    if codes.dtype != u8 or exps.dtype != u8 or len(shape) != 3 or shape[2] != ACT_GROUP or shape[:2] != exps.shape or \
+            not codes.is_contiguous() or not exps.is_contiguous() or not codes.is_cuda:
         raise ValueError("codes must be a contiguous uint8 CUDA tensor [groups, columns, 32], exponents [groups, columns]")
     _same_device(codes.device, exps)
-    return exps.shape
+    return shape[0], shape[1]
 
 
 def act_pack(x, out=None, stream=None):
@@ -295,16 +318,22 @@ def act_pack(x, out=None, stream=None):
     shapes [ceil(tokens / 32), columns, 32] and [ceil(tokens / 32), columns]. 32
     tokens of a column share a power of two; a value keeps four significant bits."""
     torch = _torch()
-    ld = _matrix(x, "x")
-    n, cols = x.shape
-    shape = (-(-n // ACT_GROUP), cols)
-    with _Call(x.device, stream) as call:
-        codes, exps = out if out is not None else (call.empty((*shape, ACT_GROUP), torch.uint8), call.empty(shape, torch.uint8))
-        if tuple(_packed(codes, exps)) != shape:
+    n, cols, ld = _matrix(x, "x")
+    dev, code, groups = x.device, _type_code(x), -(-n // ACT_GROUP)
+    if dev.index != _device():
+        return _on(dev, act_pack, x, out, stream)
+    if out is None:
+        codes = torch.empty((groups, cols, ACT_GROUP), dtype=torch.uint8, device=dev)
+        exps = codes.new_empty((groups, cols))
+    else:
+        codes, exps = out
+        if _packed(codes, exps) != (groups, cols):
             raise ValueError("out must be codes [ceil(tokens / 32), columns, 32] and exponents [ceil(tokens / 32), columns]")
-        _same_device(x.device, codes)
-        _done(lib().himuon_act_pack(n, cols, x.data_ptr(), ld, _dtype_code(x), codes.data_ptr(), exps.data_ptr(), call.raw),
-              "himuon_act_pack")
+        _same_device(dev, codes)
+    _done(lib().himuon_act_pack(n, cols, x.data_ptr(), ld, code, codes.data_ptr(), exps.data_ptr(),
+                                _stream_of(stream, dev.index)), "himuon_act_pack")
+    if stream is not None and out is None:
+        _keep_alive((codes, exps), stream, dev)
     return codes, exps
 
 
@@ -313,18 +342,22 @@ def act_unpack(codes, exps, tokens, dtype=None, out=None, stream=None):
     ``dtype`` (bfloat16 by default; exact in both types)."""
     torch = _torch()
     groups, cols = _packed(codes, exps)
-    n = int(tokens)
+    n, dev, fresh = int(tokens), codes.device, ()
     if n < 0 or -(-n // ACT_GROUP) != groups:
         raise ValueError("tokens does not match the number of groups")
-    with _Call(codes.device, stream) as call:
-        if out is None:
-            out = call.empty((n, cols), torch.bfloat16 if dtype is None else dtype)
-        elif tuple(out.shape) != (n, cols) or (dtype is not None and out.dtype != dtype):
-            raise ValueError("out must be tokens x columns of the asked type")
-        ld = _matrix(out, "out")
-        _same_device(codes.device, out)
-        _done(lib().himuon_act_unpack(n, cols, codes.data_ptr(), exps.data_ptr(), out.data_ptr(), ld, _dtype_code(out), call.raw),
-              "himuon_act_unpack")
+    if dev.index != _device():
+        return _on(dev, act_unpack, codes, exps, n, dtype, out, stream)
+    if out is None:
+        out = torch.empty((n, cols), dtype=torch.bfloat16 if dtype is None else dtype, device=dev)
+        fresh = (out,)
+    elif tuple(out.shape) != (n, cols) or (dtype is not None and out.dtype != dtype):
+        raise ValueError("out must be tokens x columns of the asked type")
+    ld = _matrix(out, "out")[2]
+    _same_device(dev, out)
+    _done(lib().himuon_act_unpack(n, cols, codes.data_ptr(), exps.data_ptr(), out.data_ptr(), ld, _type_code(out),
+                                  _stream_of(stream, dev.index)), "himuon_act_unpack")
+    if stream is not None:
+        _keep_alive(fresh, stream, dev)
     return out
 
 
@@ -333,24 +366,31 @@ def weight_grad(grad, codes, exps, out=None, dtype=None, accumulate=False, works
     outputs [tokens, rows] and its inputs x held in 8 bits: rows x columns in
     ``dtype`` (default: ``grad``'s), or added to ``out`` with ``accumulate``. The result
     may be what ``step`` takes as a gradient."""
-    _torch()
-    ld = _matrix(grad, "grad")
+    torch = _torch()
+    n, rows, ld = _matrix(grad, "grad")
     groups, cols = _packed(codes, exps)
-    n, rows = grad.shape
     if -(-n // ACT_GROUP) != groups:
         raise ValueError("grad and the activation differ in tokens")
     if accumulate and out is None:
         raise ValueError("accumulate needs the tensor to add to")
-    code = _dtype_code(grad)
-    with _Call(grad.device, stream) as call:
-        if out is None:
-            out = call.empty((rows, cols), grad.dtype if dtype is None else dtype)
-        elif tuple(out.shape) != (rows, cols) or (dtype is not None and out.dtype != dtype):
-            raise ValueError("out must be rows x columns of the asked type")
-        ld_out = _matrix(out, "out")
-        _same_device(grad.device, codes, out)
-        L = lib()
-        ws = call.workspace(L.himuon_weight_grad_workspace_size(n, rows, cols, grad.data_ptr(), ld, code), workspace, "himuon_weight_grad")
-        _done(L.himuon_weight_grad(n, rows, cols, grad.data_ptr(), ld, code, codes.data_ptr(), exps.data_ptr(), out.data_ptr(),
-                                   ld_out, _dtype_code(out), int(bool(accumulate)), *ws, call.raw), "himuon_weight_grad")
+    code, dev, at = _type_code(grad), grad.device, grad.data_ptr()
+    if dev.index != _device():
+        return _on(dev, weight_grad, grad, codes, exps, out, dtype, accumulate, workspace, stream)
+    L = lib()
+    workspace = _workspace(L.himuon_weight_grad_workspace_size(n, rows, cols, at, ld, code), workspace, grad,
+                           "himuon_weight_grad")
+    fresh = [workspace]
+    if out is None:
+        out = torch.empty((rows, cols), dtype=grad.dtype if dtype is None else dtype, device=dev)
+        fresh.append(out)
+    elif tuple(out.shape) != (rows, cols) or (dtype is not None and out.dtype != dtype):
+        raise ValueError("out must be rows x columns of the asked type")
+    ld_out = _matrix(out, "out")[2]
+    _same_device(dev, codes, out)
+    _done(L.himuon_weight_grad(n, rows, cols, at, ld, code, codes.data_ptr(), exps.data_ptr(), out.data_ptr(), ld_out,
+                               _type_code(out), bool(accumulate), workspace.data_ptr(),
+                               workspace.numel() * workspace.element_size(), _stream_of(stream, dev.index)),
+          "himuon_weight_grad")
+    if stream is not None:
+        _keep_alive(fresh, stream, dev)
     return out
