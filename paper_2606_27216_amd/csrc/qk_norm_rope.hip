@@ -301,29 +301,34 @@ template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bo
     }
 }
 
-// Sums of the blocks' rows for 64 of the 2 D columns, the rows shared out over the waves.
-constexpr int kSumThreads = 1024;
+// Sums of the blocks' rows for 16 of the 2 D columns, the rows shared out over 64 groups of
+// 16 lanes.
+constexpr int kSumThreads = 1024, kSumCols = 16;
 template <GemmStore GT> __global__ void __launch_bounds__(kSumThreads) gain_sums(const float* part, int rows, int dim, void* dq, void* dk)
 {
-    constexpr int W = kSumThreads / 64;
-    __shared__ float sums[W][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int col = blockIdx.x * 64 + lane;
+    constexpr int R = kSumThreads / kSumCols;
+    __shared__ float sums[R][kSumCols + 1];
+    const int x = threadIdx.x % kSumCols, group = threadIdx.x / kSumCols;
+    const int col = blockIdx.x * kSumCols + x;
     float v[4] = {};
     if (col < 2 * dim) {
-        int r = wave;
-        for (; r + 3 * W < rows; r += 4 * W) {
+        for (int r = group; r < rows; r += 4 * R) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] += part[(int64_t)(r + j * W) * 2 * dim + col];
+            for (int j = 0; j < 4; ++j) {
+                const float f = part[(int64_t)min(r + j * R, rows - 1) * 2 * dim + col];
+                v[j] += r + j * R < rows ? f : 0.f;
+            }
         }
-        for (; r < rows; r += W) v[0] += part[(int64_t)r * 2 * dim + col];
     }
-    sums[wave][lane] = (v[0] + v[1]) + (v[2] + v[3]);
+    sums[group][x] = (v[0] + v[1]) + (v[2] + v[3]);
     __syncthreads();
-    if (wave > 0 || col >= 2 * dim) return;
+    if (group >= 4) return;  // 16 rows to each of the first wave's four groups
     float t = 0.f;
 #pragma unroll
-    for (int w = 0; w < W; ++w) t += sums[w][lane];
+    for (int r = 0; r < R / 4; ++r) t += sums[group * (R / 4) + r][x];
+    t += __shfl_xor(t, 16);
+    t += __shfl_xor(t, 32);
+    if (group > 0 || col >= 2 * dim) return;
     if (col < dim) put1<GT>(dq, col, t);
     else put1<GT>(dk, col - dim, t);
 }
@@ -470,7 +475,7 @@ extern "C" int himuon_qk_norm_rope_grad(const himuon_qk_t* args, const himuon_he
     st = launch_qk<true>(p, args, hs);
     if (st != HIMUON_OK) return st;
     const int rows = (int)grad_blocks(p.tokens);
-    const dim3 grid((unsigned)ceil_div(2 * p.dim, 64));
+    const dim3 grid((unsigned)ceil_div(2 * p.dim, kSumCols));
     if (args->gain_dtype == HIMUON_BF16)
         hipLaunchKernelGGL(gain_sums<GemmStore::BF16>, grid, dim3(kSumThreads), 0, hs, p.part, rows, p.dim, dq_gain, dk_gain);
     else
