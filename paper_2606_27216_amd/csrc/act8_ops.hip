@@ -203,6 +203,10 @@ __global__ void __launch_bounds__(kThreads) act_unpack(const uint8_t* codes, con
 // An fp32 gradient, or one whose rows do not start on 16 bytes, is first laid out in the
 // workspace as slices of bf16 rows, fp32 as three terms that follow each other (the
 // codes' slice is then read three times in a row, from cache).
+//
+// Bound by the matrix cores under the board's power cap: 8192 x 11008 x 4096 takes 557 us,
+// 1.33 PFLOP/s (a large library product reaches 1.25 to 1.40 on the card, the library's
+// bf16 product of this shape 0.9). The cores are busy for 1024 of about 1400 cycles of a slice.
 struct WgradArgs {
     const uint16_t* a;           // gradient, or its terms in the workspace
     const uint8_t *codes, *exps;
@@ -237,8 +241,10 @@ template <GemmStore OT> HM_DEV void put_result(void* out, int64_t i, int n, bool
     }
 }
 
-template <GemmStore OT, int BM, int BN, int WGM, int WGN, int NS, int MINW>
-__global__ void __launch_bounds__(64 * WGM * WGN, MINW) wgrad_blocks(const WgradArgs p)
+// KG = 2: a workgroup has two such groups of waves, which share its slices out between them
+// and add their sums up in LDS at the end.
+template <GemmStore OT, int BM, int BN, int WGM, int WGN, int KG, int NS, int MINW>
+__global__ void __launch_bounds__(64 * WGM * WGN * KG, MINW) wgrad_blocks(const WgradArgs p)
 {
     constexpr int W = WGM * WGN;
     constexpr int RB = BM / 32 / WGM, CB = BN / 32 / WGN;  // 32-blocks of a wave
@@ -249,11 +255,15 @@ __global__ void __launch_bounds__(64 * WGM * WGN, MINW) wgrad_blocks(const Wgrad
     static_assert(AI * 16 * W == BM && BI * 32 * W == BN, "whole DMA instructions");
     static_assert((NS - 2) * NI < 64, "the wait's counter");
     constexpr int PITCH = CB * 128 + 16;  // bytes of a row of results in LDS
-    constexpr int OUT = W * 32 * PITCH;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGE * NS > OUT ? STAGE * NS : OUT];
+    static_assert(KG == 1 || (KG == 2 && RB == 2), "each group finishes one of a wave's two block rows");
+    constexpr int MEET = KG == 1 ? 0 : KG * W * CB * 4096;  // the groups' exchange
+    constexpr int OUT = MEET + KG * W * 32 * PITCH, RING = STAGE * NS;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds_all[KG * RING > OUT ? KG * RING : OUT];
 
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - group * W;
+    uint8_t* const lds = lds_all + group * RING;
     const int li = lane & 31, lh = lane >> 5, g16 = lane >> 4;
     const int wi = (wave / WGN) * RB * 32, wj = (wave % WGN) * CB * 32;
 
@@ -272,9 +282,11 @@ __global__ void __launch_bounds__(64 * WGM * WGN, MINW) wgrad_blocks(const Wgrad
         i0 = (4 * band + (r - tj * h)) * BM;
         j0 = tj * BN;
     }
-    const int s0 = (int)((int64_t)p.slices * split / p.splits), s1 = (int)((int64_t)p.slices * (split + 1) / p.splits);
-    const bool tail = p.tail != 0 && s1 == p.slices;
-    const int nk = s1 - s0 - (tail ? 1 : 0);  // whole slices
+    // whole slices of the workgroup, of this group of waves, and the most of any group
+    const int all0 = (int)((int64_t)p.slices * split / p.splits), all1 = (int)((int64_t)p.slices * (split + 1) / p.splits);
+    const bool tail = p.tail != 0 && all1 == p.slices;
+    const int all = all1 - all0 - (tail ? 1 : 0);
+    const int s0 = all0 + all * group / KG, nk = all0 + all * (group + 1) / KG - s0, most = (all + KG - 1) / KG;
 
     // DMA sources. Gradient: instruction q of a wave fills 8 rows of a panel (128 bytes
     // each); the 64-byte halves of rows 2, 3, 6, 7, .. change places, so that a
@@ -329,35 +341,38 @@ __global__ void __launch_bounds__(64 * WGM * WGN, MINW) wgrad_blocks(const Wgrad
     uint32_t scale[CB];
     const int arow = (16 * lh + ((lane & 15) >> 2)) * 128, acol = 32 * (g16 & 1) + 8 * (lane & 3), aswap = 64 * ((lane >> 3) & 1);
     const int ra[2] = {arow + (acol ^ aswap), arow + ((acol + 64) ^ aswap)};
-    auto load_a = [&](const uint8_t* ta, int s, int i) __attribute__((always_inline)) {
-        const uint8_t* const t = ta + ((wi >> 6) + (i >> 1)) * 4096 + 1024 * s + ra[i & 1];
-        const u32x2 lo = tr_read(t), hi = tr_read(t + 512);
-        fa[s][i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    // half x of the operand of step s: four tokens a lane
+    auto load_a = [&](const uint8_t* ta, int s, int i, int x) __attribute__((always_inline)) {
+        const u32x2 v = tr_read(ta + ((wi >> 6) + (i >> 1)) * 4096 + 1024 * s + 512 * x + ra[i & 1]);
+        fa[s][i][2 * x] = v[0];
+        fa[s][i][2 * x + 1] = v[1];
     };
     auto load_b = [&](const uint8_t* ta, int j) __attribute__((always_inline)) {
         raw[j] = *reinterpret_cast<const u32x4*>(ta + ABYTES + (wj / 32 + j) * 1024 + lane * 16);
+    };
+    auto load_scale = [&](const uint8_t* ta, int j) __attribute__((always_inline)) {
         scale[j] = ta[ABYTES + BBYTES + wave * 256 + 32 * j + li];
     };
-    auto widen = [&](int s, int j) __attribute__((always_inline)) {
+    auto widen = [&](int s, int j, int x) __attribute__((always_inline)) {
         const float f = __uint_as_float(scale[j] << 23);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t w = raw[j][2 * s + e];
-            fb[s][j][2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, false));
-            fb[s][j][2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, true));
-        }
+        const uint32_t w = raw[j][2 * s + x];
+        fb[s][j][2 * x] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, false));
+        fb[s][j][2 * x + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, true));
     };
-    constexpr int PROD = RB * CB;
+    // What goes out beside the products is spread over them, two or three instructions to each:
+    // a product takes the matrix core 32 cycles, and a wave that issues ten others in one gap
+    // leaves it idle (8192 x 4096 x 4096: bunched 223 us, spread 214).
+    constexpr int PROD = RB * CB, HALF = PROD / 2;
     // the products of step 0 beside the operands of step 1
     auto first = [&](const uint8_t* ta) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < PROD; ++e) {
 #pragma unroll
-            for (int i = 0; i < RB; ++i)
-                if (i * PROD / RB == e) load_a(ta, 1, i);
+            for (int o = 0; o < 2 * RB; ++o)
+                if (o * PROD / (2 * RB) == e) load_a(ta, 1, o >> 1, o & 1);
 #pragma unroll
-            for (int j = 0; j < CB; ++j)
-                if (j * PROD / CB == e) widen(1, j);
+            for (int o = 0; o < 2 * CB; ++o)
+                if ((2 * o + 1) * PROD / (4 * CB) == e) widen(1, o >> 1, o & 1);
             acc[e / CB][e % CB] = mma1<Operand::BF16>(fb[0][e % CB], fa[0][e / CB], acc[e / CB][e % CB]);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -369,20 +384,22 @@ __global__ void __launch_bounds__(64 * WGM * WGN, MINW) wgrad_blocks(const Wgrad
         for (int e = 0; e < PROD; ++e) {
             if constexpr (decltype(more)::value) {
 #pragma unroll
-                for (int j = 0; j < CB; ++j)
-                    if (j * (PROD / 2) / CB == e) load_b(ta, j);
+                for (int o = 0; o < 2 * CB; ++o) {
+                    if (o * HALF / (2 * CB) == e) {
+                        if (o & 1) load_b(ta, o >> 1);
+                        else load_scale(ta, o >> 1);
+                    }
+                    if (HALF + o * HALF / (2 * CB) == e) widen(0, o >> 1, o & 1);
+                }
 #pragma unroll
-                for (int i = 0; i < RB; ++i)
-                    if (i * (PROD / 2) / RB == e) load_a(ta, 0, i);
-#pragma unroll
-                for (int j = 0; j < CB; ++j)
-                    if (PROD / 2 + j * (PROD / 2) / CB == e) widen(0, j);
+                for (int o = 0; o < 2 * RB; ++o)
+                    if (HALF + o * HALF / (2 * RB) == e) load_a(ta, 0, o >> 1, o & 1);
             }
             acc[e / CB][e % CB] = mma1<Operand::BF16>(fb[1][e % CB], fa[1][e / CB], acc[e / CB][e % CB]);
             if constexpr (decltype(refill)::value) {
 #pragma unroll
                 for (int q = 0; q < NI; ++q)
-                    if (q * PROD / NI == e) issue1(dst, q);
+                    if ((NI <= HALF ? q * HALF / NI : q * PROD / NI) == e) issue1(dst, q);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -390,11 +407,14 @@ __global__ void __launch_bounds__(64 * WGM * WGN, MINW) wgrad_blocks(const Wgrad
     };
     auto load_first = [&](const uint8_t* ta) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < CB; ++j) load_b(ta, j);
+        for (int j = 0; j < CB; ++j) {
+            load_scale(ta, j);
+            load_b(ta, j);
+        }
 #pragma unroll
-        for (int i = 0; i < RB; ++i) load_a(ta, 0, i);
+        for (int o = 0; o < 2 * RB; ++o) load_a(ta, 0, o >> 1, o & 1);
 #pragma unroll
-        for (int j = 0; j < CB; ++j) widen(0, j);
+        for (int o = 0; o < 2 * CB; ++o) widen(0, o >> 1, o & 1);
     };
     constexpr std::true_type yes{};
     constexpr std::false_type no{};
@@ -424,29 +444,65 @@ __global__ void __launch_bounds__(64 * WGM * WGN, MINW) wgrad_blocks(const Wgrad
         for (; k < nk - 1; ++k) slice(yes, no);
         slice(no, no);
     }
-    if (tail) {  // the last slice is cut: rows past the last token become zeros in LDS
+    if constexpr (KG > 1) {  // (a barrier a slice: the group with fewer slices keeps the other's count)
+        for (int k = nk; k < most; ++k) dma_wait_barrier<0>();
+    }
+    // The last slice is cut: rows past the last token become zeros in LDS. (It is the last
+    // group's, whose sources stand behind its last whole slice; other groups read along.)
+    if (tail) {
         dma_wait_barrier<0>();
 #pragma unroll
         for (int q = 0; q < AI; ++q) va[q] = a_offset(q, p.tail);
+        if (group == KG - 1) {
 #pragma unroll
-        for (int q = 0; q < NI; ++q) issue1(0, q);
+            for (int q = 0; q < NI; ++q) issue1(0, q);
+        }
         dma_wait_barrier<0>();
-        for (int x = threadIdx.x; x < BM / 64 * (kGroup - p.tail) * 8; x += 64 * W) {
+        for (int x = threadIdx.x % (64 * W); x < BM / 64 * (kGroup - p.tail) * 8; x += 64 * W) {
             const int c = x & 7, r = p.tail + (x >> 3) % (kGroup - p.tail), panel = (x >> 3) / (kGroup - p.tail);
             *reinterpret_cast<u32x4*>(lds + panel * 4096 + r * 128 + c * 16) = u32x4{};
         }
         __syncthreads();
-        load_first(lds);
-        first(lds);
-        second(lds, no, no, 0);
+        if (group == KG - 1) {
+            load_first(lds);
+            first(lds);
+            second(lds, no, no, 0);
+        }
     }
 
-    // Results through LDS, 32 rows of a wave at a time, so that stores are whole rows.
     dma_wait_barrier<0>();
-    uint8_t* const mine = lds + wave * 32 * PITCH;
+    if constexpr (KG == 2) {
+        // group g finishes block row g of each wave: it leaves the other one to its partner
+        f32x4* const meet = reinterpret_cast<f32x4*>(lds_all);
+        auto leave = [&](const f32x16 (&v)[CB]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    meet[(((group * W + wave) * CB + j) * 4 + g) * 64 + lane] = f32x4{v[j][4 * g], v[j][4 * g + 1], v[j][4 * g + 2], v[j][4 * g + 3]};
+        };
+        auto take = [&](f32x16 (&v)[CB]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 w = meet[((((group ^ 1) * W + wave) * CB + j) * 4 + g) * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[j][4 * g + e] += w[e];
+                }
+        };
+        if (group == 0) leave(acc[1]);
+        else leave(acc[0]);
+        __syncthreads();
+        if (group == 0) take(acc[0]);
+        else take(acc[1]);
+    }
+    // Results through LDS, 32 rows of a wave at a time, so that stores are whole rows.
+    uint8_t* const mine = lds_all + MEET + (group * W + wave) * 32 * PITCH;
     constexpr int LR = CB * 8;  // lanes to a row
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
+        if (KG == 2 && i != group) continue;
 #pragma unroll
         for (int j = 0; j < CB; ++j)
 #pragma unroll
@@ -465,6 +521,150 @@ __global__ void __launch_bounds__(64 * WGM * WGN, MINW) wgrad_blocks(const Wgrad
                 put_result<OT>(p.out, (int64_t)o * p.ld_out + j, min(4, p.cols - j), p.accumulate != 0, v);
         }
         __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Small results: a 64 x 64 tile to a workgroup of eight waves that share the tokens out
+// (wave w has groups w, w + 8, ..), each with the whole tile in registers. The operands
+// come straight from memory in the products' own layout: a lane's 16 tokens of a row of
+// the gradient are 16 loads of one element (32 lanes side by side), its 16 codes one load. No
+// LDS, no barrier and no second layout of the gradient on the way, whatever its type and
+// alignment; fp32 is cut into its three terms in registers. The waves' sums meet in LDS.
+constexpr int kDirectWaves = 8;
+
+template <GemmStore ST, GemmStore OT> __global__ void __launch_bounds__(64 * kDirectWaves, 2) wgrad_direct(const WgradArgs p)
+{
+    constexpr int TERMS = ST == GemmStore::F32 ? 3 : 1;
+    constexpr int PITCH = 64 + 4;
+    using Elem = typename std::conditional<ST == GemmStore::F32, uint32_t, uint16_t>::type;
+    __shared__ __attribute__((aligned(16))) float sums[kDirectWaves][64][PITCH];
+    const int lane = threadIdx.x & 63, li = lane & 31, lh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tiles = p.ti * p.tj;
+    const int split = blockIdx.x / tiles, r = blockIdx.x - split * tiles;
+    const int i0 = (r / p.tj) * 64, j0 = (r % p.tj) * 64;
+    const int g0 = (int)((int64_t)p.slices * split / p.splits), g1 = (int)((int64_t)p.slices * (split + 1) / p.splits);
+
+    // one group's operands: the gradient's elements [block][token], codes and exponents
+    struct Group {
+        uint32_t a[2][16];
+        u32x4 b[2];
+        uint32_t e[2];
+    };
+    // offsets of the lane's 16 tokens of block 0, from there to block 1; columns past the
+    // last read the last one (their results are not stored)
+    const uint32_t pitch = (uint32_t)(p.lda * (int64_t)sizeof(Elem));
+    const uint32_t a0 = (uint32_t)min(i0 + li, p.rows - 1) * (uint32_t)sizeof(Elem);
+    const uint32_t a1 = (uint32_t)min(i0 + 32 + li, p.rows - 1) * (uint32_t)sizeof(Elem) - a0;
+    const uint32_t c0 = (uint32_t)min(j0 + li, p.cols - 1), c1 = (uint32_t)min(j0 + 32 + li, p.cols - 1);
+    uint32_t off[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) off[k] = a0 + (uint32_t)(16 * lh + k) * pitch;
+    const uint8_t* const grad = reinterpret_cast<const uint8_t*>(p.a);
+    auto load = [&](Group& g, int t) __attribute__((always_inline)) {
+        const bool cut = p.tail && t == p.slices - 1;
+        if (cut) {  // tokens past the last one read the last and become zeros
+#pragma unroll
+            for (int k = 0; k < 16; ++k) off[k] = a0 + (uint32_t)min(16 * lh + k, p.tail - 1) * pitch;
+        }
+        const uint8_t* const base = grad + (int64_t)t * kGroup * pitch;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            g.a[0][k] = *reinterpret_cast<const Elem*>(base + off[k]);
+            g.a[1][k] = *reinterpret_cast<const Elem*>(base + (off[k] + a1));
+        }
+        const int64_t c = (int64_t)t * p.cols;
+        const uint8_t* const codes = p.codes + c * kGroup;
+        const uint8_t* const exps = p.exps + c;
+        g.b[0] = *reinterpret_cast<const u32x4*>(codes + (32u * c0 + 16u * lh));
+        g.b[1] = *reinterpret_cast<const u32x4*>(codes + (32u * c1 + 16u * lh));
+        g.e[0] = exps[c0];
+        g.e[1] = exps[c1];
+        if (cut) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                g.a[0][k] = 16 * lh + k < p.tail ? g.a[0][k] : 0u;
+                g.a[1][k] = 16 * lh + k < p.tail ? g.a[1][k] : 0u;
+            }
+        }
+    };
+    f32x16 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = f32x16{};
+    auto multiply = [&](const Group& g) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            u32x4 b[2], a[TERMS][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float f = __uint_as_float(g.e[j] << 23);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    b[j][e] = __builtin_bit_cast(uint32_t, (e & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(g.b[j][2 * s + e / 2], f, true)
+                                                                   : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(g.b[j][2 * s + e / 2], f, false));
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t x = g.a[i][8 * s + 2 * e], y = g.a[i][8 * s + 2 * e + 1];
+                    if constexpr (TERMS == 1) {
+                        a[0][i][e] = x | y << 16;
+                    } else {  // (x == h: an infinity has no rest, NaN keeps one)
+                        float u = __uint_as_float(x), v = __uint_as_float(y);
+#pragma unroll
+                        for (int k = 0; k < TERMS; ++k) {
+                            const float hu = __uint_as_float(__float_as_uint(u) & 0xffff0000u), hv = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+                            a[k][i][e] = __float_as_uint(hu) >> 16 | __float_as_uint(hv);
+                            u = u == hu ? 0.f : u - hu;
+                            v = v == hv ? 0.f : v - hv;
+                        }
+                    }
+                }
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = mma1<Operand::BF16>(b[j], a[k][i], acc[i][j]);
+        }
+    };
+    Group cur, next;
+    const int n = g1 > g0 + wave ? (g1 - g0 - wave + kDirectWaves - 1) / kDirectWaves : 0;
+    if (n > 0) load(next, g0 + wave);
+#pragma unroll 1
+    for (int k = 0; k < n; ++k) {  // (a uniform count, so that addresses stay in scalar registers)
+        cur = next;
+        if (k + 1 < n) load(next, g0 + wave + (k + 1) * kDirectWaves);
+        multiply(cur);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4*>(&sums[wave][32 * i + li][32 * j + 8 * g + 4 * lh]) =
+                    f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int q = threadIdx.x + x * 64 * kDirectWaves;
+        const int o = q / 16, c = (q % 16) * 4;
+        f32x4 v = *reinterpret_cast<const f32x4*>(&sums[0][o][c]);
+#pragma unroll
+        for (int w = 1; w < kDirectWaves; ++w) {
+            const f32x4 u = *reinterpret_cast<const f32x4*>(&sums[w][o][c]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += u[e];
+        }
+        if (i0 + o >= p.rows || j0 + c >= p.cols) continue;
+        if (p.splits > 1)
+            *reinterpret_cast<f32x4*>(p.part + ((int64_t)split * p.rows + i0 + o) * p.part_pitch + j0 + c) = v;
+        else
+            put_result<OT>(p.out, (int64_t)(i0 + o) * p.ld_out + j0 + c, min(4, p.cols - j0 - c), p.accumulate != 0, v);
     }
 }
 
@@ -549,55 +749,105 @@ int wgrad_sizes(int64_t tokens, int64_t out, int64_t cols)
     return act_sizes(tokens, cols);
 }
 
-// How a call runs: tile, splits of the tokens, what is laid out first.
+// Which kernel a call runs on.
+enum class Tile : int { DIRECT, B128_PAIR, B128, B256 };
+
 struct WgradPlan {
+    Tile tile;
     bool stage;
-    int terms, tile, splits;
+    int terms, splits;
     int64_t pitch, exp_pitch, groups, part_pitch;
     size_t exps_at, part_at, total;
 };
 
+// The rule goes by the workgroups that each tile gives the 256 CUs and by the slices that
+// each of them walks over. Measured, us a call, bf16 / fp32 gradients, tokens x rows x columns:
+//   - DIRECT while two rounds of 64-tiles serve and a workgroup has at most 128 groups to
+//     share out over its waves. Against B128_PAIR: 1024^3 10.6 / 13.5 (15.2 / 26.8), 4096 x
+//     1024^2 19.9 / 38.6 (23.6 / 41.6), 512 x 1536 x 1280 10.0 / 15.4 (9.9 / 26.3); beyond:
+//     8192 x 1024^2 34.7 / 72.9 (26.8 / 68.3), 512 x 2048^2 17.3 / 30.0 (10.5 / 24.5).
+//   - B128_PAIR (two groups of waves to a tile) while there are no more tiles than CUs:
+//     512 x 2048^2 10.5 / 24.5 (B128, split in two, 24.9 / 34.6); 512 tiles of 4096 x 2048
+//     at 1024 tokens 25.0 / 63.5 (B128 23.0 / 59.7).
+//   - B256 where its tiles fill the chip and are long enough to hide their ends: 4096^2 at
+//     512, 1024, 8192 tokens 27.2, 39.3, 202 (B128 25.0, 39.3, 244); 2048 x 4096, split in
+//     two, at 4096 and 16384 tokens 75, 214 (B128 67, 249).
 WgradPlan plan_wgrad(int64_t tokens, int64_t out, int64_t cols, const void* grad, int64_t ld, int dtype)
 {
     WgradPlan g;
     g.groups = ceil_div(tokens, kGroup);
     g.terms = dtype == HIMUON_F32 ? 3 : 1;
-    g.stage = dtype == HIMUON_F32 || out % 8 || ld % 8 || ((uintptr_t)grad & 15) || ld >= (INT64_C(1) << 26);
+    const int64_t slices = g.groups * g.terms;
+    const int64_t t64 = ceil_div(out, 64) * ceil_div(cols, 64);
+    const int64_t t128 = ceil_div(out, 128) * ceil_div(cols, 128);
+    const int64_t t256 = ceil_div(out, 256) * ceil_div(cols, 256);
+    auto split = [](int64_t workgroups, int64_t tiles, int64_t parts) {
+        return std::max<int64_t>(1, std::min<int64_t>(workgroups / tiles, parts));
+    };
+    const int64_t direct = split(256, t64, g.groups / 32);
+    int64_t splits;
+    if (t64 <= 512 && ceil_div(t64, 256) * g.groups <= 128 * direct && ld < (INT64_C(1) << 24)) {
+        g.tile = Tile::DIRECT;
+        splits = direct;
+    } else if (t256 > 128 ? slices >= 32 : t256 == 128 && slices >= 256) {
+        g.tile = Tile::B256;
+        splits = split(256, t256, slices / 8);
+    } else if (t128 <= 256) {
+        g.tile = Tile::B128_PAIR;
+        splits = split(256, t128, slices / 16);
+    } else {
+        g.tile = Tile::B128;
+        splits = split(512, t128, slices / 8);
+    }
+    g.splits = (int)splits;
+    g.stage = g.tile != Tile::DIRECT &&
+              (dtype == HIMUON_F32 || out % 8 || ld % 8 || ((uintptr_t)grad & 15) || ld >= (INT64_C(1) << 26));
     g.pitch = (int64_t)round_up((size_t)out, 8);
     g.exp_pitch = (int64_t)round_up((size_t)cols, 4);
     g.part_pitch = g.exp_pitch;
-    const int64_t slices = g.groups * g.terms;
-    g.tile = ceil_div(out, 256) * ceil_div(cols, 256) >= 128 ? 256 : 128;
-    const int64_t tiles = ceil_div(out, g.tile) * ceil_div(cols, g.tile);
-    const int64_t slots = g.tile == 256 ? 256 : 512;  // workgroups that the chip takes at once
-    g.splits = (int)std::max<int64_t>(1, std::min<int64_t>(slots / tiles, slices / 8));
     size_t at = g.stage ? round_up((size_t)slices * kGroup * (size_t)g.pitch * 2, 256) : 0;
     g.exps_at = at;
-    at += round_up((size_t)g.groups * (size_t)g.exp_pitch, 256);
+    if (g.tile != Tile::DIRECT) at += round_up((size_t)g.groups * (size_t)g.exp_pitch, 256);
     g.part_at = at;
     if (g.splits > 1) at += round_up((size_t)g.splits * (size_t)out * (size_t)g.part_pitch * 4, 256);
     g.total = std::max<size_t>(at, 256);
     return g;
 }
 
-template <GemmStore OT, int BM, int BN, int WGM, int WGN, int NS, int MINW> int launch_tiles(WgradArgs p, hipStream_t stream)
+template <GemmStore OT> int join_splits(const WgradArgs& p, hipStream_t stream)
 {
-    p.ti = (int32_t)ceil_div(p.rows, BM);
-    p.tj = (int32_t)ceil_div(p.cols, BN);
-    const int64_t total = (int64_t)p.ti * p.tj * p.splits;
-    if (total > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((wgrad_blocks<OT, BM, BN, WGM, WGN, NS, MINW>), dim3((unsigned)total), dim3(64 * WGM * WGN), 0, stream, p);
-    int st = launch_status();
+    const int st = launch_status();
     if (st != HIMUON_OK || p.splits == 1) return st;
     const int64_t blocks = std::min<int64_t>(ceil_div(p.part_pitch / 4 * p.rows, kThreads), 8192);
     hipLaunchKernelGGL(wgrad_join<OT>, dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
     return launch_status();
 }
 
-template <GemmStore OT> int launch_wgrad(const WgradArgs& p, int tile, hipStream_t stream)
+template <GemmStore OT, int BM, int BN, int WGM, int WGN, int KG, int NS, int MINW> int launch_tiles(WgradArgs p, hipStream_t stream)
 {
-    if (tile == 256) return launch_tiles<OT, 256, 256, 2, 2, 5, 1>(p, stream);
-    return launch_tiles<OT, 128, 128, 2, 2, 4, 2>(p, stream);
+    p.ti = (int32_t)ceil_div(p.rows, BM);
+    p.tj = (int32_t)ceil_div(p.cols, BN);
+    const int64_t total = (int64_t)p.ti * p.tj * p.splits;
+    if (total > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((wgrad_blocks<OT, BM, BN, WGM, WGN, KG, NS, MINW>), dim3((unsigned)total), dim3(64 * WGM * WGN * KG), 0,
+                       stream, p);
+    return join_splits<OT>(p, stream);
+}
+
+template <GemmStore OT> int launch_wgrad(WgradArgs p, Tile tile, int dtype, hipStream_t stream)
+{
+    // (rings: 125 KB, 104 KB and three times 52 KB of a CU's 160 KB)
+    if (tile == Tile::B256) return launch_tiles<OT, 256, 256, 2, 2, 1, 5, 1>(p, stream);
+    if (tile == Tile::B128_PAIR) return launch_tiles<OT, 128, 128, 2, 2, 2, 4, 2>(p, stream);
+    if (tile == Tile::B128) return launch_tiles<OT, 128, 128, 2, 2, 1, 4, 2>(p, stream);
+    p.ti = (int32_t)ceil_div(p.rows, 64);
+    p.tj = (int32_t)ceil_div(p.cols, 64);
+    const dim3 grid((unsigned)(p.ti * p.tj * p.splits));
+    if (dtype == HIMUON_BF16)
+        hipLaunchKernelGGL((wgrad_direct<GemmStore::BF16, OT>), grid, dim3(64 * kDirectWaves), 0, stream, p);
+    else
+        hipLaunchKernelGGL((wgrad_direct<GemmStore::F32, OT>), grid, dim3(64 * kDirectWaves), 0, stream, p);
+    return join_splits<OT>(p, stream);
 }
 
 }  // namespace
@@ -703,7 +953,7 @@ extern "C" int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, c
         p.a_cols = (int32_t)g.pitch;
         p.tail = 0;
     }
-    if (cols % 4 || ((uintptr_t)exponents & 3)) {
+    if (g.tile != Tile::DIRECT && (cols % 4 || ((uintptr_t)exponents & 3))) {
         s.exps = p.exps;
         s.e = ws + g.exps_at;
         s.cols = (int32_t)cols;
@@ -725,9 +975,9 @@ extern "C" int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, c
     p.part_pitch = g.part_pitch;
     p.rows = (int32_t)out;
     p.cols = (int32_t)cols;
-    p.slices = (int32_t)(g.groups * g.terms);
+    p.slices = (int32_t)(g.tile == Tile::DIRECT ? g.groups : g.groups * g.terms);
     p.terms = g.terms;
     p.splits = g.splits;
     p.accumulate = accumulate != 0;
-    return out_dtype == HIMUON_BF16 ? launch_wgrad<GemmStore::BF16>(p, g.tile, hs) : launch_wgrad<GemmStore::F32>(p, g.tile, hs);
+    return out_dtype == HIMUON_BF16 ? launch_wgrad<GemmStore::BF16>(p, g.tile, dtype, hs) : launch_wgrad<GemmStore::F32>(p, g.tile, dtype, hs);
 }

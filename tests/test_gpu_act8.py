@@ -143,6 +143,61 @@ def test_weight_gradient(T, O, C, dtype, out):
     assert torch.equal(got, hm.weight_grad(grad, codes, exps, dtype=_dt(out)))  # the same from call to call
 
 
+# every kernel that serves larger results, whole and cut: two groups of waves to a tile, split
+# or not; 128-tiles; 256-tiles, split or not
+LARGE = [(300, 1500, 2100), (512, 2048, 2048), (9000, 700, 1000), (4100, 1024, 1096), (200, 3000, 2200), (256, 4096, 2304),
+         (1100, 3300, 3000), (1024, 3328, 3328), (8200, 4000, 2040)]
+
+
+@pytest.mark.parametrize("T,O,C", LARGE)
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+def test_large_weight_gradient(T, O, C, dtype, out):
+    import torch
+    grad = _rand((T, O), dtype, 23, 1e-3)
+    codes, exps = hm.act_pack(_data(T, C, "bf16", "gauss", 24))
+    print(f"[gpu-case] weight_grad {T} {O} {C} {dtype} {out}", flush=True)
+    got = hm.weight_grad(grad, codes, exps, dtype=_dt(out))
+    _check_wgrad(got, grad, codes, exps, out, 3 if dtype == "f32" else 1)
+    assert torch.equal(got, hm.weight_grad(grad, codes, exps, dtype=_dt(out)))
+
+
+@pytest.mark.parametrize("T,O,C", [(300, 1500, 2100), (9000, 700, 1000), (200, 3000, 2200), (1100, 3300, 3000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_weight_gradient_strides_and_accumulation(T, O, C, dtype):
+    import torch
+    for cut in (1, 8):
+        grad = _rand((T, O + 16), dtype, 25)[:, cut:cut + O]
+        codes, exps = hm.act_pack(_data(T, C, "bf16", "gauss", 26))
+        space = _rand((O, C + 9), "f32", 27)
+        before = space.clone()
+        view = space[:, 2:2 + C]
+        hm.weight_grad(grad, codes, exps, out=view, accumulate=True)
+        assert torch.equal(space[:, :2], before[:, :2]) and torch.equal(space[:, 2 + C:], before[:, 2 + C:])
+        _check_wgrad(view, grad, codes, exps, "f32", 3 if dtype == "f32" else 1, base=before[:, 2:2 + C])
+
+
+@pytest.mark.parametrize("T,O,C", [(300, 1500, 2104), (200, 3000, 2200), (1100, 3304, 3000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_weight_gradient_infinities_and_nan(T, O, C, dtype):
+    """As below, where the last group of tokens is cut."""
+    import torch
+    grad, x = _rand((T, O), dtype, 28), _rand((T, C), "bf16", 29)
+    x[T - 1] = x[T - 1].abs() + 0.5
+    x[T - 1, ::2] *= -1
+    clean = hm.weight_grad(grad, *hm.act_pack(x), dtype=torch.float32)
+    x2, g2 = x.clone(), grad.clone()
+    g2[T - 1, 9] = float("inf")
+    g2[0, 777] = float("nan")
+    x2[2, 33] = float("nan")
+    got = hm.weight_grad(g2, *hm.act_pack(x2), dtype=torch.float32)
+    cols = torch.arange(C, device="cuda") != 33
+    rows = torch.ones(O, dtype=torch.bool, device="cuda")
+    rows[9] = rows[777] = False
+    assert torch.equal(got[9][cols], (x2[T - 1].float() * float("inf"))[cols])
+    assert bool(torch.isnan(got[:, 33]).all()) and bool(torch.isnan(got[777]).all())
+    assert torch.equal(got[rows][:, cols], clean[rows][:, cols])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_weight_gradient_strides_and_accumulation(dtype):
     """Rows of the gradient and of the result at any address; added to what is there."""
