@@ -12,7 +12,8 @@
 // chunk over 512 columns. Runs that lie inside a chunk go to the table at once; a run
 // that crosses chunks leaves one fp32 partial sum per chunk, and a last launch
 // adds these up in order. So a token that makes up much of a batch is spread over the
-// chip like any other. Rows that no token names are set to zero beside the sums.
+// chip like any other. The sort is short launches that wait more than they work: blocks
+// that set the table to zero ride in them, and the sums then write the rows that occur.
 #include "elementwise8.h"
 #include "train_ops.h"
 
@@ -90,6 +91,36 @@ template <GemmStore ST> int launch_embed_st(const EmbedArgs& p, hipStream_t stre
     return launch_embed<ST, 64, 4>(p, stream);
 }
 
+// ------------------------------------------------------------------- zeros
+
+// Rows set to zero by the blocks of a launch from `first` on.
+struct FillArgs {
+    uint8_t* out;
+    int64_t row_bytes, ld_bytes, from, to;  // rows
+    int32_t first, blocks;
+};
+
+template <int THREADS> __device__ __forceinline__ void fill_rows(const FillArgs& f)
+{
+    typedef uint32_t Chunk __attribute__((ext_vector_type(4)));
+    typedef Chunk ChunkAny __attribute__((aligned(2)));
+    const int64_t b = (int64_t)blockIdx.x - f.first;
+    auto zero = [](uint8_t* p, int64_t n) {
+        if (n >= 16) *reinterpret_cast<ChunkAny*>(p) = Chunk{};
+        else
+            for (int64_t i = 0; i < n; i += 2) *reinterpret_cast<uint16_t*>(p + i) = 0;
+    };
+    if (f.ld_bytes == f.row_bytes) {
+        uint8_t* const base = f.out + f.from * f.ld_bytes;
+        const int64_t n = (f.to - f.from) * f.row_bytes;
+        for (int64_t i = (b * THREADS + threadIdx.x) * 16; i < n; i += (int64_t)f.blocks * THREADS * 16) zero(base + i, n - i);
+    } else {
+        const int64_t step = (int64_t)f.blocks * (THREADS / kWave);
+        for (int64_t r = f.from + b * (THREADS / kWave) + (threadIdx.x >> 6); r < f.to; r += step)
+            for (int64_t i = (threadIdx.x & 63) * 16; i < f.row_bytes; i += 1024) zero(f.out + r * f.ld_bytes + i, f.row_bytes - i);
+    }
+}
+
 // ------------------------------------------------------------------ sorting
 
 // Digits of at most 10 bits; a key is the token, n_rows for one outside the table.
@@ -102,9 +133,9 @@ struct SortArgs {
     const uint32_t *key_in, *pos_in;
     uint32_t *key_out, *pos_out;
     uint32_t* hist;              // [tiles][bins]
-    uint8_t* named;              // rows that some token names, whole 16 bytes (cleared and marked by the first digit)
     int64_t rows;
     int32_t n, wide, tiles, shift, bits, first;
+    FillArgs fill;
 };
 
 __device__ __forceinline__ uint32_t sort_key(const SortArgs& p, int i)
@@ -118,14 +149,10 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs& p, int i)
 __global__ void __launch_bounds__(kThreads) sort_count(const SortArgs p)
 {
     __shared__ uint32_t h[kMaxBins];
+    if ((int)blockIdx.x >= p.fill.first) return fill_rows<kThreads>(p.fill);
     const int bins = 1 << p.bits;
     for (int b = threadIdx.x; b < bins; b += kThreads) h[b] = 0;
-    if (p.first) {
-        for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < (p.rows + 15) / 16; r += (int64_t)gridDim.x * kThreads)
-            reinterpret_cast<uint4*>(p.named)[r] = uint4{};
-    }
     __syncthreads();
-    if ((int)blockIdx.x >= p.tiles) return;
 #pragma unroll
     for (int k = 0; k < kIpt; ++k) {
         const int i = blockIdx.x * kTile + k * kThreads + threadIdx.x;
@@ -144,6 +171,7 @@ __global__ void __launch_bounds__(kThreads) sort_scatter(const SortArgs p)
     constexpr int BPT = kMaxBins / kThreads;  // bins per thread
     __shared__ uint32_t cnt[W][kMaxBins];
     __shared__ uint32_t wsum[W];
+    if ((int)blockIdx.x >= p.fill.first) return fill_rows<kThreads>(p.fill);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int bins = 1 << p.bits;
     for (int b = tid; b < W * kMaxBins; b += kThreads) (&cnt[0][0])[b] = 0;
@@ -154,7 +182,6 @@ __global__ void __launch_bounds__(kThreads) sort_scatter(const SortArgs p)
     for (int k = 0; k < kIpt; ++k) {
         const int i = base + k * kWave + lane;
         key[k] = i < p.n ? sort_key(p, i) : 0u;
-        if (p.first && i < p.n && key[k] < (uint32_t)p.rows) p.named[key[k]] = 1;
     }
     volatile uint32_t* const mine = cnt[wave];
 #pragma unroll
@@ -236,102 +263,45 @@ __global__ void __launch_bounds__(kThreads) sort_scatter(const SortArgs p)
     }
 }
 
-// All digits of a short list in one launch: a block of 1024 threads keeps keys and
-// positions in LDS (up to kSmall of them).
-constexpr int kSmallThreads = 1024;
-constexpr int kSmall = kSmallThreads * kIpt;
+// A short list in one launch: an entry's place is the number of entries before it, those
+// with a smaller key and earlier ones with the same. A block ranks 64 entries, its waves
+// share out what these are compared with.
+constexpr int kRankThreads = 1024;
+constexpr int kRankMost = 4096;
 
-__global__ void __launch_bounds__(kSmallThreads) sort_small(const SortArgs p, int digits)
+__global__ void __launch_bounds__(kRankThreads) sort_rank(const SortArgs p)
 {
-    constexpr int W = kSmallThreads / kWave;
-    __shared__ uint32_t keys[kSmall], poss[kSmall];
-    __shared__ uint16_t cnt[W][kMaxBins];
-    __shared__ uint32_t wsum[W];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int bins = 1 << p.bits;
-    uint32_t key[kIpt], pos[kIpt], rank[kIpt];
-    const int base = wave * (kWave * kIpt);
-    if (p.named) {
-        for (int64_t r = tid; r < (p.rows + 15) / 16; r += kSmallThreads) reinterpret_cast<uint4*>(p.named)[r] = uint4{};
-    }
-#pragma unroll
-    for (int k = 0; k < kIpt; ++k) {
-        const int i = base + k * kWave + lane;
-        key[k] = i < p.n ? sort_key(p, i) : 0u;
-        pos[k] = (uint32_t)i;
-    }
-    volatile uint16_t* const mine = cnt[wave];
-    for (int d = 0; d < digits; ++d) {
-        const int shift = d * p.bits;
-        for (int b = tid; b < W * kMaxBins / 2; b += kSmallThreads) reinterpret_cast<uint32_t*>(&cnt[0][0])[b] = 0;
-        __syncthreads();
-        if (d == 0 && p.named) {
-#pragma unroll
-            for (int k = 0; k < kIpt; ++k)
-                if (base + k * kWave + lane < p.n && key[k] < (uint32_t)p.rows) p.named[key[k]] = 1;
-        }
-#pragma unroll
-        for (int k = 0; k < kIpt; ++k) {
-            const bool valid = base + k * kWave + lane < p.n;
-            const uint32_t g = (key[k] >> shift) & (uint32_t)(bins - 1);
-            uint64_t peers = __ballot(valid);
-            for (int b = 0; b < p.bits; ++b) {
-                const bool one = (g >> b) & 1;
-                const uint64_t m = __ballot(one);
-                peers &= one ? m : ~m;
+    constexpr int W = kRankThreads / kWave;
+    __shared__ uint32_t count[W][kWave];
+    if ((int)blockIdx.x >= p.fill.first) return fill_rows<kRankThreads>(p.fill);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = blockIdx.x * kWave + lane;
+    const uint32_t key = i < p.n ? sort_key(p, i) : 0u;
+    uint32_t before = 0;
+    for (int c = wave; c * kWave < p.n; c += W) {
+        const int j = c * kWave + lane;
+        const uint32_t other = j < p.n ? sort_key(p, j) : 0xffffffffu;
+        if (c == (int)blockIdx.x) {
+#pragma unroll 16
+            for (int l = 0; l < kWave; ++l) {
+                const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)other, l);
+                before += (k < key || (k == key && l < lane)) ? 1u : 0u;
             }
-            const uint32_t below = (uint32_t)__popcll(peers & ((UINT64_C(1) << lane) - 1));
-            const uint32_t start = mine[g];
-            __builtin_amdgcn_wave_barrier();
-            rank[k] = start + below;
-            if (valid && below == 0) mine[g] = (uint16_t)(start + (uint32_t)__popcll(peers));
-            __builtin_amdgcn_wave_barrier();
-        }
-        __syncthreads();
-        uint32_t sum = 0;  // thread b: digit b
-#pragma unroll
-        for (int w = 0; w < W; ++w) sum += cnt[w][tid];
-        uint32_t scan = sum;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            const uint32_t v = __shfl_up(scan, o);
-            if (lane >= o) scan += v;
-        }
-        if (lane == 63) wsum[wave] = scan;
-        __syncthreads();
-        uint32_t at = scan - sum;
-        for (int w = 0; w < wave; ++w) at += wsum[w];
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const uint32_t c = cnt[w][tid];
-            cnt[w][tid] = (uint16_t)at;
-            at += c;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kIpt; ++k) {
-            if (base + k * kWave + lane < p.n) {
-                const uint32_t to = cnt[wave][(key[k] >> shift) & (uint32_t)(bins - 1)] + rank[k];
-                keys[to] = key[k];
-                poss[to] = pos[k];
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kIpt; ++k) {
-            const int i = base + k * kWave + lane;
-            key[k] = i < p.n ? keys[i] : 0u;
-            pos[k] = i < p.n ? poss[i] : 0u;
+        } else {
+            const uint32_t limit = key + (c < (int)blockIdx.x ? 1u : 0u);  // (keys are below 2^31)
+#pragma unroll 16
+            for (int l = 0; l < kWave; ++l) before += (uint32_t)__builtin_amdgcn_readlane((int)other, l) < limit ? 1u : 0u;
         }
     }
+    count[wave][lane] = before;
+    __syncthreads();
+    if (wave > 0 || i >= p.n) return;
+    uint32_t at = 0;
 #pragma unroll
-    for (int k = 0; k < kIpt; ++k) {
-        const int i = base + k * kWave + lane;
-        if (i < p.n) {
-            p.key_out[i] = key[k];
-            p.pos_out[i] = pos[k];
-        }
-    }
+    for (int w = 0; w < W; ++w) at += count[w][lane];
+    p.key_out[at] = key;
+    p.pos_out[at] = (uint32_t)i;
 }
 
 // --------------------------------------------------------------------- sums
@@ -341,13 +311,12 @@ constexpr uint32_t kNone = 0xffffffffu;
 
 struct SumArgs {
     const uint32_t *key, *pos;      // sorted
-    const uint8_t* named;           // null: rows without a token are left alone
     const void* grad;
     void* out;
     float* part;                    // [chunks][2][dim]: the run that a chunk begins in, the one that it ends in
     int64_t rows, ld_grad, ld_out;
-    int64_t units, fill_blocks;
-    int32_t n, dim, slabs, chunks, accumulate, fill_rows;
+    int64_t units;
+    int32_t n, dim, slabs, chunks, accumulate;
     float scale;
 };
 
@@ -372,18 +341,6 @@ template <GemmStore ST, GemmStore OT, int S> __global__ void __launch_bounds__(k
 {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t sum_blocks = (p.units + kThreads / kWave - 1) / (kThreads / kWave);
-    if ((int64_t)blockIdx.x >= sum_blocks) {  // rows without a token
-        const int64_t r0 = ((int64_t)blockIdx.x - sum_blocks) * (kThreads / kWave) * p.fill_rows + wave * p.fill_rows;
-        for (int64_t r = r0; r < min(r0 + p.fill_rows, p.rows); ++r) {
-            if (p.named[r]) continue;
-            for (int c = lane * 8; c < p.dim; c += kSlab) {
-                float z[8] = {};
-                store8<OT>(p.out, r * p.ld_out + c, min(8, p.dim - c), false, z);
-            }
-        }
-        return;
-    }
     const int64_t unit = (int64_t)blockIdx.x * (kThreads / kWave) + wave;
     if (unit >= p.units) return;
     const int chunk = (int)(unit / p.slabs);
@@ -432,7 +389,7 @@ template <GemmStore ST, GemmStore OT, int S> __global__ void __launch_bounds__(k
 // Adds up the partial sums of the runs that cross chunks: block (chunk, slab) has
 // the run that begins in its chunk and goes on after it. The later chunks are
 // shared out over the waves in order.
-constexpr int kJoinThreads = 512;
+constexpr int kJoinThreads = 256;
 template <GemmStore OT, int S> __global__ void __launch_bounds__(kJoinThreads) join_runs(const SumArgs p)
 {
     constexpr int W = kJoinThreads / kWave;
@@ -440,9 +397,9 @@ template <GemmStore OT, int S> __global__ void __launch_bounds__(kJoinThreads) j
     const int chunk = blockIdx.x;
     const int64_t first = (int64_t)chunk * S, after = first + S;
     if (after >= p.n) return;
-    const uint32_t key = p.key[after];
-    if (key >= (uint32_t)p.rows || p.key[after - 1] != key) return;
-    if (p.key[first] == key && first > 0 && p.key[first - 1] == key) return;  // began in an earlier chunk
+    const uint32_t key = p.key[after], end = p.key[after - 1], begin = p.key[first], previous = p.key[max(first - 1, (int64_t)0)];
+    if (key >= (uint32_t)p.rows || end != key) return;
+    if (begin == key && first > 0 && previous == key) return;  // began in an earlier chunk
     const int lane = threadIdx.x & 63;
     // the last chunk that holds a part: 64 chunks' first entries are asked at once
     int last = chunk + 1;
@@ -496,14 +453,11 @@ template <GemmStore ST, GemmStore OT, int S> int launch_sums(SumArgs p, hipStrea
 {
     p.chunks = (int)ceil_div(p.n, S);
     p.units = (int64_t)p.chunks * p.slabs;
-    const int64_t blocks = ceil_div(p.units, kThreads / kWave) + p.fill_blocks;
+    const int64_t blocks = ceil_div(p.units, kThreads / kWave);
     if (blocks > INT32_MAX || p.slabs > 65535) return HIMUON_ERR_UNSUPPORTED;
-    if (blocks > 0) {
-        hipLaunchKernelGGL((sum_runs<ST, OT, S>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
-        const int st = launch_status();
-        if (st != HIMUON_OK) return st;
-    }
-    if (p.chunks < 2) return HIMUON_OK;
+    hipLaunchKernelGGL((sum_runs<ST, OT, S>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
+    const int st = launch_status();
+    if (st != HIMUON_OK || p.chunks < 2) return st;
     hipLaunchKernelGGL((join_runs<OT, S>), dim3((unsigned)p.chunks, (unsigned)p.slabs), dim3(kJoinThreads), 0, stream, p);
     return launch_status();
 }
@@ -524,7 +478,7 @@ int key_bits(int64_t rows)
 }
 
 struct GradPlan {
-    size_t key[2], pos[2], hist, named, part, total;
+    size_t key[2], pos[2], hist, part, total;
     int digits, bits, tiles, chunk;
 };
 
@@ -547,9 +501,8 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
         g.pos[b] = take((size_t)n * 4);
     }
     g.hist = take(((size_t)g.tiles << g.bits) * 4);
-    g.named = take((size_t)rows);
     g.part = take((size_t)ceil_div(n, g.chunk) * 2 * (size_t)dim * 4);
-    g.total = at;
+    g.total = std::max<size_t>(at, 256);
     return g;
 }
 
@@ -621,44 +574,55 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
     SortArgs s{};
     s.tokens = tokens;
     s.hist = reinterpret_cast<uint32_t*>(ws + g.hist);
-    s.named = ws + g.named;
     s.rows = n_rows;
     s.n = (int32_t)n_tokens;
     s.wide = index == HIMUON_I64;
     s.tiles = g.tiles;
     s.bits = g.bits;
+    s.fill.out = static_cast<uint8_t*>(dtable);
+    s.fill.row_bytes = dim * dtype_size(out_dtype);
+    s.fill.ld_bytes = ld_dtable * dtype_size(out_dtype);
+    // launch `part` of `parts` of the sort, `blocks` blocks of its own and those that fill
+    auto with_fill = [&](int64_t part, int64_t parts, int64_t blocks, int threads) -> dim3 {
+        s.fill.from = n_rows * part / parts;
+        s.fill.to = n_rows * (part + 1) / parts;
+        s.fill.first = (int32_t)blocks;
+        s.fill.blocks = 0;
+        if (!accumulate)  // (a block fills about 64 bytes a thread and round)
+            s.fill.blocks = (int32_t)std::min<int64_t>(ceil_div((s.fill.to - s.fill.from) * s.fill.row_bytes, threads * 64), 8192);
+        return dim3((unsigned)(blocks + s.fill.blocks));
+    };
     int from = 0;
-    const bool small = n_tokens > 0 && n_tokens <= kSmall;
-    if (small) {
+    if (n_tokens <= kRankMost) {
         s.first = 1;
-        if (accumulate) s.named = nullptr;
         s.key_out = reinterpret_cast<uint32_t*>(ws + g.key[0]);
         s.pos_out = reinterpret_cast<uint32_t*>(ws + g.pos[0]);
-        hipLaunchKernelGGL(sort_small, dim3(1), dim3(kSmallThreads), 0, hs, s, g.digits);
+        const dim3 grid = with_fill(0, 1, ceil_div(n_tokens, kWave), kRankThreads);
+        hipLaunchKernelGGL(sort_rank, grid, dim3(kRankThreads), 0, hs, s);
         const int st = launch_status();
-        if (st != HIMUON_OK) return st;
-    }
-    for (int d = 0; !small && d < (n_tokens ? g.digits : 1); ++d) {
-        s.first = d == 0;
-        s.shift = d * g.bits;
-        s.key_in = reinterpret_cast<const uint32_t*>(ws + g.key[from]);
-        s.pos_in = reinterpret_cast<const uint32_t*>(ws + g.pos[from]);
-        s.key_out = reinterpret_cast<uint32_t*>(ws + g.key[from ^ 1]);
-        s.pos_out = reinterpret_cast<uint32_t*>(ws + g.pos[from ^ 1]);
-        from ^= 1;
-        const int clear = d == 0 ? (int)std::min<int64_t>(ceil_div(n_rows, kThreads * 16), 256) : 1;
-        hipLaunchKernelGGL(sort_count, dim3((unsigned)std::max(g.tiles, clear)), dim3(kThreads), 0, hs, s);
-        int st = launch_status();
-        if (st != HIMUON_OK) return st;
-        if (n_tokens == 0) break;
-        hipLaunchKernelGGL(sort_scatter, dim3((unsigned)g.tiles), dim3(kThreads), 0, hs, s);
-        st = launch_status();
-        if (st != HIMUON_OK) return st;
+        if (st != HIMUON_OK || n_tokens == 0) return st;
+    } else {
+        for (int d = 0; d < g.digits; ++d) {
+            s.first = d == 0;
+            s.shift = d * g.bits;
+            s.key_in = reinterpret_cast<const uint32_t*>(ws + g.key[from]);
+            s.pos_in = reinterpret_cast<const uint32_t*>(ws + g.pos[from]);
+            s.key_out = reinterpret_cast<uint32_t*>(ws + g.key[from ^ 1]);
+            s.pos_out = reinterpret_cast<uint32_t*>(ws + g.pos[from ^ 1]);
+            from ^= 1;
+            dim3 grid = with_fill(2 * d, 2 * g.digits, g.tiles, kThreads);
+            hipLaunchKernelGGL(sort_count, grid, dim3(kThreads), 0, hs, s);
+            int st = launch_status();
+            if (st != HIMUON_OK) return st;
+            grid = with_fill(2 * d + 1, 2 * g.digits, g.tiles, kThreads);
+            hipLaunchKernelGGL(sort_scatter, grid, dim3(kThreads), 0, hs, s);
+            st = launch_status();
+            if (st != HIMUON_OK) return st;
+        }
     }
     SumArgs p{};
     p.key = reinterpret_cast<const uint32_t*>(ws + g.key[from]);
     p.pos = reinterpret_cast<const uint32_t*>(ws + g.pos[from]);
-    p.named = accumulate ? nullptr : ws + g.named;
     p.grad = grad;
     p.out = dtable;
     p.part = reinterpret_cast<float*>(ws + g.part);
@@ -670,9 +634,6 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
     p.slabs = (int32_t)ceil_div(dim, kSlab);
     p.accumulate = accumulate != 0;
     p.scale = scale;
-    // about 16 KB to a wave
-    p.fill_rows = (int32_t)std::max<int64_t>(1, std::min<int64_t>(64, 16384 / (dim * dtype_size(out_dtype))));
-    p.fill_blocks = accumulate ? 0 : ceil_div(n_rows, (int64_t)p.fill_rows * (kThreads / kWave));
     if (dtype == HIMUON_BF16)
         return out_dtype == HIMUON_BF16 ? launch_sums_t<GemmStore::BF16, GemmStore::BF16>(p, g.chunk, hs)
                                         : launch_sums_t<GemmStore::BF16, GemmStore::F32>(p, g.chunk, hs);
