@@ -98,17 +98,21 @@ struct FillArgs {
     uint8_t* out;
     int64_t row_bytes, ld_bytes, from, to;  // rows
     int32_t first, blocks;
+    int32_t stream;  // past the caches
 };
 
-template <int THREADS> __device__ __forceinline__ void fill_rows(const FillArgs& f)
+template <int THREADS, bool STREAM> __device__ __forceinline__ void fill_rows_as(const FillArgs& f)
 {
     typedef uint32_t Chunk __attribute__((ext_vector_type(4)));
     typedef Chunk ChunkAny __attribute__((aligned(2)));
     const int64_t b = (int64_t)blockIdx.x - f.first;
     auto zero = [](uint8_t* p, int64_t n) {
-        if (n >= 16) *reinterpret_cast<ChunkAny*>(p) = Chunk{};
-        else
+        if (n >= 16) {
+            if constexpr (STREAM) __builtin_nontemporal_store(Chunk{}, reinterpret_cast<ChunkAny*>(p));
+            else *reinterpret_cast<ChunkAny*>(p) = Chunk{};
+        } else {
             for (int64_t i = 0; i < n; i += 2) *reinterpret_cast<uint16_t*>(p + i) = 0;
+        }
     };
     if (f.ld_bytes == f.row_bytes) {
         uint8_t* const base = f.out + f.from * f.ld_bytes;
@@ -119,6 +123,12 @@ template <int THREADS> __device__ __forceinline__ void fill_rows(const FillArgs&
         for (int64_t r = f.from + b * (THREADS / kWave) + (threadIdx.x >> 6); r < f.to; r += step)
             for (int64_t i = (threadIdx.x & 63) * 16; i < f.row_bytes; i += 1024) zero(f.out + r * f.ld_bytes + i, f.row_bytes - i);
     }
+}
+
+template <int THREADS> __device__ __forceinline__ void fill_rows(const FillArgs& f)
+{
+    if (f.stream) fill_rows_as<THREADS, true>(f);
+    else fill_rows_as<THREADS, false>(f);
 }
 
 // ------------------------------------------------------------------ sorting
@@ -344,7 +354,9 @@ template <GemmStore ST, GemmStore OT, int S> __global__ void __launch_bounds__(k
     const int64_t unit = (int64_t)blockIdx.x * (kThreads / kWave) + wave;
     if (unit >= p.units) return;
     const int chunk = (int)(unit / p.slabs);
-    const int c = (int)(unit - (int64_t)chunk * p.slabs) * kSlab + lane * 8;
+    const int lane_col = (int)(unit - (int64_t)chunk * p.slabs) * kSlab + lane * 8;
+    const bool col = lane_col < p.dim;  // (lanes past the last column read the first ones and store nothing)
+    const int c = col ? lane_col : 0;
     // lane l holds entry chunk S - 1 + l: the one before the chunk, its S, the one after
     const int64_t i = (int64_t)chunk * S - 1 + lane;
     const bool there = i >= 0 && i < p.n && lane < S + 2;
@@ -352,27 +364,31 @@ template <GemmStore ST, GemmStore OT, int S> __global__ void __launch_bounds__(k
     const uint32_t pos = there ? p.pos[i] : 0u;
     if (key >= (uint32_t)p.rows) key = kNone;
     const int count = __popcll(__ballot(key != kNone && lane >= 1 && lane <= S));  // sorted: the first ones
-    const bool col = c < p.dim;
     const int nc = min(8, p.dim - c);
     float acc[8] = {};
     bool begun = count > 0 && lane_value(key, 0) != lane_value(key, 1);  // the current run began in this chunk
-    constexpr int B = 8;
-    for (int e0 = 0; e0 < count; e0 += B) {
-        float v[B][8];
+    // rows of B entries are in flight while those before them are summed
+    constexpr int B = ST == GemmStore::BF16 ? 8 : 4;
+    Raw8<ST> cur[B], next[B];
+    auto load = [&](Raw8<ST> (&v)[B], int e0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < B; ++e) {
-            if (e0 + e < count && col)
-                load8<ST>(p.grad, (int64_t)lane_value(pos, e0 + e + 1) * p.ld_grad + c, nc, false, v[e]);
-        }
+        for (int e = 0; e < B; ++e)
+            v[e] = get_raw8<ST>(p.grad, (int64_t)lane_value(pos, min(e0 + e, count - 1) + 1) * p.ld_grad + c, nc);
+    };
+    if (count == 0) return;
+    load(next, 0);
+#pragma unroll 1
+    for (int e0 = 0; e0 < count; e0 += B) {
+#pragma unroll
+        for (int e = 0; e < B; ++e) cur[e] = next[e];
+        if (e0 + B < count) load(next, e0 + B);
 #pragma unroll
         for (int e = 0; e < B; ++e) {
             if (e0 + e >= count) break;
             const uint32_t k = lane_value(key, e0 + e + 1);
             const bool last = lane_value(key, e0 + e + 2) != k;
-            if (col) {
 #pragma unroll
-                for (int x = 0; x < 8; ++x) acc[x] += v[e][x];
-            }
+            for (int x = 0; x < 8; ++x) acc[x] += raw_value<ST>(cur[e], x);
             if (last || e0 + e + 1 == S) {
                 if (col) {
                     if (begun && last) put_row<OT>(p, k, c, acc);
@@ -386,67 +402,88 @@ template <GemmStore ST, GemmStore OT, int S> __global__ void __launch_bounds__(k
     }
 }
 
-// Adds up the partial sums of the runs that cross chunks: block (chunk, slab) has
-// the run that begins in its chunk and goes on after it. The later chunks are
-// shared out over the waves in order.
-constexpr int kJoinThreads = 256;
-template <GemmStore OT, int S> __global__ void __launch_bounds__(kJoinThreads) join_runs(const SumArgs p)
+// Adds up the partial sums of the runs that cross chunks. A wave has the run that begins in
+// its chunk and goes on after it; runs of more than kOwnParts parts are shared out over all
+// waves of the block, in order (one token 30000 times, 640 columns: the whole call 60 us
+// with each run left to four waves, 50 so).
+constexpr int kOwnParts = 32;
+
+template <GemmStore OT, int S, int kJoinWaves> __global__ void __launch_bounds__(kJoinWaves * kWave) join_runs(const SumArgs p)
 {
-    constexpr int W = kJoinThreads / kWave;
-    __shared__ float part[W - 1][kWave][8 + 1];
-    const int chunk = blockIdx.x;
-    const int64_t first = (int64_t)chunk * S, after = first + S;
-    if (after >= p.n) return;
-    const uint32_t key = p.key[after], end = p.key[after - 1], begin = p.key[first], previous = p.key[max(first - 1, (int64_t)0)];
-    if (key >= (uint32_t)p.rows || end != key) return;
-    if (begin == key && first > 0 && previous == key) return;  // began in an earlier chunk
+    __shared__ float lds[kJoinWaves][kWave][8 + 1];
+    __shared__ int parts[kJoinWaves];  // of each wave's run, if it is shared out
     const int lane = threadIdx.x & 63;
-    // the last chunk that holds a part: 64 chunks' first entries are asked at once
-    int last = chunk + 1;
-    for (;;) {
-        const int64_t i = (int64_t)(last + 1 + lane) * S;
-        const uint64_t ends = __ballot(i >= p.n || p.key[min(i, (int64_t)p.n - 1)] != key);
-        if (ends) {
-            last += __ffsll((unsigned long long)ends) - 1;
-            break;
-        }
-        last += 64;
-    }
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c = blockIdx.y * kSlab + lane * 8;
-    const int nc = min(8, p.dim - c);
-    const int m = last - chunk, per = (m + W - 1) / W;
-    const int from = chunk + 1 + wave * per, to = min(from + per, last + 1);
+    const int chunk = blockIdx.x * kJoinWaves + wave;
+    const int c = blockIdx.y * kSlab + lane * 8, nc = min(8, p.dim - c);
+    const int64_t first = (int64_t)chunk * S, after = first + S, most = (int64_t)p.n - 1;
+    const uint32_t before = p.key[min(max(first - 1, (int64_t)0), most)], begin = p.key[min(first, most)],
+                   end = p.key[min(after - 1, most)], next = p.key[min(after, most)];
+    int n = 0;  // chunks after this one that the run reaches into
+    if (after <= most && next == end && end < (uint32_t)p.rows && !(begin == end && first > 0 && before == end)) {
+        // 64 chunks' first entries are asked at once, `step` apart; how many belong to the run
+        auto ask = [&](int64_t from, int64_t step) -> int {
+            const int64_t i = (from + lane * step) * S;
+            const uint64_t out = __ballot(i > most || p.key[min(i, most)] != end);
+            return out ? __ffsll((unsigned long long)out) - 1 : kWave;
+        };
+        n = ask(chunk + 1, 1);
+        if (n == kWave) {
+            for (;;) {
+                const int m = ask((int64_t)chunk + 1 + n, kWave);  // (its first one need not be)
+                if (m == 0) break;
+                n += (m - 1) * kWave;
+                if (m < kWave) break;
+            }
+            n += ask((int64_t)chunk + 1 + n, 1);
+        }
+    }
     float acc[8] = {};
-    if (c < p.dim) {
-        if (wave == 0) load8<GemmStore::F32>(p.part, (2 * (int64_t)chunk + 1) * p.dim + c, nc, false, acc);
+    // adds parts from .. to - 1 of the run that begins in chunk `at` (0: that chunk's own)
+    auto add = [&](int at, int from, int to) __attribute__((always_inline)) {
         constexpr int B = 8;
         for (int k0 = from; k0 < to; k0 += B) {
             float v[B][8];
 #pragma unroll
-            for (int b = 0; b < B; ++b)
-                if (k0 + b < to) load8<GemmStore::F32>(p.part, 2 * (int64_t)(k0 + b) * p.dim + c, nc, false, v[b]);
+            for (int b = 0; b < B; ++b) {
+                const int k = min(k0 + b, to - 1);
+                load8<GemmStore::F32>(p.part, (2 * (int64_t)(at + k) + (k == 0 ? 1 : 0)) * p.dim + c, nc, false, v[b]);
+            }
 #pragma unroll
             for (int b = 0; b < B; ++b) {
-                if (k0 + b < to) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) acc[e] += v[b][e];
-                }
+                for (int e = 0; e < 8; ++e) acc[e] += k0 + b < to ? v[b][e] : 0.f;
             }
         }
-    }
-    if (wave > 0) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) part[wave - 1][lane][e] = acc[e];
+    };
+    const bool shared_out = n + 1 > kOwnParts;
+    if (lane == 0) parts[wave] = shared_out ? n + 1 : 0;
+    if (n > 0 && !shared_out && c < p.dim) {
+        add(chunk, 0, n + 1);
+        put_row<OT>(p, end, c, acc);
     }
     __syncthreads();
-    if (wave > 0 || c >= p.dim) return;
+    for (int w = 0; w < kJoinWaves; ++w) {
+        const int m = __builtin_amdgcn_readfirstlane(parts[w]);
+        if (m == 0) continue;
+        const int per = (m + kJoinWaves - 1) / kJoinWaves, from = min(wave * per, m), to = min(from + per, m);
 #pragma unroll
-    for (int w = 0; w < W - 1; ++w) {
+        for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+        if (c < p.dim) add(blockIdx.x * kJoinWaves + w, from, to);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += part[w][lane][e];
+        for (int e = 0; e < 8; ++e) lds[wave][lane][e] = acc[e];
+        __syncthreads();
+        if (wave == w && c < p.dim) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = lds[0][lane][e];
+            for (int x = 1; x < kJoinWaves; ++x) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] += lds[x][lane][e];
+            }
+            put_row<OT>(p, end, c, acc);
+        }
+        __syncthreads();
     }
-    put_row<OT>(p, key, c, acc);
 }
 
 template <GemmStore ST, GemmStore OT, int S> int launch_sums(SumArgs p, hipStream_t stream)
@@ -458,7 +495,12 @@ template <GemmStore ST, GemmStore OT, int S> int launch_sums(SumArgs p, hipStrea
     hipLaunchKernelGGL((sum_runs<ST, OT, S>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
     const int st = launch_status();
     if (st != HIMUON_OK || p.chunks < 2) return st;
-    hipLaunchKernelGGL((join_runs<OT, S>), dim3((unsigned)p.chunks, (unsigned)p.slabs), dim3(kJoinThreads), 0, stream, p);
+    // (a block of 16 waves starts later than one of four: 1500 tokens 21.2 us and 18.5)
+    if (p.n <= 2048)
+        hipLaunchKernelGGL((join_runs<OT, S, 4>), dim3((unsigned)ceil_div(p.chunks, 4), (unsigned)p.slabs), dim3(4 * kWave), 0, stream, p);
+    else
+        hipLaunchKernelGGL((join_runs<OT, S, 16>), dim3((unsigned)ceil_div(p.chunks, 16), (unsigned)p.slabs), dim3(16 * kWave), 0, stream,
+                           p);
     return launch_status();
 }
 
@@ -468,7 +510,10 @@ template <GemmStore ST, GemmStore OT> int launch_sums_t(const SumArgs& p, int s,
 }
 
 // Entries per chunk: short chunks while long ones would leave much of the chip idle.
-int chunk_size(int64_t n, int64_t dim) { return ceil_div(n, 32) * ceil_div(dim, kSlab) < 2048 ? 8 : 32; }
+int chunk_size(int64_t n)
+{
+    return n <= 8192 ? 8 : 32;
+}
 
 int key_bits(int64_t rows)
 {
@@ -489,7 +534,7 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
     g.digits = (kb + 9) / 10;
     g.bits = std::max(2, (kb + g.digits - 1) / g.digits);  // (bins in groups of four)
     g.tiles = (int)ceil_div(n, kTile);
-    g.chunk = chunk_size(n, dim);
+    g.chunk = chunk_size(n);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t o = at;
@@ -582,6 +627,11 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
     s.fill.out = static_cast<uint8_t*>(dtable);
     s.fill.row_bytes = dim * dtype_size(out_dtype);
     s.fill.ld_bytes = ld_dtable * dtype_size(out_dtype);
+    // Zeros go past the caches where the rows to be summed are many enough to be worth their
+    // place there. 16384 x 4096 (134 MB) into 32000 rows 92 us so, 119 not; 32768 x 2048
+    // into 50000 of fp32 120 and 150; but 4096 x 2560 (21 MB) into 32000 50 and 42, 2000 x
+    // 4096 (16 MB) 62 and 49.
+    s.fill.stream = n_tokens * dim * dtype_size(dtype) >= (INT64_C(64) << 20);
     // launch `part` of `parts` of the sort, `blocks` blocks of its own and those that fill
     auto with_fill = [&](int64_t part, int64_t parts, int64_t blocks, int threads) -> dim3 {
         s.fill.from = n_rows * part / parts;

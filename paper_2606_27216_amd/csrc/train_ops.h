@@ -39,6 +39,47 @@ __device__ __forceinline__ int64_t load_index(const void* p, int64_t i, bool wid
 // and to any address that is a multiple of the element's size.
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
+// The same as they lie in memory, the first n of them (loads in flight take half the
+// registers, and no instruction waits for them before they are used).
+template <GemmStore ST> struct Raw8 {
+    Chunk4 w[ST == GemmStore::BF16 ? 1 : 2];
+};
+
+template <GemmStore ST> __device__ __forceinline__ Raw8<ST> get_raw8(const void* base, int64_t i, int n)
+{
+    Raw8<ST> r;
+    if constexpr (ST == GemmStore::BF16) {
+        const uint16_t* const p = static_cast<const uint16_t*>(base) + i;
+        if (n == 8) {
+            r.w[0] = *reinterpret_cast<const Chunk4Any16*>(p);
+        } else {
+            uint32_t h[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] = e < n ? p[e] : 0u;
+            r.w[0] = Chunk4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+        }
+    } else {
+        const float* const p = static_cast<const float*>(base) + i;
+        if (n == 8) {
+            r.w[0] = *reinterpret_cast<const Chunk4Any32*>(p);
+            r.w[1] = *reinterpret_cast<const Chunk4Any32*>(p + 4);
+        } else {
+            uint32_t h[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] = e < n ? __float_as_uint(p[e]) : 0u;
+            r.w[0] = Chunk4{h[0], h[1], h[2], h[3]};
+            r.w[1] = Chunk4{h[4], h[5], h[6], h[7]};
+        }
+    }
+    return r;
+}
+
+template <GemmStore ST> __device__ __forceinline__ float raw_value(const Raw8<ST>& r, int e)
+{
+    if constexpr (ST == GemmStore::BF16) return __uint_as_float((e & 1) ? (r.w[0][e >> 1] & 0xffff0000u) : (r.w[0][e >> 1] << 16));
+    else return __uint_as_float(r.w[e >> 2][e & 3]);
+}
+
 template <GemmStore ST> __device__ __forceinline__ f32x8 get8(const void* base, int64_t i)
 {
     float v[8];
