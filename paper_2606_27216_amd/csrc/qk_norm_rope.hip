@@ -8,10 +8,12 @@
 // so one pass over x (and dy) is all there is to read: both sums over a head are
 // taken at once, and r is computed again in the backward pass.
 //
-// A head is 8 pairs to a lane: L lanes hold it, a wave 64 / L heads of one token. The
-// two elements of a pair sit in one lane, so the rotation needs no exchange, and a
-// token's cosines and sines and the gains stay in registers while the wave walks
-// over its heads. Memory bounds it.
+// A lane holds eight pairs of a head, both elements of each, so the rotation needs no
+// exchange; L lanes hold the head, a wave 64 / L heads. Where heads are many, a wave walks over
+// those of one token, whose cosines and sines stay in registers with the gains. Where a
+// token's heads fit the wave, each group of lanes keeps one head and the wave walks over
+// tokens, several at a time. Memory bounds it: 8 x 1024 tokens, 32 + 32 heads of 128, bf16, forward
+// 48 us (273 MB, 5.7 TB/s); 16 x 1024 tokens, 16 + 8 heads, backward 72 us (306 MB, 4.3 TB/s).
 #include "elementwise8.h"
 #include "train_ops.h"
 
@@ -37,7 +39,7 @@ struct QkArgs {
     const void* positions;
     float* part;                   // backward: [blocks][2][D]
     int64_t tokens, seq, table_rows, units;
-    int32_t hq, hk, dim, rot, wide, parts, gain_bf16;
+    int32_t hq, hk, dim, rot, wide, parts, gain_bf16, slots;
     float eps, inv_dim;
 };
 
@@ -52,30 +54,47 @@ template <int L> __device__ __forceinline__ float head_sum(float v)
     if constexpr (L >= 8) v += dpp(v, std::integral_constant<int, 0x141>{});  // the other four of eight
     if constexpr (L >= 16) v += dpp(v, std::integral_constant<int, 0x140>{}); // the other eight of sixteen
     if constexpr (L >= 32) v += __shfl_xor(v, 16);
+    if constexpr (L >= 64) v += __shfl_xor(v, 32);
     return v;
 }
 
-// Where the eight pairs of a lane lie in a head: first elements a, a + 1, .., second
-// ones b, b + 1, ..; or (INTER) 16 elements from a on, pairs side by side.
+// The pairs of a head: the rotated ones first, then the others, each kind in runs of eight;
+// the last run of a kind ends with its last pair and repeats pairs of the run before it
+// where their number is no multiple of eight.
 struct Place {
-    int a, b, pair, n;  // n: pairs that exist
+    int pair;     // the run's first pair
+    int n;        // pairs that exist: 8, fewer if there are no eight of the kind, 0 for an idle lane
+    int skip;     // leading ones that the run before has too: not to be counted again
+    int a, b;     // first and second element of the first pair (the next ones follow; with INTER, side by side)
 };
 
-template <bool INTER> __device__ __forceinline__ Place place(int pair, int dim, int rot)
+template <bool INTER> __device__ __forceinline__ void pair_elements(int pair, int dim, int rot, int& a, int& b)
 {
-    Place w;
-    w.pair = pair;
-    w.n = max(0, min(8, dim / 2 - pair));
+    const int turned = rot / 2, rest = (dim - rot) / 2;
     if (INTER) {
-        w.a = 2 * pair;
-        w.b = 2 * pair + 1;
-    } else if (pair < rot / 2) {
-        w.a = pair;
-        w.b = rot / 2 + pair;
+        a = 2 * pair;
+        b = a + 1;
+    } else if (pair < turned) {
+        a = pair;
+        b = turned + pair;
     } else {
-        w.a = rot + (pair - rot / 2);
-        w.b = w.a + (dim - rot) / 2;
+        a = rot + pair - turned;
+        b = a + rest;
     }
+}
+
+template <bool INTER> __device__ __forceinline__ Place place(int l, int dim, int rot)
+{
+    const int turned = rot / 2, rest = (dim - rot) / 2, runs = (turned + 7) / 8;
+    const bool second = l >= runs;
+    const int r = second ? l - runs : l, first = second ? turned : 0, count = second ? rest : turned;
+    Place w;
+    w.n = max(0, min(8, count - 8 * r));
+    const int start = w.n > 0 ? min(8 * r, max(0, count - 8)) : 0;
+    w.skip = w.n > 0 ? 8 * r - start : 0;
+    if (w.n > 0) w.n = min(8, count);
+    w.pair = w.n > 0 ? first + start : 0;
+    pair_elements<INTER>(w.pair, dim, rot, w.a, w.b);
     return w;
 }
 
@@ -84,46 +103,47 @@ struct Pairs {
     f32x8 u, v;
 };
 
-// The lane's pairs of the vector at base + i. (VEC: eight whole pairs in runs of
-// elements; lanes past the head read its first pairs and get zeros.)
-template <GemmStore ST, bool INTER, bool VEC>
-__device__ __forceinline__ Pairs load_pairs(const void* base, int64_t i, const Place& w, int dim, int rot)
+// The lane's pairs of the vector at base + i. VEC: whole runs (idle lanes read the first
+// one); otherwise runs may be short.
+template <GemmStore ST, bool INTER, bool VEC> __device__ __forceinline__ Pairs load_pairs(const void* base, int64_t i, const Place& w)
 {
     Pairs x;
-    if constexpr (VEC) {
-        const bool on = w.n > 0;
+    if (VEC || w.n == 8 || w.n == 0) {
         if constexpr (INTER) {
-            const int a = on ? w.a : 0;
-            const f32x8 lo = get8<ST>(base, i + a), hi = get8<ST>(base, i + a + 8);
+            // (a head of fewer than eight pairs has no whole run: its idle lanes read nothing)
+            if (!VEC && w.n == 0) {
+                x.u = x.v = f32x8{};
+                return x;
+            }
+            const f32x8 lo = get8<ST>(base, i + w.a), hi = get8<ST>(base, i + w.a + 8);
             x.u = f32x8{lo[0], lo[2], lo[4], lo[6], hi[0], hi[2], hi[4], hi[6]};
             x.v = f32x8{lo[1], lo[3], lo[5], lo[7], hi[1], hi[3], hi[5], hi[7]};
         } else {
-            x.u = get8<ST>(base, i + (on ? w.a : 0));
-            x.v = get8<ST>(base, i + (on ? w.b : 0));
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x.u[e] = on ? x.u[e] : 0.f;
-            x.v[e] = on ? x.v[e] : 0.f;
+            if (!VEC && w.n == 0) {
+                x.u = x.v = f32x8{};
+                return x;
+            }
+            x.u = get8<ST>(base, i + w.a);
+            x.v = get8<ST>(base, i + w.b);
         }
     } else {
+        constexpr int STEP = INTER ? 2 : 1;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const bool on = e < w.n;
-            const Place q = place<INTER>(on ? w.pair + e : 0, dim, rot);
-            const float a = get1<ST>(base, i + q.a), b = get1<ST>(base, i + q.b);
-            x.u[e] = on ? a : 0.f;
-            x.v[e] = on ? b : 0.f;
+            const int k = STEP * min(e, w.n - 1);
+            const float a = get1<ST>(base, i + w.a + k), b = get1<ST>(base, i + w.b + k);
+            x.u[e] = e < w.n ? a : 0.f;
+            x.v[e] = e < w.n ? b : 0.f;
         }
     }
     return x;
 }
 
 template <GemmStore ST, bool INTER, bool VEC>
-__device__ __forceinline__ void store_pairs(void* base, int64_t i, const Place& w, int dim, int rot, const Pairs& x)
+__device__ __forceinline__ void store_pairs(void* base, int64_t i, const Place& w, const Pairs& x)
 {
-    if constexpr (VEC) {
-        if (w.n == 0) return;
+    if (w.n == 0) return;
+    if (VEC || w.n == 8) {
         if constexpr (INTER) {
             put8<ST>(base, i + w.a, f32x8{x.u[0], x.v[0], x.u[1], x.v[1], x.u[2], x.v[2], x.u[3], x.v[3]});
             put8<ST>(base, i + w.a + 8, f32x8{x.u[4], x.v[4], x.u[5], x.v[5], x.u[6], x.v[6], x.u[7], x.v[7]});
@@ -132,38 +152,45 @@ __device__ __forceinline__ void store_pairs(void* base, int64_t i, const Place& 
             put8<ST>(base, i + w.b, x.v);
         }
     } else {
+        constexpr int STEP = INTER ? 2 : 1;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             if (e < w.n) {
-                const Place q = place<INTER>(w.pair + e, dim, rot);
-                put1<ST>(base, i + q.a, x.u[e]);
-                put1<ST>(base, i + q.b, x.v[e]);
+                put1<ST>(base, i + w.a + STEP * e, x.u[e]);
+                put1<ST>(base, i + w.b + STEP * e, x.v[e]);
             }
         }
     }
 }
 
+// Whether pair e of the lane counts in sums over the head. (VEC: all of a lane's do, or none.)
+template <bool VEC> __device__ __forceinline__ bool counts(const Place& w, int e)
+{
+    return VEC ? w.n > 0 : e >= w.skip && e < w.n;
+}
+
 template <bool INTER, bool VEC> __device__ __forceinline__ Pairs load_gains(const QkArgs& p, const void* gain, const Place& w)
 {
-    if (p.gain_bf16) return load_pairs<GemmStore::BF16, INTER, VEC>(gain, 0, w, p.dim, p.rot);
-    return load_pairs<GemmStore::F32, INTER, VEC>(gain, 0, w, p.dim, p.rot);
+    if (p.gain_bf16) return load_pairs<GemmStore::BF16, INTER, VEC>(gain, 0, w);
+    return load_pairs<GemmStore::F32, INTER, VEC>(gain, 0, w);
 }
 
 // The lane's cosines (u) and sines (v) of position t: 1 and 0 for what is not rotated.
-__device__ __forceinline__ Pairs load_turn(const QkArgs& p, int64_t t, const Place& w)
+template <bool VEC> __device__ __forceinline__ Pairs load_turn(const QkArgs& p, int64_t t, const Place& w, bool used = true)
 {
     const int half = p.rot / 2;
     const int64_t i = t * half + w.pair;
     Pairs x;
     x.u = f32x8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
     x.v = f32x8{};
-    if (w.pair + 8 <= half) {
+    if (w.pair >= half || !used) return x;  // (a run lies in one part)
+    if (VEC || w.n == 8) {
         x.u = get8<GemmStore::F32>(p.cs, i);
         x.v = get8<GemmStore::F32>(p.sn, i);
-    } else if (w.pair < half) {
+    } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if (w.pair + e < half) {
+            if (e < w.n) {
                 x.u[e] = p.cs[i + e];
                 x.v[e] = p.sn[i + e];
             }
@@ -181,7 +208,51 @@ __device__ __forceinline__ bool token_position(const QkArgs& p, int64_t token, i
     return in;
 }
 
-// x -> R (r x w) for the heads of one token that fall to this wave.
+// x -> R (r x w), the head's sum over L lanes.
+template <bool VEC, int L>
+__device__ __forceinline__ void forward_head(const QkArgs& p, const Place& w, const Pairs& g, const Pairs& turn, bool used, Pairs& x)
+{
+    float sq = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sq += counts<VEC>(w, e) ? x.u[e] * x.u[e] + x.v[e] * x.v[e] : 0.f;
+    const float r = rsqrtf(head_sum<L>(sq) * p.inv_dim + p.eps);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float z0 = x.u[e] * r * g.u[e], z1 = x.v[e] * r * g.v[e];
+        x.u[e] = used ? z0 * turn.u[e] - z1 * turn.v[e] : 0.f;
+        x.v[e] = used ? z1 * turn.u[e] + z0 * turn.v[e] : 0.f;
+    }
+}
+
+// x, y = dL/d(output) -> x = dL/dx, d += the gain's terms.
+template <bool VEC, int L>
+__device__ __forceinline__ void backward_head(const QkArgs& p, const Place& w, const Pairs& g, const Pairs& turn, bool used, Pairs& x,
+                                              Pairs& y, Pairs& d)
+{
+    float sq = 0.f, dot = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float a = y.u[e] * turn.u[e] + y.v[e] * turn.v[e], c = y.v[e] * turn.u[e] - y.u[e] * turn.v[e];
+        y.u[e] = a;  // dz
+        y.v[e] = c;
+        sq += counts<VEC>(w, e) ? x.u[e] * x.u[e] + x.v[e] * x.v[e] : 0.f;
+        dot += counts<VEC>(w, e) ? a * g.u[e] * x.u[e] + c * g.v[e] * x.v[e] : 0.f;
+    }
+    sq = head_sum<L>(sq);
+    dot = head_sum<L>(dot);
+    const float r = rsqrtf(sq * p.inv_dim + p.eps);
+    const float m = r * r * (dot * p.inv_dim);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        d.u[e] += used ? y.u[e] * (x.u[e] * r) : 0.f;
+        d.v[e] += used ? y.v[e] * (x.v[e] * r) : 0.f;
+        x.u[e] = used ? r * (y.u[e] * g.u[e] - x.u[e] * m) : 0.f;
+        x.v[e] = used ? r * (y.v[e] * g.v[e] - x.v[e] * m) : 0.f;
+    }
+}
+
+// ------------------------------------------------------- many heads: a wave, one token
+
 template <GemmStore ST, bool INTER, bool VEC, int L>
 __device__ __forceinline__ void forward_heads(const QkArgs& p, const Strided& in, const Strided& out, const void* gain, int heads,
                                               int part, int64_t b, int64_t s, bool used, const Place& w, const Pairs& turn)
@@ -191,18 +262,9 @@ __device__ __forceinline__ void forward_heads(const QkArgs& p, const Strided& in
     const Pairs g = load_gains<INTER, VEC>(p, gain, w);
     const int64_t bi = b * in.sb + s * in.ss, bo = b * out.sb + s * out.ss;
     for (int h = part * G + lane / L; h < heads; h += p.parts * G) {
-        Pairs x = load_pairs<ST, INTER, VEC>(in.ptr, bi + h * in.sh, w, p.dim, p.rot);
-        float sq = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sq += x.u[e] * x.u[e] + x.v[e] * x.v[e];
-        const float r = rsqrtf(head_sum<L>(sq) * p.inv_dim + p.eps);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float z0 = x.u[e] * r * g.u[e], z1 = x.v[e] * r * g.v[e];
-            x.u[e] = used ? z0 * turn.u[e] - z1 * turn.v[e] : 0.f;
-            x.v[e] = used ? z1 * turn.u[e] + z0 * turn.v[e] : 0.f;
-        }
-        store_pairs<ST, INTER, VEC>(out.ptr, bo + h * out.sh, w, p.dim, p.rot, x);
+        Pairs x = load_pairs<ST, INTER, VEC>(in.ptr, bi + h * in.sh, w);
+        forward_head<VEC, L>(p, w, g, turn, used, x);
+        store_pairs<ST, INTER, VEC>(out.ptr, bo + h * out.sh, w, x);
     }
 }
 
@@ -213,11 +275,11 @@ template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bo
     const int64_t token = unit / p.parts;
     const int part = (int)(unit - token * p.parts);
     const int64_t b = token / p.seq, s = token - b * p.seq;
-    const Place w = place<INTER>(8 * (threadIdx.x & (L - 1)), p.dim, p.rot);
+    const Place w = place<INTER>(threadIdx.x & (L - 1), p.dim, p.rot);
     int64_t t;
     const bool used = token_position(p, token, s, t);
     Pairs turn{};
-    if (used) turn = load_turn(p, t, w);
+    if (used) turn = load_turn<VEC>(p, t, w);
     forward_heads<ST, INTER, VEC, L>(p, p.q, p.qo, p.wq, p.hq, part, b, s, used, w, turn);
     forward_heads<ST, INTER, VEC, L>(p, p.k, p.ko, p.wk, p.hk, part, b, s, used, w, turn);
 }
@@ -231,73 +293,148 @@ __device__ __forceinline__ void backward_heads(const QkArgs& p, const Strided& i
     const int lane = threadIdx.x & 63;
     const int64_t bi = b * in.sb + s * in.ss, bg = b * grad.sb + s * grad.ss, bo = b * out.sb + s * out.ss;
     for (int h = lane / L; h < heads; h += G) {
-        Pairs x = load_pairs<ST, INTER, VEC>(in.ptr, bi + h * in.sh, w, p.dim, p.rot);
-        Pairs y = load_pairs<ST, INTER, VEC>(grad.ptr, bg + h * grad.sh, w, p.dim, p.rot);
-        float sq = 0.f, dot = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float a = y.u[e] * turn.u[e] + y.v[e] * turn.v[e], c = y.v[e] * turn.u[e] - y.u[e] * turn.v[e];
-            y.u[e] = a;  // dz
-            y.v[e] = c;
-            sq += x.u[e] * x.u[e] + x.v[e] * x.v[e];
-            dot += a * g.u[e] * x.u[e] + c * g.v[e] * x.v[e];
-        }
-        sq = head_sum<L>(sq);
-        dot = head_sum<L>(dot);
-        const float r = rsqrtf(sq * p.inv_dim + p.eps);
-        const float m = r * r * (dot * p.inv_dim);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            d.u[e] += used ? y.u[e] * (x.u[e] * r) : 0.f;
-            d.v[e] += used ? y.v[e] * (x.v[e] * r) : 0.f;
-            x.u[e] = used ? r * (y.u[e] * g.u[e] - x.u[e] * m) : 0.f;
-            x.v[e] = used ? r * (y.v[e] * g.v[e] - x.v[e] * m) : 0.f;
-        }
-        store_pairs<ST, INTER, VEC>(out.ptr, bo + h * out.sh, w, p.dim, p.rot, x);
+        Pairs x = load_pairs<ST, INTER, VEC>(in.ptr, bi + h * in.sh, w);
+        Pairs y = load_pairs<ST, INTER, VEC>(grad.ptr, bg + h * grad.sh, w);
+        backward_head<VEC, L>(p, w, g, turn, used, x, y, d);
+        store_pairs<ST, INTER, VEC>(out.ptr, bo + h * out.sh, w, x);
     }
 }
 
-// A wave takes tokens `units` apart; its sums for the gains stay in registers until
-// the end, when the block adds its own up in LDS and leaves one row of partial sums.
+// Element x (first or second of pair x / 2) of a block's partial sums for a gain.
+template <bool INTER> __device__ __forceinline__ void put_gain(const QkArgs& p, int key, int x, float v)
+{
+    int a, b;
+    pair_elements<INTER>(x >> 1, p.dim, p.rot, a, b);
+    p.part[((int64_t)blockIdx.x * 2 + key) * p.dim + (x & 1 ? b : a)] = v;
+}
+
+// Blocks (.., 0) have the queries, (.., 1) the keys: one gain and one set of sums in
+// registers. A wave takes tokens `units` apart; its sums stay in registers until the
+// end, when the block adds its own up in LDS and leaves a row of partial sums.
 template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bounds__(kThreads) qk_backward(const QkArgs p)
 {
-    __shared__ float sums[kWaves][2][L * 16];
+    __shared__ float sums[kWaves][L * 16];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place w = place<INTER>(8 * (threadIdx.x & (L - 1)), p.dim, p.rot);
-    const Pairs gq = load_gains<INTER, VEC>(p, p.wq, w), gk = load_gains<INTER, VEC>(p, p.wk, w);
-    Pairs dq{}, dk{};
+    const int key = blockIdx.y;
+    const Place w = place<INTER>(threadIdx.x & (L - 1), p.dim, p.rot);
+    const Strided in = key ? p.k : p.q, grad = key ? p.gk : p.gq, out = key ? p.ko : p.qo;
+    const int heads = key ? p.hk : p.hq;
+    const Pairs g = load_gains<INTER, VEC>(p, key ? p.wk : p.wq, w);
+    Pairs d{};
     for (int64_t token = (int64_t)blockIdx.x * kWaves + wave; token < p.tokens; token += p.units) {
         const int64_t b = token / p.seq, s = token - b * p.seq;
         int64_t t;
         const bool used = token_position(p, token, s, t);
-        Pairs turn{};
-        if (used) turn = load_turn(p, t, w);
-        backward_heads<ST, INTER, VEC, L>(p, p.q, p.gq, p.qo, gq, p.hq, b, s, used, w, turn, dq);
-        backward_heads<ST, INTER, VEC, L>(p, p.k, p.gk, p.ko, gk, p.hk, b, s, used, w, turn, dk);
+        const Pairs turn = load_turn<VEC>(p, t, w, used);
+        backward_heads<ST, INTER, VEC, L>(p, in, grad, out, g, heads, b, s, used, w, turn, d);
     }
-    const int l = lane & (L - 1);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        float v[4] = {dq.u[e], dq.v[e], dk.u[e], dk.v[e]};
+        float u = d.u[e], v = d.v[e];
 #pragma unroll
         for (int o = L; o < 64; o <<= 1) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] += __shfl_xor(v[x], o);
+            u += __shfl_xor(u, o);
+            v += __shfl_xor(v, o);
         }
-        if (lane < L) {
+        if (lane < L && counts<VEC>(w, e)) {
+            sums[wave][2 * (w.pair + e)] = u;
+            sums[wave][2 * (w.pair + e) + 1] = v;
+        }
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < p.dim; x += kThreads) {
+        float v = 0.f;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) sums[wave][x >> 1][16 * l + 2 * e + (x & 1)] = v[x];
+        for (int wv = 0; wv < kWaves; ++wv) v += sums[wv][x];
+        put_gain<INTER>(p, key, x, v);
+    }
+}
+
+// ------------------------------------- few heads: a group of lanes, one head; a wave, tokens
+
+// A wave has 64 / L groups of lanes, `slots` of them (a power of two, the heads of a token
+// rounded up) to a token. What a group without a head or a token does is not stored.
+__device__ __forceinline__ int token_of(const QkArgs& p, int64_t first, int in_wave, bool& live, int64_t& b, int64_t& s)
+{
+    const int64_t token = first + in_wave;
+    live = token < p.tokens;
+    const uint32_t t = (uint32_t)(live ? token : p.tokens - 1), q = t / (uint32_t)p.seq;
+    b = q;
+    s = t - q * (uint32_t)p.seq;
+    return (int)t;
+}
+
+template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bounds__(kThreads) qk_forward_few(const QkArgs p)
+{
+    const int lane = threadIdx.x & 63, group = lane / L, slot = group & (p.slots - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tokens = 64 / L / p.slots;  // of a wave at a time
+    const Place w = place<INTER>(threadIdx.x & (L - 1), p.dim, p.rot);
+    const bool head = slot < p.hq + p.hk, key = head && slot >= p.hq;
+    const int h = !head ? 0 : key ? slot - p.hq : slot;
+    const Pairs g = load_gains<INTER, VEC>(p, key ? p.wk : p.wq, w);
+    uint8_t* const src = key ? p.k.ptr : p.q.ptr;
+    uint8_t* const dst = key ? p.ko.ptr : p.qo.ptr;
+    const int64_t ib = key ? p.k.sb : p.q.sb, is = key ? p.k.ss : p.q.ss, i0 = h * (key ? p.k.sh : p.q.sh);
+    const int64_t ob = key ? p.ko.sb : p.qo.sb, os = key ? p.ko.ss : p.qo.ss, o0 = h * (key ? p.ko.sh : p.qo.sh);
+    for (int64_t first = ((int64_t)blockIdx.x * kWaves + wave) * tokens; first < p.tokens; first += p.units * tokens) {
+        bool live;
+        int64_t b, s, t;
+        const int token = token_of(p, first, group / p.slots, live, b, s);
+        const bool used = token_position(p, token, s, t);
+        Pairs x = load_pairs<ST, INTER, VEC>(src, b * ib + s * is + i0, w);
+        const Pairs turn = load_turn<VEC>(p, t, w, used);
+        forward_head<VEC, L>(p, w, g, turn, used, x);
+        if (live && head) store_pairs<ST, INTER, VEC>(dst, b * ob + s * os + o0, w, x);
+    }
+}
+
+template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bounds__(kThreads) qk_backward_few(const QkArgs p)
+{
+    constexpr int G = 64 / L;
+    __shared__ float sums[kWaves * G][L * 16 + 1];
+    const int lane = threadIdx.x & 63, group = lane / L, slot = group & (p.slots - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tokens = G / p.slots;
+    const Place w = place<INTER>(threadIdx.x & (L - 1), p.dim, p.rot);
+    const bool head = slot < p.hq + p.hk, key = head && slot >= p.hq;
+    const int h = !head ? 0 : key ? slot - p.hq : slot;
+    const Pairs g = load_gains<INTER, VEC>(p, key ? p.wk : p.wq, w);
+    uint8_t* const src = key ? p.k.ptr : p.q.ptr;
+    uint8_t* const ups = key ? p.gk.ptr : p.gq.ptr;
+    uint8_t* const dst = key ? p.ko.ptr : p.qo.ptr;
+    const int64_t ib = key ? p.k.sb : p.q.sb, is = key ? p.k.ss : p.q.ss, i0 = h * (key ? p.k.sh : p.q.sh);
+    const int64_t gb = key ? p.gk.sb : p.gq.sb, gs = key ? p.gk.ss : p.gq.ss, g0 = h * (key ? p.gk.sh : p.gq.sh);
+    const int64_t ob = key ? p.ko.sb : p.qo.sb, os = key ? p.ko.ss : p.qo.ss, o0 = h * (key ? p.ko.sh : p.qo.sh);
+    Pairs d{};
+    for (int64_t first = ((int64_t)blockIdx.x * kWaves + wave) * tokens; first < p.tokens; first += p.units * tokens) {
+        bool live;
+        int64_t b, s, t;
+        const int token = token_of(p, first, group / p.slots, live, b, s);
+        const bool used = token_position(p, token, s, t) && live && head;
+        Pairs x = load_pairs<ST, INTER, VEC>(src, b * ib + s * is + i0, w);
+        Pairs y = load_pairs<ST, INTER, VEC>(ups, b * gb + s * gs + g0, w);
+        const Pairs turn = load_turn<VEC>(p, t, w, used);
+        backward_head<VEC, L>(p, w, g, turn, used, x, y, d);
+        if (live && head) store_pairs<ST, INTER, VEC>(dst, b * ob + s * os + o0, w, x);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (counts<VEC>(w, e)) {
+            sums[wave * G + group][2 * (w.pair + e)] = d.u[e];
+            sums[wave * G + group][2 * (w.pair + e) + 1] = d.v[e];
         }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * p.dim; i += kThreads) {
-        const int which = i >= p.dim, x = i - which * p.dim;  // element x of the pairs' order
+        const int which = i >= p.dim, x = i - which * p.dim;
         float v = 0.f;
-#pragma unroll
-        for (int wv = 0; wv < kWaves; ++wv) v += sums[wv][which][x];
-        const Place q = place<INTER>(x >> 1, p.dim, p.rot);
-        p.part[(int64_t)blockIdx.x * 2 * p.dim + which * p.dim + (x & 1 ? q.b : q.a)] = v;
+        for (int k = 0; k < kWaves * G; ++k) {
+            const int at = k & (p.slots - 1);
+            if (at < p.hq + p.hk && (at >= p.hq) == (which != 0)) v += sums[k][x];
+        }
+        put_gain<INTER>(p, which, x, v);
     }
 }
 
@@ -340,13 +477,28 @@ int64_t grad_blocks(int64_t tokens) { return std::max<int64_t>(1, std::min<int64
 
 template <bool BWD, GemmStore ST, bool INTER, bool VEC, int L> int launch_l(QkArgs p, hipStream_t stream)
 {
+    constexpr int G = 64 / L;
+    if constexpr (L <= 16) {
+        if (p.hq + p.hk <= G) {
+            p.slots = 1;
+            while (p.slots < p.hq + p.hk) p.slots *= 2;
+            // the forward pass leaves nothing behind: a wave for each of its tokens
+            const int64_t blocks = BWD ? grad_blocks(p.tokens) : std::min<int64_t>(ceil_div(p.tokens * p.slots, G * kWaves), 4096);
+            p.units = blocks * kWaves;
+            if constexpr (BWD)
+                hipLaunchKernelGGL((qk_backward_few<ST, INTER, VEC, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
+            else
+                hipLaunchKernelGGL((qk_forward_few<ST, INTER, VEC, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
+            return launch_status();
+        }
+    }
     if constexpr (BWD) {
         const int64_t blocks = grad_blocks(p.tokens);
         p.units = blocks * kWaves;
-        hipLaunchKernelGGL((qk_backward<ST, INTER, VEC, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
+        hipLaunchKernelGGL((qk_backward<ST, INTER, VEC, L>), dim3((unsigned)blocks, 2), dim3(kThreads), 0, stream, p);
     } else {
         // few tokens: a token's heads are shared out over several waves
-        const int64_t groups = ceil_div(std::max(p.hq, p.hk), 64 / L);
+        const int64_t groups = ceil_div(std::max(p.hq, p.hk), G);
         p.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(groups, 4096 / std::max<int64_t>(1, p.tokens)));
         p.units = p.tokens * p.parts;
         const int64_t blocks = ceil_div(p.units, kWaves);
@@ -358,16 +510,20 @@ template <bool BWD, GemmStore ST, bool INTER, bool VEC, int L> int launch_l(QkAr
 
 template <bool BWD, GemmStore ST, bool INTER, bool VEC> int launch_vec(const QkArgs& p, hipStream_t stream)
 {
-    if (p.dim <= 64) return launch_l<BWD, ST, INTER, VEC, 4>(p, stream);
-    if (p.dim <= 128) return launch_l<BWD, ST, INTER, VEC, 8>(p, stream);
-    if (p.dim <= 256) return launch_l<BWD, ST, INTER, VEC, 16>(p, stream);
-    return launch_l<BWD, ST, INTER, VEC, 32>(p, stream);
+    // lanes to a head: one for each run of eight pairs
+    const int lanes = (int)(ceil_div(p.rot / 2, 8) + ceil_div((p.dim - p.rot) / 2, 8));
+    if (lanes <= 4) return launch_l<BWD, ST, INTER, VEC, 4>(p, stream);
+    if (lanes <= 8) return launch_l<BWD, ST, INTER, VEC, 8>(p, stream);
+    if (lanes <= 16) return launch_l<BWD, ST, INTER, VEC, 16>(p, stream);
+    if (lanes <= 32) return launch_l<BWD, ST, INTER, VEC, 32>(p, stream);
+    if constexpr (!VEC) return launch_l<BWD, ST, INTER, VEC, 64>(p, stream);
+    return HIMUON_ERR_UNSUPPORTED;
 }
 
 template <bool BWD, GemmStore ST> int launch_st(const QkArgs& p, bool inter, hipStream_t stream)
 {
-    // whole groups of eight pairs in every lane, on one side of the rotated part
-    const bool vec = p.dim % 16 == 0 && (inter || p.rot % 16 == 0);
+    // whole runs, none of which repeats pairs (VEC)
+    const bool vec = p.dim % 16 == 0 && p.rot % 16 == 0;
     if (inter) return vec ? launch_vec<BWD, ST, true, true>(p, stream) : launch_vec<BWD, ST, true, false>(p, stream);
     return vec ? launch_vec<BWD, ST, false, true>(p, stream) : launch_vec<BWD, ST, false, false>(p, stream);
 }

@@ -223,6 +223,17 @@ def _heads_like(t, what, shape, like):
     return packed
 
 
+def _outputs(out, q, k, sq, sk):
+    """The two output tensors (fresh ones if ``out`` is None), and both as himuon_heads_t."""
+    if out is not None:
+        oq, ok = out
+        return oq, ok, _heads_like(oq, "out", sq, q), _heads_like(ok, "out", sk, k)
+    oq, ok = q.new_empty(sq), k.new_empty(sk)
+    seq, hq, hk, dim = sq[-3], sq[-2], sk[-2], sq[-1]
+    return (oq, ok, _HEADS.pack(oq.data_ptr(), seq * hq * dim, hq * dim, dim),
+            _HEADS.pack(ok.data_ptr(), seq * hk * dim, hk * dim, dim))
+
+
 def _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved):
     """(shape of q, of k, himuon_qk_t, and q and k as himuon_heads_t), checked."""
     torch = _torch()
@@ -267,9 +278,8 @@ def qk_norm_rope(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, inter
     dev = q.device
     if dev.index != _device():
         return _on(dev, qk_norm_rope, q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, out, stream)
-    oq, ok = out if out is not None else (q.new_empty(sq), q.new_empty(sk))
-    _done(lib().himuon_qk_norm_rope(args, hq, hk, _heads_like(oq, "out", sq, q), _heads_like(ok, "out", sk, k),
-                                    _stream_of(stream, dev.index)), "himuon_qk_norm_rope")
+    oq, ok, ho, hp = _outputs(out, q, k, sq, sk)
+    _done(lib().himuon_qk_norm_rope(args, hq, hk, ho, hp, _stream_of(stream, dev.index)), "himuon_qk_norm_rope")
     if stream is not None and out is None:
         _keep_alive((oq, ok), stream, dev)
     return oq, ok
@@ -290,10 +300,9 @@ def qk_norm_rope_grad(g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions=None, 
     batch, seq = (sq[0], sq[1]) if len(sq) == 4 else (1, sq[0])
     workspace = _workspace(L.himuon_qk_norm_rope_grad_workspace_size(batch, seq, sq[-1]), workspace, q,
                            "himuon_qk_norm_rope_grad")
-    oq, ok = out if out is not None else (q.new_empty(sq), q.new_empty(sk))
+    oq, ok, ho, hp = _outputs(out, q, k, sq, sk)
     dwq, dwk = q_gain.new_empty(sq[-1]), k_gain.new_empty(sq[-1])
-    _done(L.himuon_qk_norm_rope_grad(args, gq, gk, hq, hk, _heads_like(oq, "out", sq, q), _heads_like(ok, "out", sk, k),
-                                     dwq.data_ptr(), dwk.data_ptr(), workspace.data_ptr(),
+    _done(L.himuon_qk_norm_rope_grad(args, gq, gk, hq, hk, ho, hp, dwq.data_ptr(), dwk.data_ptr(), workspace.data_ptr(),
                                      workspace.numel() * workspace.element_size(), _stream_of(stream, dev.index)),
           "himuon_qk_norm_rope_grad")
     if stream is not None:
