@@ -239,6 +239,31 @@ def test_weight_gradient_infinities_and_nan_stay_in_their_row_or_column(dtype, T
     assert torch.equal(got[rows][:, cols], clean[rows][:, cols])
 
 
+def test_past_32_bits():
+    """Activations, codes and gradients of more than 2^31 elements."""
+    import torch
+    T, C = 66000, 33000
+    x = torch.empty(T, C, dtype=torch.bfloat16, device="cuda")
+    x[:64] = _rand((64, C), "bf16", 40)
+    for i in range(64, T, 6000):
+        x[i:i + 6000] = x[(i // 64) % 7]
+    x[T - 90:] = _rand((90, C), "bf16", 41)
+    codes, exps = hm.act_pack(x)
+    last = hm.act_pack(x[T - T % 32 - 64:].contiguous())
+    assert torch.equal(codes[-3:], last[0]) and torch.equal(exps[-3:], last[1])
+    back = hm.act_unpack(codes, exps, T)
+    assert torch.equal(back[T - 40:], hm.act_unpack(*last, T % 32 + 64)[-40:])
+    del back
+    # the gradient's last columns, and the input's, alone
+    small = _rand((T, 40), "bf16", 42, 1e-3)
+    packed = hm.act_pack(small)
+    wide = hm.weight_grad(x, *packed, dtype=torch.float32)  # x as the gradient
+    _check_wgrad(wide[-33:], x[:, -33:], *packed, "f32")
+    tall = hm.weight_grad(small, codes, exps, dtype=torch.float32)
+    part = (codes[:, -50:].contiguous(), exps[:, -50:].contiguous())
+    _check_wgrad(tall[:, -50:], small, *part, "f32")
+
+
 def test_weight_gradient_extreme_values():
     """fp32 gradients near the ends of the range: no term overflows on the way."""
     import torch

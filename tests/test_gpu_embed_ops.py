@@ -102,6 +102,27 @@ def test_lookup_past_32_bits():
     assert torch.equal(hm.embed(pick, table), table[pick])
 
 
+def test_gradient_past_32_bits():
+    """Rows of a table whose elements lie beyond 2^31, into rows with a stride."""
+    import torch
+    rows, width = 270000, 8192
+    out = torch.full((rows, width + 8), 3.0, dtype=torch.bfloat16, device="cuda")
+    tokens = torch.tensor([0, rows - 1, 262144, rows - 1, 262143], device="cuda")
+    grad = _rand((5, width), "bf16", 30)
+    hm.embed_grad(tokens, grad, rows, out=out[:, :width])
+    assert torch.equal(out[262144, :width], grad[2]) and torch.equal(out[262143, :width], grad[4]) and torch.equal(out[0, :width], grad[0])
+    assert torch.equal(out[rows - 1, :width], (grad[1].float() + grad[3].float()).bfloat16())
+    assert bool((out[:, width:] == 3).all())
+    assert int((out[:, :width] != 0).any(1).sum()) == 4
+
+
+def test_gradient_of_many_tokens():
+    """Hundreds of tiles in the sort, thousands of chunks in the sums."""
+    n, rows, width = 300001, 40000, 24
+    tokens, grad = _ids(n, rows, 31), _rand((n, width), "bf16", 32)
+    _check_grad(hm.embed_grad(tokens, grad, rows, dtype=_dt("f32")), tokens, grad, rows, 1.0, "f32")
+
+
 @pytest.mark.parametrize("n,rows,width", [(1, 1, 1), (2, 2, 8), (100, 37, 3), (1500, 5003, 103), (1025, 1023, 64), (1024, 1024, 512),
                                           (9000, 70000, 520), (3000, (1 << 20) + 3, 17), (20000, 300, 1032)])
 @pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
