@@ -520,8 +520,9 @@ int himuon_embed(int64_t n_tokens, const void* tokens, int index, int64_t n_rows
  * in an order that depends on the tokens alone. Tokens outside [0, n_rows) give nothing.
  * grad        n_tokens x dim, storage `dtype`.
  * dtable      n_rows x dim, storage `out_dtype`; must not overlap grad.
- * workspace   himuon_embed_grad_workspace_size(n_tokens, n_rows, dim) bytes (0:
- *             invalid sizes), 16-byte aligned.
+ * workspace   himuon_embed_grad_workspace_size(n_tokens, n_rows, dim) bytes,
+ *             16-byte aligned (0: none is needed, as for a short batch, or the
+ *             sizes are invalid; NULL will do).
  */
 size_t himuon_embed_grad_workspace_size(int64_t n_tokens, int64_t n_rows, int64_t dim);
 
@@ -623,8 +624,9 @@ int himuon_act_unpack(int64_t n_tokens, int64_t cols, const void* codes, const v
  * grad       n_tokens x out, storage `dtype`, ld_grad >= out.
  * dweight    out x cols, storage `out_dtype`, ld_dweight >= cols; may be what
  *            himuon_step takes as a gradient.
- * workspace  himuon_weight_grad_workspace_size(...) bytes (0: invalid sizes),
- *            256-byte aligned. The size depends on grad's type, leading dimension
+ * workspace  himuon_weight_grad_workspace_size(...) bytes, 256-byte aligned (0:
+ *            none is needed, as for many small results, or the sizes are
+ *            invalid; NULL will do). The size depends on grad's type, leading dimension
  *            and address (16-byte aligned rows of bf16 are read in place).
  */
 size_t himuon_weight_grad_workspace_size(int64_t n_tokens, int64_t out, int64_t cols, const void* grad, int64_t ld_grad,

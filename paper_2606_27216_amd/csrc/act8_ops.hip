@@ -807,10 +807,11 @@ WgradPlan plan_wgrad(int64_t tokens, int64_t out, int64_t cols, const void* grad
     g.part_pitch = g.exp_pitch;
     size_t at = g.stage ? round_up((size_t)slices * kGroup * (size_t)g.pitch * 2, 256) : 0;
     g.exps_at = at;
+    // (the exponents of whole rows of 4 bytes at an aligned address are read in place)
     if (g.tile != Tile::DIRECT) at += round_up((size_t)g.groups * (size_t)g.exp_pitch, 256);
     g.part_at = at;
     if (g.splits > 1) at += round_up((size_t)g.splits * (size_t)out * (size_t)g.part_pitch * 4, 256);
-    g.total = std::max<size_t>(at, 256);
+    g.total = at;
     return g;
 }
 
@@ -924,7 +925,7 @@ extern "C" int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, c
     if (!small_product(n_tokens, ld_grad) || !small_product(out, ld_dweight)) return HIMUON_ERR_INVALID_ARG;
     if (!dweight || (n_tokens && (!grad || !codes || !exponents || ((uintptr_t)codes & 15)))) return HIMUON_ERR_INVALID_ARG;
     WgradPlan g = plan_wgrad(n_tokens, out, cols, grad, ld_grad, dtype);
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < g.total) return HIMUON_ERR_WORKSPACE;
+    if (g.total > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < g.total)) return HIMUON_ERR_WORKSPACE;
     if (n_tokens == 0 && accumulate) return HIMUON_OK;
     StreamDevice on(stream);
     if (on.status != HIMUON_OK) return on.status;

@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kThreads) sort_scatter(const SortArgs p)
 // with a smaller key and earlier ones with the same. A block ranks 64 entries, its waves
 // share out what these are compared with.
 constexpr int kRankThreads = 1024;
-constexpr int kRankMost = 4096;
+constexpr int kRankMost = 6144;
 
 __global__ void __launch_bounds__(kRankThreads) sort_rank(const SortArgs p)
 {
@@ -486,6 +486,137 @@ template <GemmStore OT, int S, int kJoinWaves> __global__ void __launch_bounds__
     }
 }
 
+// ------------------------------------------------------------- short batches
+
+// A batch of few tokens in one launch, without a sort. Block i has token i: its waves
+// compare a part of the batch each with it. Unless it occurs earlier too, they sum the
+// rows where it occurs, in order, and the parts are added up in order. The blocks behind
+// these set rows to zero that no token names, which each finds out for its own.
+constexpr int kFewThreads = 512, kFewWaves = kFewThreads / kWave;
+constexpr int kFewMost = 1024;
+constexpr int kFewParts = kFewMost / kFewThreads;  // tokens of a lane
+
+struct FewArgs {
+    SortArgs sort;                  // tokens, rows, n, wide, first
+    SumArgs sum;
+    uint8_t* out;
+    int64_t row_bytes, ld_bytes;
+    int32_t fill_rows;              // rows of a block
+    int32_t share;                  // tokens of a wave
+};
+
+template <GemmStore ST, GemmStore OT> __global__ void __launch_bounds__(kFewThreads) sum_few(const FewArgs f)
+{
+    typedef uint32_t Chunk __attribute__((ext_vector_type(4)));
+    typedef Chunk ChunkAny __attribute__((aligned(2)));
+    constexpr int kFillMost = 4096;
+    __shared__ float part[kFewWaves - 1][kWave][8 + 1];
+    __shared__ int seen[kFewWaves];
+    __shared__ uint8_t named[kFillMost];
+    const SumArgs& p = f.sum;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int)blockIdx.x >= p.n) {
+        if (blockIdx.y > 0) return;
+        const int64_t r0 = (int64_t)((int)blockIdx.x - p.n) * f.fill_rows;
+        const int rows = (int)min((int64_t)f.fill_rows, p.rows - r0);
+        for (int r = threadIdx.x; r < rows; r += kFewThreads) named[r] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < p.n; i += kFewThreads) {
+            const int64_t r = (int64_t)sort_key(f.sort, i) - r0;
+            if (r >= 0 && r < rows) named[r] = 1;
+        }
+        __syncthreads();
+        const uint32_t per = (uint32_t)((f.row_bytes + 15) / 16);
+        // (a launch's blocks have at most 4096 rows of at most 32 KB, or one row)
+        for (uint32_t x = threadIdx.x; x < per * (uint32_t)rows; x += kFewThreads) {
+            const uint32_t r = x / per, c = (x - r * per) * 16;
+            if (named[r]) continue;
+            uint8_t* const at = f.out + (r0 + r) * f.ld_bytes + c;
+            const int64_t left = f.row_bytes - c;
+            if (left >= 16) *reinterpret_cast<ChunkAny*>(at) = Chunk{};
+            else
+                for (int64_t i = 0; i < left; i += 2) *reinterpret_cast<uint16_t*>(at + i) = 0;
+        }
+        return;
+    }
+    const int mine = blockIdx.x;
+    const uint32_t key = sort_key(f.sort, mine);
+    if (key >= (uint32_t)p.rows) return;
+    uint64_t same[kFewParts];
+    int first = p.n;  // of this wave's tokens, the first one that is the same
+#pragma unroll
+    for (int g = kFewParts - 1; g >= 0; --g) {
+        const int x = g * kWave + lane, i = wave * f.share + x;
+        const bool on = x < f.share && i < p.n;
+        same[g] = __ballot(on && sort_key(f.sort, on ? i : 0) == key);
+        if (same[g]) first = wave * f.share + g * kWave + __ffsll((unsigned long long)same[g]) - 1;
+    }
+    if (lane == 0) seen[wave] = first;
+    __syncthreads();
+    int earliest = p.n;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) earliest = min(earliest, seen[w]);
+    if (earliest < mine) return;
+    const int slabs = (p.dim + kSlab - 1) / kSlab;
+    for (int slab = blockIdx.y; slab < slabs; slab += gridDim.y) {
+        const int lane_col = slab * kSlab + lane * 8;
+        const bool col = lane_col < p.dim;  // (lanes past the last column read the first ones and store nothing)
+        const int c = col ? lane_col : 0, nc = min(8, p.dim - c);
+        float acc[8] = {};
+#pragma unroll
+        for (int g = 0; g < kFewParts; ++g) {
+            uint64_t m = same[g];
+            const int base = wave * f.share + g * kWave;
+            constexpr int B = 8;
+            while (m) {
+                Raw8<ST> v[B];
+                int n = 0, at = 0;
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    if (m) {
+                        at = base + __ffsll((unsigned long long)m) - 1;
+                        m &= m - 1;
+                        ++n;
+                    }
+                    v[b] = get_raw8<ST>(p.grad, (int64_t)at * p.ld_grad + c, nc);
+                }
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[e] += b < n ? raw_value<ST>(v[b], e) : 0.f;
+                }
+            }
+        }
+        __syncthreads();
+        if (wave > 0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part[wave - 1][lane][e] = acc[e];
+        }
+        __syncthreads();
+        if (wave == 0 && col) {
+#pragma unroll
+            for (int w = 0; w < kFewWaves - 1; ++w) {
+                if (seen[w + 1] < p.n) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[e] += part[w][lane][e];
+                }
+            }
+            put_row<OT>(p, key, c, acc);
+        }
+    }
+}
+
+template <GemmStore ST, GemmStore OT> int launch_few(const FewArgs& f, hipStream_t stream)
+{
+    const int64_t fill = f.sum.accumulate ? 0 : ceil_div(f.sum.rows, f.fill_rows);
+    if (f.sum.n + fill > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    // columns shared out over blocks while these are few: one token 100 times, 4096 columns
+    const int64_t parts = std::min<int64_t>(f.sum.slabs, std::max<int64_t>(2, 2048 / f.sum.n));
+    hipLaunchKernelGGL((sum_few<ST, OT>), dim3((unsigned)(f.sum.n + fill), (unsigned)parts), dim3(kFewThreads), 0, stream, f);
+    return launch_status();
+}
+
 template <GemmStore ST, GemmStore OT, int S> int launch_sums(SumArgs p, hipStream_t stream)
 {
     p.chunks = (int)ceil_div(p.n, S);
@@ -525,6 +656,7 @@ int key_bits(int64_t rows)
 struct GradPlan {
     size_t key[2], pos[2], hist, part, total;
     int digits, bits, tiles, chunk;
+    bool few;
 };
 
 GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
@@ -533,8 +665,13 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
     const int kb = key_bits(rows);
     g.digits = (kb + 9) / 10;
     g.bits = std::max(2, (kb + g.digits - 1) / g.digits);  // (bins in groups of four)
+    // One launch against the sort's three: 100 tokens into 32000 x 256 10.0 us and 16.9, 600 into
+    // 5003 x 1000 10.1 and 17.2; but 600 into 32000 x 4096 49 and 44, 1500 of one token 35 and 22.
+    g.few = n > 0 && n <= (dim <= 2 * kSlab ? kFewMost : kFewMost / 2);
     g.tiles = (int)ceil_div(n, kTile);
     g.chunk = chunk_size(n);
+    g.total = 0;
+    if (g.few || n == 0) return g;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t o = at;
@@ -547,7 +684,7 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
     }
     g.hist = take(((size_t)g.tiles << g.bits) * 4);
     g.part = take((size_t)ceil_div(n, g.chunk) * 2 * (size_t)dim * 4);
-    g.total = std::max<size_t>(at, 256);
+    g.total = at;
     return g;
 }
 
@@ -609,13 +746,24 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
     if (n_tokens && (!tokens || !grad || grad == dtable)) return HIMUON_ERR_INVALID_ARG;
     if (!small_product(n_rows, ld_dtable) || !small_product(n_tokens, ld_grad)) return HIMUON_ERR_INVALID_ARG;
     const GradPlan g = plan_grad(n_tokens, n_rows, dim);
-    if (!workspace || workspace_bytes < g.total || ((uintptr_t)workspace & 15)) return HIMUON_ERR_WORKSPACE;
+    if (g.total > 0 && (!workspace || workspace_bytes < g.total || ((uintptr_t)workspace & 15))) return HIMUON_ERR_WORKSPACE;
     if (n_tokens == 0 && accumulate) return HIMUON_OK;
     StreamDevice on(stream);
     if (on.status != HIMUON_OK) return on.status;
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
 
+    SumArgs p{};
+    p.grad = grad;
+    p.out = dtable;
+    p.rows = n_rows;
+    p.ld_grad = ld_grad;
+    p.ld_out = ld_dtable;
+    p.n = (int32_t)n_tokens;
+    p.dim = (int32_t)dim;
+    p.slabs = (int32_t)ceil_div(dim, kSlab);
+    p.accumulate = accumulate != 0;
+    p.scale = scale;
     SortArgs s{};
     s.tokens = tokens;
     s.hist = reinterpret_cast<uint32_t*>(ws + g.hist);
@@ -624,6 +772,22 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
     s.wide = index == HIMUON_I64;
     s.tiles = g.tiles;
     s.bits = g.bits;
+    if (g.few) {
+        FewArgs f{};
+        s.first = 1;
+        f.sort = s;
+        f.sum = p;
+        f.out = static_cast<uint8_t*>(dtable);
+        f.row_bytes = dim * dtype_size(out_dtype);
+        f.ld_bytes = ld_dtable * dtype_size(out_dtype);
+        f.fill_rows = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4096, 65536 / f.row_bytes));
+        f.share = (int32_t)ceil_div(n_tokens, kFewWaves);
+        if (dtype == HIMUON_BF16)
+            return out_dtype == HIMUON_BF16 ? launch_few<GemmStore::BF16, GemmStore::BF16>(f, hs)
+                                            : launch_few<GemmStore::BF16, GemmStore::F32>(f, hs);
+        return out_dtype == HIMUON_BF16 ? launch_few<GemmStore::F32, GemmStore::BF16>(f, hs)
+                                        : launch_few<GemmStore::F32, GemmStore::F32>(f, hs);
+    }
     s.fill.out = static_cast<uint8_t*>(dtable);
     s.fill.row_bytes = dim * dtype_size(out_dtype);
     s.fill.ld_bytes = ld_dtable * dtype_size(out_dtype);
@@ -670,20 +834,9 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
             if (st != HIMUON_OK) return st;
         }
     }
-    SumArgs p{};
     p.key = reinterpret_cast<const uint32_t*>(ws + g.key[from]);
     p.pos = reinterpret_cast<const uint32_t*>(ws + g.pos[from]);
-    p.grad = grad;
-    p.out = dtable;
     p.part = reinterpret_cast<float*>(ws + g.part);
-    p.rows = n_rows;
-    p.ld_grad = ld_grad;
-    p.ld_out = ld_dtable;
-    p.n = (int32_t)n_tokens;
-    p.dim = (int32_t)dim;
-    p.slabs = (int32_t)ceil_div(dim, kSlab);
-    p.accumulate = accumulate != 0;
-    p.scale = scale;
     if (dtype == HIMUON_BF16)
         return out_dtype == HIMUON_BF16 ? launch_sums_t<GemmStore::BF16, GemmStore::BF16>(p, g.chunk, hs)
                                         : launch_sums_t<GemmStore::BF16, GemmStore::F32>(p, g.chunk, hs);

@@ -16,7 +16,7 @@ from __future__ import annotations
 import ctypes
 import struct
 
-from . import BF16, ERR_UNSUPPORTED, F32, OK, HimuonError, _dtype_code, _keep_alive, lib
+from . import BF16, F32, OK, HimuonError, _dtype_code, _keep_alive, lib
 
 I32, I64 = 0, 1              # himuon_index_t
 MAX_HEAD_DIM = 512           # HIMUON_MAX_HEAD_DIM
@@ -106,16 +106,19 @@ def _stream_of(stream, index):
     return (_raw_stream(index) if stream is None else stream.cuda_stream) or None
 
 
-def _workspace(need, given, like, what):
-    """``given``, or a fresh one of ``need`` bytes (0: the sizes are not served)."""
-    torch = _torch()
-    if need == 0:
-        raise HimuonError(ERR_UNSUPPORTED, what + "_workspace_size")
+def _workspace(need, given, like, fresh):
+    """(address, bytes) of ``given``, or of a fresh workspace of ``need`` bytes (none for 0:
+    the call needs none, or reports what is wrong with it)."""
     if given is None:
-        return torch.empty(need, dtype=torch.uint8, device=like.device)
+        if need == 0:
+            return None, 0
+        torch = _torch()
+        given = torch.empty(need, dtype=torch.uint8, device=like.device)
+        fresh.append(given)
+        return given.data_ptr(), need
     if given.device != like.device:
         raise ValueError("the workspace must be on the tensors' device")
-    return given
+    return given.data_ptr(), given.numel() * given.element_size()
 
 
 def _done(status, what):
@@ -181,8 +184,7 @@ def embed_grad(tokens, grad, num_rows, scale=1.0, out=None, dtype=None, accumula
         return _on(dev, embed_grad, tokens, grad, rows, scale, out, dtype, accumulate, workspace, stream)
     code, index = _type_code(grad), _index_code(tokens)
     L = lib()
-    workspace = _workspace(L.himuon_embed_grad_workspace_size(n, rows, width), workspace, grad, "himuon_embed_grad")
-    fresh.append(workspace)
+    ws, ws_bytes = _workspace(L.himuon_embed_grad_workspace_size(n, rows, width), workspace, grad, fresh)
     if out is None:
         out = torch.empty((rows, width), dtype=grad.dtype if dtype is None else dtype, device=dev)
         fresh.append(out)
@@ -191,8 +193,7 @@ def embed_grad(tokens, grad, num_rows, scale=1.0, out=None, dtype=None, accumula
     ld_out = _matrix(out, "out")[2]
     _same_device(dev, tokens, out)
     _done(L.himuon_embed_grad(n, tokens.data_ptr(), index, rows, width, grad.data_ptr(), ld, code, out.data_ptr(), ld_out,
-                              _type_code(out), scale, bool(accumulate), workspace.data_ptr(),
-                              workspace.numel() * workspace.element_size(), _stream_of(stream, dev.index)),
+                              _type_code(out), scale, bool(accumulate), ws, ws_bytes, _stream_of(stream, dev.index)),
           "himuon_embed_grad")
     if stream is not None:
         _keep_alive(fresh, stream, dev)
@@ -298,15 +299,15 @@ def qk_norm_rope_grad(g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions=None, 
     gq, gk = _heads_like(g_q, "g_q", sq, q), _heads_like(g_k, "g_k", sk, k)
     L = lib()
     batch, seq = (sq[0], sq[1]) if len(sq) == 4 else (1, sq[0])
-    workspace = _workspace(L.himuon_qk_norm_rope_grad_workspace_size(batch, seq, sq[-1]), workspace, q,
-                           "himuon_qk_norm_rope_grad")
+    fresh = []
+    ws, ws_bytes = _workspace(L.himuon_qk_norm_rope_grad_workspace_size(batch, seq, sq[-1]), workspace, q, fresh)
     oq, ok, ho, hp = _outputs(out, q, k, sq, sk)
     dwq, dwk = q_gain.new_empty(sq[-1]), k_gain.new_empty(sq[-1])
-    _done(L.himuon_qk_norm_rope_grad(args, gq, gk, hq, hk, ho, hp, dwq.data_ptr(), dwk.data_ptr(), workspace.data_ptr(),
-                                     workspace.numel() * workspace.element_size(), _stream_of(stream, dev.index)),
+    _done(L.himuon_qk_norm_rope_grad(args, gq, gk, hq, hk, ho, hp, dwq.data_ptr(), dwk.data_ptr(), ws, ws_bytes,
+                                     _stream_of(stream, dev.index)),
           "himuon_qk_norm_rope_grad")
     if stream is not None:
-        _keep_alive((oq, ok, dwq, dwk, workspace), stream, dev)
+        _keep_alive((oq, ok, dwq, dwk, *fresh), stream, dev)
     return oq, ok, dwq, dwk
 
 
@@ -386,9 +387,8 @@ def weight_grad(grad, codes, exps, out=None, dtype=None, accumulate=False, works
     if dev.index != _device():
         return _on(dev, weight_grad, grad, codes, exps, out, dtype, accumulate, workspace, stream)
     L = lib()
-    workspace = _workspace(L.himuon_weight_grad_workspace_size(n, rows, cols, at, ld, code), workspace, grad,
-                           "himuon_weight_grad")
-    fresh = [workspace]
+    fresh = []
+    ws, ws_bytes = _workspace(L.himuon_weight_grad_workspace_size(n, rows, cols, at, ld, code), workspace, grad, fresh)
     if out is None:
         out = torch.empty((rows, cols), dtype=grad.dtype if dtype is None else dtype, device=dev)
         fresh.append(out)
@@ -397,8 +397,7 @@ def weight_grad(grad, codes, exps, out=None, dtype=None, accumulate=False, works
     ld_out = _matrix(out, "out")[2]
     _same_device(dev, codes, out)
     _done(L.himuon_weight_grad(n, rows, cols, at, ld, code, codes.data_ptr(), exps.data_ptr(), out.data_ptr(), ld_out,
-                               _type_code(out), bool(accumulate), workspace.data_ptr(),
-                               workspace.numel() * workspace.element_size(), _stream_of(stream, dev.index)),
+                               _type_code(out), bool(accumulate), ws, ws_bytes, _stream_of(stream, dev.index)),
           "himuon_weight_grad")
     if stream is not None:
         _keep_alive(fresh, stream, dev)

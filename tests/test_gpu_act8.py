@@ -369,5 +369,6 @@ def test_refusals():
     with pytest.raises(TypeError):
         hm.weight_grad(g.half(), codes, exps)
     with pytest.raises(hm.HimuonError) as e:
-        hm.weight_grad(g, codes, exps, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        hm.weight_grad(_rand((300, 1501), "bf16", 22), *hm.act_pack(_rand((300, 2100), "bf16", 22)),
+                       workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.status == hm.ERR_WORKSPACE

@@ -66,23 +66,24 @@ def test_sizes_beyond_the_kernels(name, good, bad):
 
 def test_workspaces():
     L = hm.lib()
-    need = L.himuon_embed_grad_workspace_size(4, 10, 8)
+    need = L.himuon_embed_grad_workspace_size(100000, 10, 8)
     assert need > 0 and L.himuon_embed_grad_workspace_size(-1, 10, 8) == 0 and L.himuon_embed_grad_workspace_size(4, 0, 8) == 0
-    assert _call("embed_grad", GRAD, ws=None) == hm.ERR_WORKSPACE and _call("embed_grad", GRAD, ws=P + 8) == hm.ERR_WORKSPACE
-    assert _call("embed_grad", GRAD, ws_bytes=need - 1) == hm.ERR_WORKSPACE
+    assert L.himuon_embed_grad_workspace_size(4, 10, 8) == 0  # a short batch needs none
+    for bad in (dict(ws=None), dict(ws=P + 8), dict(ws_bytes=need - 1)):
+        assert _call("embed_grad", GRAD, n=100000, **bad) == hm.ERR_WORKSPACE
     # keys and positions twice, and two partial rows a chunk of 32 tokens
     assert L.himuon_embed_grad_workspace_size(65536, 32000, 4096) < 65536 * 16 + 65536 // 32 * 2 * 4096 * 4 + (1 << 20)
     # the gradient is read in place if it can be: an odd address or fp32 needs room for its terms
     size = L.himuon_weight_grad_workspace_size
     T, O, C = 8192, 11008, 4096
     small = size(T, O, C, P, O, hm.BF16)
-    assert 0 < small < 8 << 20
+    assert 0 < small < 8 << 20 and size(64, 16, 8, P, 16, hm.BF16) == 0
     assert size(T, O, C, P + 2, O, hm.BF16) >= T * O * 2 and size(T, O, C, P, O + 1, hm.BF16) >= T * O * 2
     assert size(T, O, C, P, O, hm.F32) >= 3 * T * O * 2
     assert size(T, O, C, P, O - 1, hm.BF16) == 0 and size(T, 0, C, P, O, hm.BF16) == 0 and size(T, O, C, P, O, 7) == 0
-    need = size(64, 16, 8, P, 16, hm.BF16)
-    assert _call("weight_grad", WGRAD, ws=None) == hm.ERR_WORKSPACE and _call("weight_grad", WGRAD, ws=P + 16) == hm.ERR_WORKSPACE
-    assert _call("weight_grad", WGRAD, ws_bytes=need - 1) == hm.ERR_WORKSPACE
+    need = size(9000, 700, 1000, P, 700, hm.BF16)
+    for bad in (dict(ws=None), dict(ws=P + 16), dict(ws_bytes=need - 1)):
+        assert _call("weight_grad", WGRAD, n=9000, out=700, cols=1000, ld_grad=700, ld_dw=1000, **bad) == hm.ERR_WORKSPACE
     size = L.himuon_qk_norm_rope_grad_workspace_size
     assert size(2, 3, 64) > 0 and size(2, 3, 0) == 0 and size(2, 3, 514) == 0 and size(-1, 3, 64) == 0
     assert size(1 << 20, 1 << 20, 64) == 0
