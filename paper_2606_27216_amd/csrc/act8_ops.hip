@@ -769,9 +769,13 @@ struct WgradPlan {
 //   - B128_PAIR (two groups of waves to a tile) while there are no more tiles than CUs:
 //     512 x 2048^2 10.5 / 24.5 (B128, split in two, 24.9 / 34.6); 512 tiles of 4096 x 2048
 //     at 1024 tokens 25.0 / 63.5 (B128 23.0 / 59.7).
-//   - B256 where its tiles fill the chip and are long enough to hide their ends: 4096^2 at
-//     512, 1024, 8192 tokens 27.2, 39.3, 202 (B128 25.0, 39.3, 244); 2048 x 4096, split in
-//     two, at 4096 and 16384 tokens 75, 214 (B128 67, 249).
+//   - B256 or B128 by their rounds over the chip, in slices of a 256-tile (about 0.62 us): a
+//     round of 256-tiles takes its slices and 8 for its ends, each split 15 for the join; a
+//     CU works 128-tiles off at 0.32 a slice, three of them at a time. Measured, B256 and
+//     B128: 4096^2 (256 tiles) at 256, 1024, 8192 tokens 21.0 and 18.9, 39.3 and 39.3, 202 and
+//     244; 4928 x 3264 (260 tiles, two rounds) at 2681 tokens 141 and 88; 11008 x 4096 (688
+//     tiles) at 256, 2048 55 and 38, 171 and 171; 2048 x 4096 (128 tiles, two splits) at 4096,
+//     16384 75 and 67, 214 and 249.
 WgradPlan plan_wgrad(int64_t tokens, int64_t out, int64_t cols, const void* grad, int64_t ld, int dtype)
 {
     WgradPlan g;
@@ -789,15 +793,16 @@ WgradPlan plan_wgrad(int64_t tokens, int64_t out, int64_t cols, const void* grad
     if (t64 <= 512 && ceil_div(t64, 256) * g.groups <= 128 * direct && ld < (INT64_C(1) << 24)) {
         g.tile = Tile::DIRECT;
         splits = direct;
-    } else if (t256 > 128 ? slices >= 32 : t256 == 128 && slices >= 256) {
-        g.tile = Tile::B256;
-        splits = split(256, t256, slices / 8);
     } else if (t128 <= 256) {
         g.tile = Tile::B128_PAIR;
         splits = split(256, t128, slices / 16);
     } else {
-        g.tile = Tile::B128;
-        splits = split(512, t128, slices / 8);
+        splits = split(256, t256, slices / 8);
+        const double by256 = (double)ceil_div(t256 * splits, 256) * ((double)slices / (double)splits + 8) + 4 +
+                             (splits > 1 ? 15. * (double)splits : 0.);
+        const double by128 = 0.32 * (double)ceil_div(t128, 256) * (double)slices + 8;
+        g.tile = by256 <= by128 ? Tile::B256 : Tile::B128;
+        if (g.tile == Tile::B128) splits = 1;
     }
     g.splits = (int)splits;
     g.stage = g.tile != Tile::DIRECT &&
