@@ -106,6 +106,13 @@ def _stream_of(stream, index):
     return (_raw_stream(index) if stream is None else stream.cuda_stream) or None
 
 
+def _new(like, shape, dtype):
+    """A fresh tensor on ``like``'s device, of its type unless another one is asked for."""
+    if dtype is None or dtype == like.dtype:
+        return like.new_empty(shape)
+    return _torch().empty(shape, dtype=dtype, device=like.device)
+
+
 def _workspace(need, given, like, fresh):
     """(address, bytes) of ``given``, or of a fresh workspace of ``need`` bytes (none for 0:
     the call needs none, or reports what is wrong with it)."""
@@ -166,7 +173,7 @@ def embed_grad(tokens, grad, num_rows, scale=1.0, out=None, dtype=None, accumula
     (``tokens.shape + (width,)`` or 2-D with strided rows); the result is
     ``num_rows`` x width in ``dtype`` (default: ``grad``'s), or is added to ``out``
     with ``accumulate``."""
-    torch = _torch()
+    _torch()
     if not tokens.is_cuda or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous CUDA tensor")
     n, fresh = tokens.numel(), []
@@ -186,7 +193,7 @@ def embed_grad(tokens, grad, num_rows, scale=1.0, out=None, dtype=None, accumula
     L = lib()
     ws, ws_bytes = _workspace(L.himuon_embed_grad_workspace_size(n, rows, width), workspace, grad, fresh)
     if out is None:
-        out = torch.empty((rows, width), dtype=grad.dtype if dtype is None else dtype, device=dev)
+        out = _new(grad, (rows, width), dtype)
         fresh.append(out)
     elif tuple(out.shape) != (rows, width) or (dtype is not None and out.dtype != dtype):
         raise ValueError("out must be num_rows x width of the asked type")
@@ -204,7 +211,7 @@ def embed_grad(tokens, grad, num_rows, scale=1.0, out=None, dtype=None, accumula
 
 def _heads(t, what):
     """A [batch, seq, heads, dim] or [tokens, heads, dim] tensor: its shape, and himuon_heads_t."""
-    shape, s = t.shape, t.stride()
+    shape, s = tuple(t.shape), t.stride()
     n = len(shape)
     if n == 4:
         packed = _HEADS.pack(t.data_ptr(), s[0], s[1], s[2])
@@ -255,7 +262,7 @@ def _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved):
     index, at = I64, 0
     if positions is not None:
         index, at = _index_code(positions), positions.data_ptr()
-        if positions.shape != sq[:-2] or not positions.is_contiguous():
+        if tuple(positions.shape) != sq[:-2] or not positions.is_contiguous():
             raise ValueError("positions must be a contiguous tensor, one per token")
     batch, seq = (sq[0], sq[1]) if len(sq) == 4 else (1, sq[0])
     return sq, sk, _QK.pack(batch, seq, sq[-2], sk[-2], dim, 2 * table[1], bool(interleaved), _type_code(q), _type_code(q_gain),
@@ -291,6 +298,7 @@ def qk_norm_rope_grad(g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions=None, 
     """The backward pass of ``qk_norm_rope``: from the gradients ``g_q``, ``g_k`` of its
     outputs and its inputs, (dq, dk, dq_gain, dk_gain). ``out``: the tensors for dq
     and dk (``g_q`` and ``g_k`` themselves are allowed)."""
+    torch = _torch()
     sq, sk, args, hq, hk = _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
     dev = q.device
     if dev.index != _device():
@@ -302,7 +310,7 @@ def qk_norm_rope_grad(g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions=None, 
     fresh = []
     ws, ws_bytes = _workspace(L.himuon_qk_norm_rope_grad_workspace_size(batch, seq, sq[-1]), workspace, q, fresh)
     oq, ok, ho, hp = _outputs(out, q, k, sq, sk)
-    dwq, dwk = q_gain.new_empty(sq[-1]), k_gain.new_empty(sq[-1])
+    dwq, dwk = torch.empty_like(q_gain), torch.empty_like(k_gain)
     _done(L.himuon_qk_norm_rope_grad(args, gq, gk, hq, hk, ho, hp, dwq.data_ptr(), dwk.data_ptr(), ws, ws_bytes,
                                      _stream_of(stream, dev.index)),
           "himuon_qk_norm_rope_grad")
@@ -376,7 +384,7 @@ def weight_grad(grad, codes, exps, out=None, dtype=None, accumulate=False, works
     outputs [tokens, rows] and its inputs x held in 8 bits: rows x columns in
     ``dtype`` (default: ``grad``'s), or added to ``out`` with ``accumulate``. The result
     may be what ``step`` takes as a gradient."""
-    torch = _torch()
+    _torch()
     n, rows, ld = _matrix(grad, "grad")
     groups, cols = _packed(codes, exps)
     if -(-n // ACT_GROUP) != groups:
@@ -390,7 +398,7 @@ def weight_grad(grad, codes, exps, out=None, dtype=None, accumulate=False, works
     fresh = []
     ws, ws_bytes = _workspace(L.himuon_weight_grad_workspace_size(n, rows, cols, at, ld, code), workspace, grad, fresh)
     if out is None:
-        out = torch.empty((rows, cols), dtype=grad.dtype if dtype is None else dtype, device=dev)
+        out = _new(grad, (rows, cols), dtype)
         fresh.append(out)
     elif tuple(out.shape) != (rows, cols) or (dtype is not None and out.dtype != dtype):
         raise ValueError("out must be rows x columns of the asked type")
