@@ -204,9 +204,12 @@ __global__ void __launch_bounds__(kThreads) act_unpack(const uint8_t* codes, con
 // workspace as slices of bf16 rows, fp32 as three terms that follow each other (the
 // codes' slice is then read three times in a row, from cache).
 //
-// Bound by the matrix cores under the board's power cap: 8192 x 11008 x 4096 takes 557 us,
-// 1.33 PFLOP/s (a large library product reaches 1.25 to 1.40 on the card, the library's
-// bf16 product of this shape 0.9). The cores are busy for 1024 of about 1400 cycles of a slice.
+// Bound by the matrix cores under the board's power cap: 8192 x 11008 x 4096 takes 551 us,
+// 1.34 PFLOP/s (a large library product reaches 1.25 to 1.40 on the card, the library's
+// bf16 product of this shape 0.9). The cores are busy for 62% of the launch's cycles: 688
+// tiles of 256 are 2.7 rounds of the chip, and a slice takes about 1400 cycles for 1024 of
+// products. Eight waves of 128 x 64 to a tile against four of 128 x 128 (560) and of 256 x 64,
+// which widen each code once instead of twice (556); a ring of four or six slices 557.
 struct WgradArgs {
     const uint16_t* a;           // gradient, or its terms in the workspace
     const uint8_t *codes, *exps;
@@ -361,7 +364,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN * KG, MINW) wgrad_blocks(const 
     };
     // What goes out beside the products is spread over them, two or three instructions to each:
     // a product takes the matrix core 32 cycles, and a wave that issues ten others in one gap
-    // leaves it idle (8192 x 4096 x 4096: bunched 223 us, spread 214).
+    // leaves it idle (8192 x 4096 x 4096, four waves to a tile: bunched 223 us, spread 214).
     constexpr int PROD = RB * CB, HALF = PROD / 2;
     // the products of step 0 beside the operands of step 1
     auto first = [&](const uint8_t* ta) __attribute__((always_inline)) {
@@ -771,7 +774,7 @@ struct WgradPlan {
 //     at 1024 tokens 25.0 / 63.5 (B128 23.0 / 59.7).
 //   - B256 or B128 by their rounds over the chip, in slices of a 256-tile (about 0.62 us): a
 //     round of 256-tiles takes its slices and 8 for its ends, each split 15 for the join; a
-//     CU works 128-tiles off at 0.32 a slice, three of them at a time. Measured, B256 and
+//     CU works 128-tiles off at 0.345 a slice, three of them at a time. Measured, B256 and
 //     B128: 4096^2 (256 tiles) at 256, 1024, 8192 tokens 21.0 and 18.9, 39.3 and 39.3, 202 and
 //     244; 4928 x 3264 (260 tiles, two rounds) at 2681 tokens 141 and 88; 11008 x 4096 (688
 //     tiles) at 256, 2048 55 and 38, 171 and 171; 2048 x 4096 (128 tiles, two splits) at 4096,
@@ -800,7 +803,7 @@ WgradPlan plan_wgrad(int64_t tokens, int64_t out, int64_t cols, const void* grad
         splits = split(256, t256, slices / 8);
         const double by256 = (double)ceil_div(t256 * splits, 256) * ((double)slices / (double)splits + 8) + 4 +
                              (splits > 1 ? 15. * (double)splits : 0.);
-        const double by128 = 0.32 * (double)ceil_div(t128, 256) * (double)slices + 8;
+        const double by128 = 0.345 * (double)ceil_div(t128, 256) * (double)slices + 8;
         g.tile = by256 <= by128 ? Tile::B256 : Tile::B128;
         if (g.tile == Tile::B128) splits = 1;
     }
@@ -842,8 +845,8 @@ template <GemmStore OT, int BM, int BN, int WGM, int WGN, int KG, int NS, int MI
 
 template <GemmStore OT> int launch_wgrad(WgradArgs p, Tile tile, int dtype, hipStream_t stream)
 {
-    // (rings: 125 KB, 104 KB and three times 52 KB of a CU's 160 KB)
-    if (tile == Tile::B256) return launch_tiles<OT, 256, 256, 2, 2, 1, 5, 1>(p, stream);
+    // (rings: 130 KB, 104 KB and three times 52 KB of a CU's 160 KB)
+    if (tile == Tile::B256) return launch_tiles<OT, 256, 256, 2, 4, 1, 5, 2>(p, stream);
     if (tile == Tile::B128_PAIR) return launch_tiles<OT, 128, 128, 2, 2, 2, 4, 2>(p, stream);
     if (tile == Tile::B128) return launch_tiles<OT, 128, 128, 2, 2, 1, 4, 2>(p, stream);
     p.ti = (int32_t)ceil_div(p.rows, 64);
