@@ -619,7 +619,8 @@ int himuon_act_unpack(int64_t n_tokens, int64_t cols, const void* codes, const v
  *     dweight[o, i] (+)= sum over tokens t of grad[t, o] * x[t, i],
  * added to dweight if accumulate != 0. bf16 gradients are exact operands of the
  * matrix cores; fp32 ones are taken as three bf16 terms, which hold all 24 bits.
- * Products are exact and accumulated in fp32.
+ * Products are exact and accumulated in fp32. (Codes as himuon_act_pack writes
+ * them: the places behind the last token are zeros.)
  *
  * grad       n_tokens x out, storage `dtype`, ld_grad >= out.
  * dweight    out x cols, storage `out_dtype`, ld_dweight >= cols; may be what

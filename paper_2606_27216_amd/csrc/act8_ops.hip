@@ -206,9 +206,8 @@ __global__ void __launch_bounds__(kThreads) act_unpack(const uint8_t* codes, con
 //
 // Bound by the matrix cores under the board's power cap: 8192 x 11008 x 4096 takes 551 us,
 // 1.34 PFLOP/s (a large library product reaches 1.25 to 1.40 on the card, the library's
-// bf16 product of this shape 0.9). The cores are busy for 62% of the launch's cycles: 688
-// tiles of 256 are 2.7 rounds of the chip, and a slice takes about 1400 cycles for 1024 of
-// products. Eight waves of 128 x 64 to a tile against four of 128 x 128 (560) and of 256 x 64,
+// bf16 product of this shape 0.9). The cores are busy for 68% of the launch's cycles: 688
+// tiles of 256 are 2.7 rounds of the chip, and a slice takes longer than its 1024 cycles of products. Eight waves of 128 x 64 to a tile against four of 128 x 128 (560) and of 256 x 64,
 // which widen each code once instead of twice (556); a ring of four or six slices 557.
 struct WgradArgs {
     const uint16_t* a;           // gradient, or its terms in the workspace
@@ -533,6 +532,8 @@ __global__ void __launch_bounds__(64 * WGM * WGN * KG, MINW) wgrad_blocks(const 
 // the gradient are 16 loads of one element (32 lanes side by side), its 16 codes one load. No
 // LDS, no barrier and no second layout of the gradient on the way, whatever its type and
 // alignment; fp32 is cut into its three terms in registers. The waves' sums meet in LDS.
+// 1111 x 1003 x 777: fp32 13 us with the call, 12 of them on the chip; bound by the latency of
+// five groups in a row and by the cutting.
 constexpr int kDirectWaves = 8;
 
 template <GemmStore ST, GemmStore OT> __global__ void __launch_bounds__(64 * kDirectWaves, 2) wgrad_direct(const WgradArgs p)
@@ -615,14 +616,15 @@ template <GemmStore ST, GemmStore OT> __global__ void __launch_bounds__(64 * kDi
                     const uint32_t x = g.a[i][8 * s + 2 * e], y = g.a[i][8 * s + 2 * e + 1];
                     if constexpr (TERMS == 1) {
                         a[0][i][e] = x | y << 16;
-                    } else {  // (x == h: an infinity has no rest, NaN keeps one)
+                    } else {
                         float u = __uint_as_float(x), v = __uint_as_float(y);
 #pragma unroll
                         for (int k = 0; k < TERMS; ++k) {
                             const float hu = __uint_as_float(__float_as_uint(u) & 0xffff0000u), hv = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-                            a[k][i][e] = __float_as_uint(hu) >> 16 | __float_as_uint(hv);
-                            u = u == hu ? 0.f : u - hu;
-                            v = v == hv ? 0.f : v - hv;
+                            a[k][i][e] = __builtin_amdgcn_perm(__float_as_uint(v), __float_as_uint(u), 0x07060302u);
+                            // (an infinity has no rest, NaN keeps one; a rest is no infinity)
+                            u = k == 0 && u == hu ? 0.f : u - hu;
+                            v = k == 0 && v == hv ? 0.f : v - hv;
                         }
                     }
                 }
@@ -766,8 +768,8 @@ struct WgradPlan {
 // The rule goes by the workgroups that each tile gives the 256 CUs and by the slices that
 // each of them walks over. Measured, us a call, bf16 / fp32 gradients, tokens x rows x columns:
 //   - DIRECT while two rounds of 64-tiles serve and a workgroup has at most 128 groups to
-//     share out over its waves. Against B128_PAIR: 1024^3 10.6 / 13.5 (15.2 / 26.8), 4096 x
-//     1024^2 19.9 / 38.6 (23.6 / 41.6), 512 x 1536 x 1280 10.0 / 15.4 (9.9 / 26.3); beyond:
+//     share out over its waves. Against B128_PAIR: 1024^3 9.3 / 12.0 (15.2 / 26.8), 4096 x
+//     1024^2 20.0 / 35.4 (23.6 / 41.6), 512 x 1536 x 1280 10.0 / 15.4 (9.9 / 26.3); beyond:
 //     8192 x 1024^2 34.7 / 72.9 (26.8 / 68.3), 512 x 2048^2 17.3 / 30.0 (10.5 / 24.5).
 //   - B128_PAIR (two groups of waves to a tile) while there are no more tiles than CUs:
 //     512 x 2048^2 10.5 / 24.5 (B128, split in two, 24.9 / 34.6); 512 tiles of 4096 x 2048

@@ -13,7 +13,8 @@
 // those of one token, whose cosines and sines stay in registers with the gains. Where a
 // token's heads fit the wave, each group of lanes keeps one head and the wave walks over
 // tokens, several at a time. Memory bounds it: 8 x 1024 tokens, 32 + 32 heads of 128, bf16, forward
-// 48 us (273 MB, 5.7 TB/s); 16 x 1024 tokens, 16 + 8 heads, backward 72 us (306 MB, 4.3 TB/s).
+// 48 us (273 MB, 5.7 TB/s); 16 x 1024 tokens, 16 + 8 heads, backward 53 us and
+// 4.6 for the gains' sums (306 MB, 5.8 TB/s).
 #include "elementwise8.h"
 #include "train_ops.h"
 
