@@ -16,7 +16,7 @@ from __future__ import annotations
 import ctypes
 import struct
 
-from . import BF16, F32, OK, HimuonError, _dtype_code, _keep_alive, lib
+from . import BF16, F32, OK, HimuonError, _dtype_code, lib
 
 I32, I64 = 0, 1              # himuon_index_t
 MAX_HEAD_DIM = 512           # HIMUON_MAX_HEAD_DIM
@@ -94,16 +94,34 @@ def _same_device(dev, *tensors):
             raise ValueError("tensors must be on one device")
 
 
-def _on(dev, f, *args):
-    """``f(*args)`` with ``dev`` the current device (the default stream has no handle
-    that names its device)."""
+def _away(dev, stream):
+    """Whether a call is for another device or stream than the current ones."""
+    index = dev.index
+    return index != _device() or (stream is not None and (stream.cuda_stream != _raw_stream(index) or stream.device != dev))
+
+
+def _on(dev, stream, f, *args):
+    """``f(*args)`` with ``dev`` the current device (the default stream has no handle that
+    names its device) and ``stream`` the current stream: what the call allocates is then
+    that stream's memory, of which no work on another stream is left. Results may be read
+    and freed on the stream that was current before."""
     torch = _torch()
-    with torch.cuda.device(dev):
-        return f(*args)
+    if stream is None:
+        with torch.cuda.device(dev):
+            return f(*args)
+    if stream.device != dev:
+        raise ValueError("the stream must be on the tensors' device")
+    here = torch.cuda.current_stream(dev)
+    with torch.cuda.stream(stream):
+        result = f(*args)
+    if stream != here:
+        for t in result if isinstance(result, tuple) else (result,):
+            t.record_stream(here)
+    return result
 
 
-def _stream_of(stream, index):
-    return (_raw_stream(index) if stream is None else stream.cuda_stream) or None
+def _stream_of(index):
+    return _raw_stream(index) or None
 
 
 def _new(like, shape, dtype):
@@ -113,19 +131,19 @@ def _new(like, shape, dtype):
     return _torch().empty(shape, dtype=dtype, device=like.device)
 
 
-def _workspace(need, given, like, fresh):
-    """(address, bytes) of ``given``, or of a fresh workspace of ``need`` bytes (none for 0:
-    the call needs none, or reports what is wrong with it)."""
+def _workspace(need, given, like):
+    """(tensor, address, bytes) of ``given``, or of a fresh workspace of ``need`` bytes (none
+    for 0: the call needs none, or reports what is wrong with it). The caller holds the
+    tensor until its work is enqueued."""
     if given is None:
         if need == 0:
-            return None, 0
+            return None, None, 0
         torch = _torch()
         given = torch.empty(need, dtype=torch.uint8, device=like.device)
-        fresh.append(given)
-        return given.data_ptr(), need
+        return given, given.data_ptr(), need
     if given.device != like.device:
         raise ValueError("the workspace must be on the tensors' device")
-    return given.data_ptr(), given.numel() * given.element_size()
+    return given, given.data_ptr(), given.numel() * given.element_size()
 
 
 def _done(status, what):
@@ -144,13 +162,13 @@ def embed(tokens, table, scale=1.0, out=None, stream=None):
     rows, width, ld = _matrix(table, "table")
     if not tokens.is_cuda or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous CUDA tensor")
-    dev, n, fresh = table.device, tokens.numel(), ()
-    if dev.index != _device():
-        return _on(dev, embed, tokens, table, scale, out, stream)
+    dev, n = table.device, tokens.numel()
+    if _away(dev, stream):
+        return _on(dev, stream, embed, tokens, table, scale, out)
     code, index = _type_code(table), _index_code(tokens)
     if out is None:
         out = table.new_empty((*tokens.shape, width))
-        fresh, ld_out = (out,), width
+        ld_out = width
         _same_device(dev, tokens)
     else:
         if out.dtype != table.dtype or tuple(out.shape) not in ((n, width), (*tokens.shape, width)):
@@ -160,9 +178,7 @@ def embed(tokens, table, scale=1.0, out=None, stream=None):
         ld_out = _matrix(out, "out")[2] if out.dim() == 2 else width
         _same_device(dev, tokens, out)
     _done(lib().himuon_embed(n, tokens.data_ptr(), index, rows, width, table.data_ptr(), ld, out.data_ptr(), ld_out,
-                             scale, code, _stream_of(stream, dev.index)), "himuon_embed")
-    if stream is not None:
-        _keep_alive(fresh, stream, dev)
+                             scale, code, _stream_of(dev.index)), "himuon_embed")
     return out
 
 
@@ -176,7 +192,7 @@ def embed_grad(tokens, grad, num_rows, scale=1.0, out=None, dtype=None, accumula
     _torch()
     if not tokens.is_cuda or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous CUDA tensor")
-    n, fresh = tokens.numel(), []
+    n = tokens.numel()
     if grad.dim() != 2:
         if tuple(grad.shape[:-1]) != tuple(tokens.shape) or not grad.is_contiguous():
             raise ValueError("grad must have one row per token")
@@ -187,23 +203,20 @@ def embed_grad(tokens, grad, num_rows, scale=1.0, out=None, dtype=None, accumula
     if accumulate and out is None:
         raise ValueError("accumulate needs the tensor to add to")
     dev, rows = grad.device, int(num_rows)
-    if dev.index != _device():
-        return _on(dev, embed_grad, tokens, grad, rows, scale, out, dtype, accumulate, workspace, stream)
+    if _away(dev, stream):
+        return _on(dev, stream, embed_grad, tokens, grad, rows, scale, out, dtype, accumulate, workspace)
     code, index = _type_code(grad), _index_code(tokens)
     L = lib()
-    ws, ws_bytes = _workspace(L.himuon_embed_grad_workspace_size(n, rows, width), workspace, grad, fresh)
+    held, ws, ws_bytes = _workspace(L.himuon_embed_grad_workspace_size(n, rows, width), workspace, grad)
     if out is None:
         out = _new(grad, (rows, width), dtype)
-        fresh.append(out)
     elif tuple(out.shape) != (rows, width) or (dtype is not None and out.dtype != dtype):
         raise ValueError("out must be num_rows x width of the asked type")
     ld_out = _matrix(out, "out")[2]
     _same_device(dev, tokens, out)
     _done(L.himuon_embed_grad(n, tokens.data_ptr(), index, rows, width, grad.data_ptr(), ld, code, out.data_ptr(), ld_out,
-                              _type_code(out), scale, bool(accumulate), ws, ws_bytes, _stream_of(stream, dev.index)),
+                              _type_code(out), scale, bool(accumulate), ws, ws_bytes, _stream_of(dev.index)),
           "himuon_embed_grad")
-    if stream is not None:
-        _keep_alive(fresh, stream, dev)
     return out
 
 
@@ -284,12 +297,10 @@ def qk_norm_rope(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, inter
     ``out``         the two tensors to write (q and k themselves are allowed)."""
     sq, sk, args, hq, hk = _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
     dev = q.device
-    if dev.index != _device():
-        return _on(dev, qk_norm_rope, q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, out, stream)
+    if _away(dev, stream):
+        return _on(dev, stream, qk_norm_rope, q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, out)
     oq, ok, ho, hp = _outputs(out, q, k, sq, sk)
-    _done(lib().himuon_qk_norm_rope(args, hq, hk, ho, hp, _stream_of(stream, dev.index)), "himuon_qk_norm_rope")
-    if stream is not None and out is None:
-        _keep_alive((oq, ok), stream, dev)
+    _done(lib().himuon_qk_norm_rope(args, hq, hk, ho, hp, _stream_of(dev.index)), "himuon_qk_norm_rope")
     return oq, ok
 
 
@@ -301,21 +312,18 @@ def qk_norm_rope_grad(g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions=None, 
     torch = _torch()
     sq, sk, args, hq, hk = _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
     dev = q.device
-    if dev.index != _device():
-        return _on(dev, qk_norm_rope_grad, g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, out,
-                   workspace, stream)
+    if _away(dev, stream):
+        return _on(dev, stream, qk_norm_rope_grad, g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, out,
+                   workspace)
     gq, gk = _heads_like(g_q, "g_q", sq, q), _heads_like(g_k, "g_k", sk, k)
     L = lib()
     batch, seq = (sq[0], sq[1]) if len(sq) == 4 else (1, sq[0])
-    fresh = []
-    ws, ws_bytes = _workspace(L.himuon_qk_norm_rope_grad_workspace_size(batch, seq, sq[-1]), workspace, q, fresh)
+    held, ws, ws_bytes = _workspace(L.himuon_qk_norm_rope_grad_workspace_size(batch, seq, sq[-1]), workspace, q)
     oq, ok, ho, hp = _outputs(out, q, k, sq, sk)
     dwq, dwk = torch.empty_like(q_gain), torch.empty_like(k_gain)
     _done(L.himuon_qk_norm_rope_grad(args, gq, gk, hq, hk, ho, hp, dwq.data_ptr(), dwk.data_ptr(), ws, ws_bytes,
-                                     _stream_of(stream, dev.index)),
+                                     _stream_of(dev.index)),
           "himuon_qk_norm_rope_grad")
-    if stream is not None:
-        _keep_alive((oq, ok, dwq, dwk, *fresh), stream, dev)
     return oq, ok, dwq, dwk
 
 
@@ -338,8 +346,8 @@ def act_pack(x, out=None, stream=None):
     torch = _torch()
     n, cols, ld = _matrix(x, "x")
     dev, code, groups = x.device, _type_code(x), -(-n // ACT_GROUP)
-    if dev.index != _device():
-        return _on(dev, act_pack, x, out, stream)
+    if _away(dev, stream):
+        return _on(dev, stream, act_pack, x, out)
     if out is None:
         codes = torch.empty((groups, cols, ACT_GROUP), dtype=torch.uint8, device=dev)
         exps = codes.new_empty((groups, cols))
@@ -349,9 +357,7 @@ def act_pack(x, out=None, stream=None):
             raise ValueError("out must be codes [ceil(tokens / 32), columns, 32] and exponents [ceil(tokens / 32), columns]")
         _same_device(dev, codes)
     _done(lib().himuon_act_pack(n, cols, x.data_ptr(), ld, code, codes.data_ptr(), exps.data_ptr(),
-                                _stream_of(stream, dev.index)), "himuon_act_pack")
-    if stream is not None and out is None:
-        _keep_alive((codes, exps), stream, dev)
+                                _stream_of(dev.index)), "himuon_act_pack")
     return codes, exps
 
 
@@ -360,22 +366,19 @@ def act_unpack(codes, exps, tokens, dtype=None, out=None, stream=None):
     ``dtype`` (bfloat16 by default; exact in both types)."""
     torch = _torch()
     groups, cols = _packed(codes, exps)
-    n, dev, fresh = int(tokens), codes.device, ()
+    n, dev = int(tokens), codes.device
     if n < 0 or -(-n // ACT_GROUP) != groups:
         raise ValueError("tokens does not match the number of groups")
-    if dev.index != _device():
-        return _on(dev, act_unpack, codes, exps, n, dtype, out, stream)
+    if _away(dev, stream):
+        return _on(dev, stream, act_unpack, codes, exps, n, dtype, out)
     if out is None:
         out = torch.empty((n, cols), dtype=torch.bfloat16 if dtype is None else dtype, device=dev)
-        fresh = (out,)
     elif tuple(out.shape) != (n, cols) or (dtype is not None and out.dtype != dtype):
         raise ValueError("out must be tokens x columns of the asked type")
     ld = _matrix(out, "out")[2]
     _same_device(dev, out)
     _done(lib().himuon_act_unpack(n, cols, codes.data_ptr(), exps.data_ptr(), out.data_ptr(), ld, _type_code(out),
-                                  _stream_of(stream, dev.index)), "himuon_act_unpack")
-    if stream is not None:
-        _keep_alive(fresh, stream, dev)
+                                  _stream_of(dev.index)), "himuon_act_unpack")
     return out
 
 
@@ -392,21 +395,17 @@ def weight_grad(grad, codes, exps, out=None, dtype=None, accumulate=False, works
     if accumulate and out is None:
         raise ValueError("accumulate needs the tensor to add to")
     code, dev, at = _type_code(grad), grad.device, grad.data_ptr()
-    if dev.index != _device():
-        return _on(dev, weight_grad, grad, codes, exps, out, dtype, accumulate, workspace, stream)
+    if _away(dev, stream):
+        return _on(dev, stream, weight_grad, grad, codes, exps, out, dtype, accumulate, workspace)
     L = lib()
-    fresh = []
-    ws, ws_bytes = _workspace(L.himuon_weight_grad_workspace_size(n, rows, cols, at, ld, code), workspace, grad, fresh)
+    held, ws, ws_bytes = _workspace(L.himuon_weight_grad_workspace_size(n, rows, cols, at, ld, code), workspace, grad)
     if out is None:
         out = _new(grad, (rows, cols), dtype)
-        fresh.append(out)
     elif tuple(out.shape) != (rows, cols) or (dtype is not None and out.dtype != dtype):
         raise ValueError("out must be rows x columns of the asked type")
     ld_out = _matrix(out, "out")[2]
     _same_device(dev, codes, out)
     _done(L.himuon_weight_grad(n, rows, cols, at, ld, code, codes.data_ptr(), exps.data_ptr(), out.data_ptr(), ld_out,
-                               _type_code(out), bool(accumulate), ws, ws_bytes, _stream_of(stream, dev.index)),
+                               _type_code(out), bool(accumulate), ws, ws_bytes, _stream_of(dev.index)),
           "himuon_weight_grad")
-    if stream is not None:
-        _keep_alive(fresh, stream, dev)
     return out
