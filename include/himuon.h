@@ -490,7 +490,9 @@ int himuon_select_compute(int dtype, int compute, int K, float a, float b, float
  * norms and products are held in fp32; a result is rounded once, on store. Every
  * result is the same, bit for bit, from call to call (no order of atomics).
  * Leading dimensions and strides count elements. Empty batches (no token) are
- * valid; sizes above INT32_MAX rows or columns are HIMUON_ERR_UNSUPPORTED.
+ * valid. Sizes that a kernel's indexes or a launch cannot hold are
+ * HIMUON_ERR_UNSUPPORTED: 2^31 rows, columns or tokens (2^30 tokens of a table's
+ * gradient, 2^29 of an activation, 2^26 columns), 2^32 threads.
  */
 
 /* Integer type of token and position arrays. */
@@ -567,8 +569,9 @@ typedef struct himuon_qk {
  *     y = R(p) (x * gain / sqrt(mean(x^2) + eps)),
  * R(p) the rotation of the pairs (u, v) by the angles of the token's position:
  * u' = u cos - v sin, v' = v cos + u sin. Outputs may be the inputs (same
- * strides). A token whose position lies outside the table is one that is not in
- * use: its outputs are zeros, and it gives no gradient.
+ * strides); an output's stride must not be 0 where there is more than one to step
+ * over. A token whose position lies outside the table is one that is not in use:
+ * its outputs are zeros, and it gives no gradient.
  */
 int himuon_qk_norm_rope(const himuon_qk_t* args, const himuon_heads_t* q, const himuon_heads_t* k,
                         const himuon_heads_t* q_out, const himuon_heads_t* k_out, void* stream);

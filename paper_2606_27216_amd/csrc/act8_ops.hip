@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kThreads) act_pack(const void* x, int64_t ld, 
             mine[2 * N * lane + ((2 * j + h) ^ (lane & (2 * N - 1)))] = u32x4{q[4 * h], q[4 * h + 1], q[4 * h + 2], q[4 * h + 3]};
         if (j < n && c0 + lane * N < cols) exps[tb * cols + c + j] = (uint8_t)code;
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_exchange();
     u32x4* const dst = reinterpret_cast<u32x4*>(codes + (tb * cols + c0) * kGroup);
     const int pieces = 2 * (int)min((int64_t)(64 * N), cols - c0);
 #pragma unroll
@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN * KG, MINW) wgrad_blocks(const 
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<f32x4*>(mine + li * PITCH + (32 * j + 8 * g + 4 * lh) * 4) =
                     f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
 #pragma unroll 4
         for (int r = lane / LR; r < 32; r += 64 / LR) {
             const f32x4 v = *reinterpret_cast<const f32x4*>(mine + r * PITCH + (lane % LR) * 16);
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN * KG, MINW) wgrad_blocks(const 
             else
                 put_result<OT>(p.out, (int64_t)o * p.ld_out + j, min(4, p.cols - j), p.accumulate != 0, v);
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
     }
 }
 
@@ -839,7 +839,7 @@ template <GemmStore OT, int BM, int BN, int WGM, int WGN, int KG, int NS, int MI
     p.ti = (int32_t)ceil_div(p.rows, BM);
     p.tj = (int32_t)ceil_div(p.cols, BN);
     const int64_t total = (int64_t)p.ti * p.tj * p.splits;
-    if (total > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    if (!launchable(total, 64 * WGM * WGN * KG)) return HIMUON_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((wgrad_blocks<OT, BM, BN, WGM, WGN, KG, NS, MINW>), dim3((unsigned)total), dim3(64 * WGM * WGN * KG), 0,
                        stream, p);
     return join_splits<OT>(p, stream);
@@ -878,7 +878,7 @@ extern "C" int himuon_act_pack(int64_t n_tokens, int64_t cols, const void* x, in
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     const int64_t slabs = ceil_div(cols, 64 * (dtype == HIMUON_BF16 ? kCols<GemmStore::BF16> : kCols<GemmStore::F32>));
     const int64_t units = ceil_div(n_tokens, kGroup) * slabs, blocks = ceil_div(units, kThreads / 64);
-    if (blocks > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    if (!launchable(blocks, kThreads)) return HIMUON_ERR_UNSUPPORTED;
     uint8_t* const q = static_cast<uint8_t*>(codes);
     uint8_t* const e = static_cast<uint8_t*>(exponents);
     if (dtype == HIMUON_BF16)
@@ -904,7 +904,7 @@ extern "C" int himuon_act_unpack(int64_t n_tokens, int64_t cols, const void* cod
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     const int64_t slabs = ceil_div(cols, 128);
     const int64_t units = ceil_div(n_tokens, kGroup) * slabs, blocks = ceil_div(units, kThreads / 64);
-    if (blocks > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    if (!launchable(blocks, kThreads)) return HIMUON_ERR_UNSUPPORTED;
     const uint8_t* const q = static_cast<const uint8_t*>(codes);
     const uint8_t* const e = static_cast<const uint8_t*>(exponents);
     if (dtype == HIMUON_BF16)

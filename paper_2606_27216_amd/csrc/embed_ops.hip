@@ -80,7 +80,7 @@ template <GemmStore ST, int LPR, int U> int launch_embed(EmbedArgs p, hipStream_
     p.segs = (int)ceil_div(p.dim, LPR * U * 8);
     p.units = ceil_div(p.n, kWave / LPR) * p.segs;
     const int64_t blocks = ceil_div(p.units, kThreads / kWave);
-    if (blocks > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    if (!launchable(blocks, kThreads)) return HIMUON_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((embed_rows<ST, LPR, U>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
     return launch_status();
 }
@@ -146,9 +146,9 @@ struct SortArgs {
     const void* tokens;          // first digit: the caller's tokens
     const uint32_t *key_in, *pos_in;
     uint32_t *key_out, *pos_out;
-    uint32_t* hist;              // [tiles][bins]
+    uint32_t* hist;              // [tiles][bins], scanned: [tiles + 1][bins]
     int64_t rows;
-    int32_t n, wide, tiles, shift, bits, first;
+    int32_t n, wide, tiles, shift, bits, first, scanned;
     FillArgs fill;
 };
 
@@ -174,6 +174,45 @@ __global__ void __launch_bounds__(kThreads) sort_count(const SortArgs p)
     }
     __syncthreads();
     for (int b = threadIdx.x; b < bins; b += kThreads) p.hist[(int64_t)blockIdx.x * bins + b] = h[b];
+}
+
+// Long lists: the tiles' counts of a digit become those of the tiles before each, with the
+// totals in a row of their own. A block has 64 digits, its waves a part of the tiles each.
+constexpr int kScanThreads = 1024;
+
+__global__ void __launch_bounds__(kScanThreads) sort_scan(const SortArgs p)
+{
+    constexpr int W = kScanThreads / kWave, U = 16;
+    __shared__ uint32_t sums[W][kWave];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int bins = 1 << p.bits, bin = blockIdx.x * kWave + lane;
+    const bool on = bin < bins;
+    uint32_t* const col = p.hist + (on ? bin : 0);
+    const int t0 = (int)((int64_t)p.tiles * wave / W), t1 = (int)((int64_t)p.tiles * (wave + 1) / W);
+    uint32_t sum = 0;
+    for (int t = t0; t < t1; t += U) {
+        uint32_t h[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) h[k] = col[(int64_t)min(t + k, t1 - 1) * bins];
+#pragma unroll
+        for (int k = 0; k < U; ++k) sum += t + k < t1 ? h[k] : 0u;
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int w = 0; w < wave; ++w) before += sums[w][lane];
+    for (int t = t0; t < t1; t += U) {
+        uint32_t h[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) h[k] = col[(int64_t)min(t + k, t1 - 1) * bins];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (t + k < t1 && on) col[(int64_t)(t + k) * bins] = before;
+            before += t + k < t1 ? h[k] : 0u;
+        }
+    }
+    if (wave == W - 1 && on) col[(int64_t)p.tiles * bins] = before;
 }
 
 // Moves a tile's keys to their places by this digit. A wave ranks 64 keys at a time:
@@ -222,7 +261,17 @@ __global__ void __launch_bounds__(kThreads) sort_scatter(const SortArgs p)
 #pragma unroll
     for (int j = 0; j < BPT; ++j) total[j] = before[j] = 0;
     const int b0 = tid * BPT;
-    if (b0 < bins) {
+    if (b0 < bins && p.scanned) {
+        const uint4* const row = reinterpret_cast<const uint4*>(p.hist) + tid;
+        const int64_t step = bins / BPT;
+        const uint4 all = row[p.tiles * step], earlier = row[blockIdx.x * step];
+        const uint32_t a[BPT] = {all.x, all.y, all.z, all.w}, v[BPT] = {earlier.x, earlier.y, earlier.z, earlier.w};
+#pragma unroll
+        for (int j = 0; j < BPT; ++j) {
+            total[j] = a[j];
+            before[j] = v[j];
+        }
+    } else if (b0 < bins) {
         const uint4* const row = reinterpret_cast<const uint4*>(p.hist) + tid;
         const int step = bins / BPT;  // (eight rows at a time, all loads in flight)
         for (int t0 = 0; t0 < p.tiles; t0 += 8) {
@@ -534,7 +583,8 @@ template <GemmStore ST, GemmStore OT> __global__ void __launch_bounds__(kFewThre
         const uint32_t per = (uint32_t)((f.row_bytes + 15) / 16);
         // (a launch's blocks have at most 4096 rows of at most 32 KB, or one row)
         for (uint32_t x = threadIdx.x; x < per * (uint32_t)rows; x += kFewThreads) {
-            const uint32_t r = x / per, c = (x - r * per) * 16;
+            const uint32_t r = x / per;
+            const int64_t c = (int64_t)(x - r * per) * 16;
             if (named[r]) continue;
             uint8_t* const at = f.out + (r0 + r) * f.ld_bytes + c;
             const int64_t left = f.row_bytes - c;
@@ -614,7 +664,7 @@ template <GemmStore ST, GemmStore OT> __global__ void __launch_bounds__(kFewThre
 template <GemmStore ST, GemmStore OT> int launch_few(const FewArgs& f, hipStream_t stream)
 {
     const int64_t fill = f.sum.accumulate ? 0 : ceil_div(f.sum.rows, f.fill_rows);
-    if (f.sum.n + fill > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    if (!launchable(f.sum.n + fill, kFewThreads)) return HIMUON_ERR_UNSUPPORTED;
     // columns shared out over blocks while these are few: one token 100 times, 4096 columns
     const int64_t parts = std::min<int64_t>(f.sum.slabs, std::max<int64_t>(2, 2048 / f.sum.n));
     hipLaunchKernelGGL((sum_few<ST, OT>), dim3((unsigned)(f.sum.n + fill), (unsigned)parts), dim3(kFewThreads), 0, stream, f);
@@ -626,7 +676,7 @@ template <GemmStore ST, GemmStore OT, int S> int launch_sums(SumArgs p, hipStrea
     p.chunks = (int)ceil_div(p.n, S);
     p.units = (int64_t)p.chunks * p.slabs;
     const int64_t blocks = ceil_div(p.units, kThreads / kWave);
-    if (blocks > INT32_MAX || p.slabs > 65535) return HIMUON_ERR_UNSUPPORTED;
+    if (!launchable(blocks, kThreads) || p.slabs > 65535) return HIMUON_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((sum_runs<ST, OT, S>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
     const int st = launch_status();
     if (st != HIMUON_OK || p.chunks < 2) return st;
@@ -660,12 +710,12 @@ int key_bits(int64_t rows)
 struct GradPlan {
     size_t key[2], pos[2], hist, part, total;
     int digits, bits, tiles, chunk;
-    bool few;
+    bool few, scan;
 };
 
 GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
 {
-    GradPlan g;
+    GradPlan g{};
     const int kb = key_bits(rows);
     g.digits = (kb + 9) / 10;
     g.bits = std::max(2, (kb + g.digits - 1) / g.digits);  // (bins in groups of four)
@@ -673,8 +723,11 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
     // 5003 x 1000 10.1 and 17.2; but 600 into 32000 x 4096 49 and 44, 1500 of one token 35 and 22.
     g.few = n > 0 && n <= (dim <= 2 * kSlab ? kFewMost : kFewMost / 2);
     g.tiles = (int)ceil_div(n, kTile);
+    // Beyond, a launch of its own adds the tiles' counts up, which otherwise every tile does for
+    // itself: 65536 x 64 into 50000 rows 52 us so and 50 not, 131072 x 64 61 and 67, 4 M x 64
+    // 591 and 2507.
+    g.scan = g.tiles > 96;
     g.chunk = chunk_size(n);
-    g.total = 0;
     if (g.few || n == 0) return g;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -686,7 +739,7 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
         g.key[b] = take((size_t)n * 4);
         g.pos[b] = take((size_t)n * 4);
     }
-    g.hist = take(((size_t)g.tiles << g.bits) * 4);
+    g.hist = take(((size_t)(g.tiles + g.scan) << g.bits) * 4);
     g.part = take((size_t)ceil_div(n, g.chunk) * 2 * (size_t)dim * 4);
     g.total = at;
     return g;
@@ -776,6 +829,7 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
     s.wide = index == HIMUON_I64;
     s.tiles = g.tiles;
     s.bits = g.bits;
+    s.scanned = g.scan;
     if (g.few) {
         FewArgs f{};
         s.first = 1;
@@ -832,6 +886,11 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
             hipLaunchKernelGGL(sort_count, grid, dim3(kThreads), 0, hs, s);
             int st = launch_status();
             if (st != HIMUON_OK) return st;
+            if (g.scan) {
+                hipLaunchKernelGGL(sort_scan, dim3((unsigned)ceil_div(INT64_C(1) << g.bits, kWave)), dim3(kScanThreads), 0, hs, s);
+                st = launch_status();
+                if (st != HIMUON_OK) return st;
+            }
             grid = with_fill(2 * d + 1, 2 * g.digits, g.tiles, kThreads);
             hipLaunchKernelGGL(sort_scatter, grid, dim3(kThreads), 0, hs, s);
             st = launch_status();

@@ -503,7 +503,7 @@ template <bool BWD, GemmStore ST, bool INTER, bool VEC, int L> int launch_l(QkAr
         p.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(groups, 4096 / std::max<int64_t>(1, p.tokens)));
         p.units = p.tokens * p.parts;
         const int64_t blocks = ceil_div(p.units, kWaves);
-        if (blocks > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+        if (!launchable(blocks, kThreads)) return HIMUON_ERR_UNSUPPORTED;
         hipLaunchKernelGGL((qk_forward<ST, INTER, VEC, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
     }
     return launch_status();
@@ -551,6 +551,12 @@ int check_args(const himuon_qk_t* a)
     return HIMUON_OK;
 }
 
+// An output's rows must not fall on each other.
+bool distinct(const himuon_qk_t* a, const himuon_heads_t* h, int heads)
+{
+    return h && (a->batch < 2 || h->stride_batch) && (a->seq < 2 || h->stride_seq) && (heads < 2 || h->stride_head);
+}
+
 bool set(Strided& s, const himuon_heads_t* h)
 {
     if (!h || !h->ptr) return false;
@@ -596,6 +602,7 @@ extern "C" int himuon_qk_norm_rope(const himuon_qk_t* args, const himuon_heads_t
     if (args->batch == 0 || args->seq == 0) return HIMUON_OK;
     QkArgs p = common(args);
     if (!set(p.q, q) || !set(p.k, k) || !set(p.qo, q_out) || !set(p.ko, k_out)) return HIMUON_ERR_INVALID_ARG;
+    if (!distinct(args, q_out, p.hq) || !distinct(args, k_out, p.hk)) return HIMUON_ERR_INVALID_ARG;
     StreamDevice on(stream);
     if (on.status != HIMUON_OK) return on.status;
     return launch_qk<false>(p, args, static_cast<hipStream_t>(stream));
@@ -622,6 +629,7 @@ extern "C" int himuon_qk_norm_rope_grad(const himuon_qk_t* args, const himuon_he
     // (without a token there is nothing to read: the gains' gradients become zero)
     if (p.tokens > 0 && (!set(p.gq, g_q) || !set(p.gk, g_k) || !set(p.q, q) || !set(p.k, k) || !set(p.qo, dq) || !set(p.ko, dk)))
         return HIMUON_ERR_INVALID_ARG;
+    if (p.tokens > 0 && (!distinct(args, dq, p.hq) || !distinct(args, dk, p.hk))) return HIMUON_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace & 15) ||
         workspace_bytes < himuon_qk_norm_rope_grad_workspace_size(args->batch, args->seq, args->head_dim))
         return HIMUON_ERR_WORKSPACE;

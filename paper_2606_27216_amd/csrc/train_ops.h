@@ -105,6 +105,18 @@ template <GemmStore ST> __device__ __forceinline__ void put1(void* base, int64_t
     else static_cast<float*>(base)[i] = v;
 }
 
+// Whether a launch of this many blocks (of `threads` each, in x) stays below 2^32 threads.
+inline bool launchable(int64_t blocks, int threads) { return blocks <= (int64_t)(UINT32_MAX / (uint32_t)threads); }
+
+// Between a wave's writes to LDS and reads of what its other lanes wrote: they are carried out
+// in order, so only the compiler has to keep it.
+__device__ __forceinline__ void wave_exchange()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // True if the product of two non-negative values stays below 2^62.
 inline bool small_product(int64_t a, int64_t b) { return a == 0 || b <= (INT64_C(1) << 62) / a; }
 
