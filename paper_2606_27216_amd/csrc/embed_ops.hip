@@ -5,9 +5,9 @@
 // Both are bound by memory. The lookup is a gather: a row (or a part of one) per
 // group of lanes, four 16-byte chunks in flight per lane.
 //
-// The gradient sorts the tokens (stable radix sort of (token, position), two or
-// three digits, ranks by ballots within a wave), so that a row's terms are
-// adjacent and its sum has one order. The sorted list is cut into chunks of S
+// The gradient sorts the tokens (stably: short lists by comparison, longer ones in parts that
+// are merged, long ones by digits, ranked by ballots within a wave), so that a row's terms
+// are adjacent and its sum has one order. The sorted list is cut into chunks of S
 // entries, whatever rows they name: a wave sums the runs of equal tokens of its
 // chunk over 512 columns. Runs that lie inside a chunk go to the table at once; a run
 // that crosses chunks leaves one fp32 partial sum per chunk, and a last launch
@@ -16,7 +16,7 @@
 // that set the table to zero ride in them, and the sums then write the rows that occur.
 //
 // Measured: lookup of 16384 x 2560 bf16 22 us (121 MB, 5.5 TB/s); gradient of 16384 x 4096
-// into 32000 rows, bf16, 85 us (396 MB that it cannot do without, 4.7 TB/s): the sort with the zeros 48,
+// into 32000 rows, bf16, 84 us (396 MB that it cannot do without, 4.7 TB/s): the sort with the zeros 48,
 // sums 31, joins 6.
 #include "elementwise8.h"
 #include "train_ops.h"
@@ -141,6 +141,7 @@ template <int THREADS> __device__ __forceinline__ void fill_rows(const FillArgs&
 constexpr int kMaxBins = 1024;
 constexpr int kIpt = 4;                      // keys per thread and tile
 constexpr int kTile = kThreads * kIpt;       // keys of a tile
+constexpr uint32_t kNone = 0xffffffffu;      // no key
 
 struct SortArgs {
     const void* tokens;          // first digit: the caller's tokens
@@ -149,6 +150,7 @@ struct SortArgs {
     uint32_t* hist;              // [tiles][bins], scanned: [tiles + 1][bins]
     int64_t rows;
     int32_t n, wide, tiles, shift, bits, first, scanned;
+    int32_t groups;              // sort_rank: of 64 entries, in a part of the list
     FillArgs fill;
 };
 
@@ -326,23 +328,23 @@ __global__ void __launch_bounds__(kThreads) sort_scatter(const SortArgs p)
     }
 }
 
-// A short list in one launch: an entry's place is the number of entries before it, those
-// with a smaller key and earlier ones with the same. A block ranks 64 entries, its waves
-// share out what these are compared with.
-constexpr int kRankThreads = 1024;
-constexpr int kRankMost = 6144;
+// Short lists are sorted by comparison: an entry's place is the number of entries before it,
+// those with a smaller key and earlier ones with the same. A block ranks 64 entries, its waves
+// share out what these are compared with: the whole list, or a part of it.
+constexpr int kRankThreads = 1024;  // where it is the whole list
 
-__global__ void __launch_bounds__(kRankThreads) sort_rank(const SortArgs p)
+template <int THREADS> __global__ void __launch_bounds__(THREADS) sort_rank(const SortArgs p)
 {
-    constexpr int W = kRankThreads / kWave;
+    constexpr int W = THREADS / kWave;
     __shared__ uint32_t count[W][kWave];
-    if ((int)blockIdx.x >= p.fill.first) return fill_rows<kRankThreads>(p.fill);
+    if ((int)blockIdx.x >= p.fill.first) return fill_rows<THREADS>(p.fill);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = blockIdx.x * kWave + lane;
+    const int c0 = (int)blockIdx.x / p.groups * p.groups, c1 = min(c0 + p.groups, (p.n + kWave - 1) / kWave);
     const uint32_t key = i < p.n ? sort_key(p, i) : 0u;
     uint32_t before = 0;
-    for (int c = wave; c * kWave < p.n; c += W) {
+    for (int c = c0 + wave; c < c1; c += W) {
         const int j = c * kWave + lane;
         const uint32_t other = j < p.n ? sort_key(p, j) : 0xffffffffu;
         if (c == (int)blockIdx.x) {
@@ -360,17 +362,70 @@ __global__ void __launch_bounds__(kRankThreads) sort_rank(const SortArgs p)
     count[wave][lane] = before;
     __syncthreads();
     if (wave > 0 || i >= p.n) return;
-    uint32_t at = 0;
+    uint32_t at = (uint32_t)(c0 * kWave);
 #pragma unroll
     for (int w = 0; w < W; ++w) at += count[w][lane];
     p.key_out[at] = key;
     p.pos_out[at] = (uint32_t)i;
 }
 
+// The sorted parts of a list, merged: an entry's place is its place in its own part and, for
+// each other part, the number of entries there that come before it, by bisection. A block
+// places 64 entries (neighbours in their part, so that they take nearly the same steps), its
+// waves have a part each at a time, in LDS.
+constexpr int kPart = 1024;
+
+template <int THREADS> __global__ void __launch_bounds__(THREADS) sort_merge(const SortArgs p)
+{
+    constexpr int W = THREADS / kWave;
+    __shared__ __attribute__((aligned(16))) uint32_t parts[W][kPart];
+    __shared__ uint32_t count[W][kWave];
+    if ((int)blockIdx.x >= p.fill.first) return fill_rows<THREADS>(p.fill);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = blockIdx.x * kWave + lane, own = (int)blockIdx.x / (kPart / kWave);
+    const uint32_t key = p.key_in[min(i, p.n - 1)];
+    uint32_t* const part = parts[wave];
+    uint32_t before = 0;
+    for (int t = wave; t * kPart < p.n; t += W) {
+        if (t == own) {
+            before += (uint32_t)(i - own * kPart);
+            continue;
+        }
+        // (the last part's reads past the list stay within the workspace, and count for nothing)
+        const int first = t * kPart + 4 * lane;
+        uint4 k[kPart / 256];
+#pragma unroll
+        for (int u = 0; u < kPart / 256; ++u) k[u] = *reinterpret_cast<const uint4*>(p.key_in + first + 256 * u);
+#pragma unroll
+        for (int u = 0; u < kPart / 256; ++u) {
+            const int at = first + 256 * u;
+            const uint4 v = uint4{at < p.n ? k[u].x : kNone, at + 1 < p.n ? k[u].y : kNone, at + 2 < p.n ? k[u].z : kNone,
+                                  at + 3 < p.n ? k[u].w : kNone};
+            *reinterpret_cast<uint4*>(part + 4 * lane + 256 * u) = v;
+        }
+        wave_exchange();
+        const uint32_t limit = key + (t < own ? 1u : 0u);
+        uint32_t n = 0;
+#pragma unroll
+        for (int step = kPart / 2; step > 0; step /= 2) n += part[n + step - 1] < limit ? step : 0;
+        n += part[n] < limit ? 1u : 0u;
+        before += n;
+        wave_exchange();
+    }
+    count[wave][lane] = before;
+    __syncthreads();
+    if (wave > 0 || i >= p.n) return;
+    uint32_t at = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) at += count[w][lane];
+    p.key_out[at] = key;
+    p.pos_out[at] = p.pos_in[i];
+}
+
 // --------------------------------------------------------------------- sums
 
 constexpr int kSlab = 512;          // columns of a wave
-constexpr uint32_t kNone = 0xffffffffu;
 
 struct SumArgs {
     const uint32_t *key, *pos;      // sorted
@@ -707,10 +762,14 @@ int key_bits(int64_t rows)
     return b;
 }
 
+// How a call's tokens are sorted.
+enum class Sort : int { RANK, MERGE, RADIX };
+
 struct GradPlan {
     size_t key[2], pos[2], hist, part, total;
     int digits, bits, tiles, chunk;
     bool few, scan;
+    Sort sort;
 };
 
 GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
@@ -723,6 +782,11 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
     // 5003 x 1000 10.1 and 17.2; but 600 into 32000 x 4096 49 and 44, 1500 of one token 35 and 22.
     g.few = n > 0 && n <= (dim <= 2 * kSlab ? kFewMost : kFewMost / 2);
     g.tiles = (int)ceil_div(n, kTile);
+    // One launch, two, or two to three for each digit. Measured, x 64 into 50000 rows: 4096
+    // tokens RANK 23.3 us, MERGE 20.5; 6144 29.1 and 22.3; MERGE and RADIX: 16384 30 and 40, 32768 37
+    // and 43, 65536 53 and 51 (x 256). With one digit RADIX has two launches as well: 6144 into 1000 rows
+    // RANK 28.7, RADIX 22.9.
+    g.sort = n <= 4096 ? Sort::RANK : n <= 49152 && g.digits > 1 ? Sort::MERGE : Sort::RADIX;
     // Beyond, a launch of its own adds the tiles' counts up, which otherwise every tile does for
     // itself: 65536 x 64 into 50000 rows 52 us so and 50 not, 131072 x 64 61 and 67, 4 M x 64
     // 591 and 2507.
@@ -739,7 +803,7 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
         g.key[b] = take((size_t)n * 4);
         g.pos[b] = take((size_t)n * 4);
     }
-    g.hist = take(((size_t)(g.tiles + g.scan) << g.bits) * 4);
+    g.hist = take(g.sort == Sort::RADIX ? ((size_t)(g.tiles + g.scan) << g.bits) * 4 : 0);
     g.part = take((size_t)ceil_div(n, g.chunk) * 2 * (size_t)dim * 4);
     g.total = at;
     return g;
@@ -850,9 +914,9 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
     s.fill.row_bytes = dim * dtype_size(out_dtype);
     s.fill.ld_bytes = ld_dtable * dtype_size(out_dtype);
     // Zeros go past the caches where the rows to be summed are many enough to be worth their
-    // place there. 16384 x 4096 (134 MB) into 32000 rows 92 us so, 119 not; 32768 x 2048
-    // into 50000 of fp32 120 and 150; but 4096 x 2560 (21 MB) into 32000 50 and 42, 2000 x
-    // 4096 (16 MB) 62 and 49.
+    // place there. 16384 x 4096 (134 MB) into 32000 rows 85 us so, 100 not; 32768 x 2048
+    // into 50000 of fp32 115 and 141; but 4096 x 2560 (21 MB) into 32000 46 and 37, 2000 x
+    // 4096 (16 MB) 60 and 47.
     s.fill.stream = n_tokens * dim * dtype_size(dtype) >= (INT64_C(64) << 20);
     // launch `part` of `parts` of the sort, `blocks` blocks of its own and those that fill
     auto with_fill = [&](int64_t part, int64_t parts, int64_t blocks, int threads) -> dim3 {
@@ -861,26 +925,51 @@ extern "C" int himuon_embed_grad(int64_t n_tokens, const void* tokens, int index
         s.fill.first = (int32_t)blocks;
         s.fill.blocks = 0;
         if (!accumulate)  // (a block fills about 64 bytes a thread and round)
-            s.fill.blocks = (int32_t)std::min<int64_t>(ceil_div((s.fill.to - s.fill.from) * s.fill.row_bytes, threads * 64), 8192);
+            s.fill.blocks = (int32_t)std::min<int64_t>(ceil_div((s.fill.to - s.fill.from) * s.fill.row_bytes, threads * 64), 1 << 20);
         return dim3((unsigned)(blocks + s.fill.blocks));
     };
+    auto from_to = [&](int from, int to) {
+        s.key_in = reinterpret_cast<const uint32_t*>(ws + g.key[from]);
+        s.pos_in = reinterpret_cast<const uint32_t*>(ws + g.pos[from]);
+        s.key_out = reinterpret_cast<uint32_t*>(ws + g.key[to]);
+        s.pos_out = reinterpret_cast<uint32_t*>(ws + g.pos[to]);
+    };
     int from = 0;
-    if (n_tokens <= kRankMost) {
+    if (g.sort == Sort::RANK) {
         s.first = 1;
-        s.key_out = reinterpret_cast<uint32_t*>(ws + g.key[0]);
-        s.pos_out = reinterpret_cast<uint32_t*>(ws + g.pos[0]);
+        s.groups = INT32_MAX;
+        from_to(1, 0);
         const dim3 grid = with_fill(0, 1, ceil_div(n_tokens, kWave), kRankThreads);
-        hipLaunchKernelGGL(sort_rank, grid, dim3(kRankThreads), 0, hs, s);
+        hipLaunchKernelGGL(sort_rank<kRankThreads>, grid, dim3(kRankThreads), 0, hs, s);
         const int st = launch_status();
         if (st != HIMUON_OK || n_tokens == 0) return st;
+    } else if (g.sort == Sort::MERGE) {
+        // Blocks of 512 threads place their entries sooner, blocks of 256 are better at setting
+        // rows to zero: 16384 x 1024 into 32000 rows (66 MB) of bf16 36.7 us and 41.0, 32768 x 2560 into
+        // 50000 (256 MB) 96.1 and 92.6, x 2048 of fp32 (410 MB) 121.0 and 115.5.
+        const bool narrow = !accumulate && n_rows * s.fill.row_bytes >= (INT64_C(200) << 20);
+        const int threads = narrow ? 256 : 512;
+        const int64_t blocks = ceil_div(n_tokens, kWave);
+        s.first = 1;
+        s.groups = kPart / kWave;
+        from_to(1, 0);
+        dim3 grid = with_fill(0, 2, blocks, threads);
+        if (narrow) hipLaunchKernelGGL(sort_rank<256>, grid, dim3(256), 0, hs, s);
+        else hipLaunchKernelGGL(sort_rank<512>, grid, dim3(512), 0, hs, s);
+        int st = launch_status();
+        if (st != HIMUON_OK) return st;
+        from_to(0, 1);
+        from = 1;
+        grid = with_fill(1, 2, blocks, threads);
+        if (narrow) hipLaunchKernelGGL(sort_merge<256>, grid, dim3(256), 0, hs, s);
+        else hipLaunchKernelGGL(sort_merge<512>, grid, dim3(512), 0, hs, s);
+        st = launch_status();
+        if (st != HIMUON_OK) return st;
     } else {
         for (int d = 0; d < g.digits; ++d) {
             s.first = d == 0;
             s.shift = d * g.bits;
-            s.key_in = reinterpret_cast<const uint32_t*>(ws + g.key[from]);
-            s.pos_in = reinterpret_cast<const uint32_t*>(ws + g.pos[from]);
-            s.key_out = reinterpret_cast<uint32_t*>(ws + g.key[from ^ 1]);
-            s.pos_out = reinterpret_cast<uint32_t*>(ws + g.pos[from ^ 1]);
+            from_to(from, from ^ 1);
             from ^= 1;
             dim3 grid = with_fill(2 * d, 2 * g.digits, g.tiles, kThreads);
             hipLaunchKernelGGL(sort_count, grid, dim3(kThreads), 0, hs, s);
