@@ -19,12 +19,15 @@
 // into 32000 rows, bf16, 84 us (396 MB that it cannot do without, 4.7 TB/s): the sort with the zeros 48,
 // sums 31, joins 6.
 #include "elementwise8.h"
+#include "ns_device.h"
 #include "train_ops.h"
 
 #include <algorithm>
 
 namespace himuon {
 namespace {
+
+using namespace dev;
 
 constexpr int kThreads = 256;
 constexpr int kWave = 64;
@@ -513,17 +516,57 @@ template <GemmStore ST, GemmStore OT, int S> __global__ void __launch_bounds__(k
 // Adds up the partial sums of the runs that cross chunks. A wave has the run that begins in
 // its chunk and goes on after it; runs of more than kOwnParts parts are shared out over all
 // waves of the block, in order (one token 30000 times, 640 columns: the whole call 60 us
-// with each run left to four waves, 50 so).
+// with each run left to four waves, 49 so).
 constexpr int kOwnParts = 32;
 
-template <GemmStore OT, int S, int kJoinWaves> __global__ void __launch_bounds__(kJoinWaves * kWave) join_runs(const SumArgs p)
+// N consecutive columns of a part, of which n exist.
+template <int N> __device__ __forceinline__ void load_part(const float* p, int n, float (&v)[N])
 {
-    __shared__ float lds[kJoinWaves][kWave][8 + 1];
+    if constexpr (N == 8) {
+        load8<GemmStore::F32>(p, 0, n, false, v);
+    } else {
+        f32x4 w{};
+        if (n == 4) w = *reinterpret_cast<const f32x4_any32*>(p);
+        else w = f32x4{p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = w[e];
+    }
+}
+
+template <GemmStore OT> __device__ __forceinline__ void put_row(const SumArgs& p, uint32_t row, int c, float (&v)[4])
+{
+    const int n = min(4, p.dim - c);
+    const int64_t i = (int64_t)row * p.ld_out + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= p.scale;
+    if (p.accumulate) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += e < n ? get1<OT>(p.out, i + e) : 0.f;
+    }
+    if (n == 4) {
+        if constexpr (OT == GemmStore::BF16)
+            *reinterpret_cast<u32x2_any16*>(static_cast<uint16_t*>(p.out) + i) =
+                u32x2{pack2<Operand::BF16>(v[0], v[1]), pack2<Operand::BF16>(v[2], v[3])};
+        else
+            *reinterpret_cast<f32x4_any32*>(static_cast<float*>(p.out) + i) = f32x4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) put1<OT>(p.out, i + e, v[e]);
+    }
+}
+
+// COLS: columns of a lane. Four instead of eight keep twice the parts in flight, but take twice
+// the blocks: one token 30000 times, 640 columns 39 us a call and 49; 32768 x 4096
+// 129 and 119, 131072 x 1024 109 and 103.
+template <GemmStore OT, int S, int kJoinWaves, int COLS> __global__ void __launch_bounds__(kJoinWaves * kWave) join_runs(const SumArgs p)
+{
+    __shared__ float lds[kJoinWaves][kWave][COLS + 1];
     __shared__ int parts[kJoinWaves];  // of each wave's run, if it is shared out
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int chunk = blockIdx.x * kJoinWaves + wave;
-    const int c = blockIdx.y * kSlab + lane * 8, nc = min(8, p.dim - c);
+    const int c = blockIdx.y * (kWave * COLS) + lane * COLS, nc = min(COLS, p.dim - c);
     const int64_t first = (int64_t)chunk * S, after = first + S, most = (int64_t)p.n - 1;
     const uint32_t before = p.key[min(max(first - 1, (int64_t)0), most)], begin = p.key[min(first, most)],
                    end = p.key[min(after - 1, most)], next = p.key[min(after, most)];
@@ -546,21 +589,21 @@ template <GemmStore OT, int S, int kJoinWaves> __global__ void __launch_bounds__
             n += ask((int64_t)chunk + 1 + n, 1);
         }
     }
-    float acc[8] = {};
+    float acc[COLS] = {};
     // adds parts from .. to - 1 of the run that begins in chunk `at` (0: that chunk's own)
     auto add = [&](int at, int from, int to) __attribute__((always_inline)) {
-        constexpr int B = 8;
+        constexpr int B = 64 / COLS;
         for (int k0 = from; k0 < to; k0 += B) {
-            float v[B][8];
+            float v[B][COLS];
 #pragma unroll
             for (int b = 0; b < B; ++b) {
                 const int k = min(k0 + b, to - 1);
-                load8<GemmStore::F32>(p.part, (2 * (int64_t)(at + k) + (k == 0 ? 1 : 0)) * p.dim + c, nc, false, v[b]);
+                load_part(p.part + (2 * (int64_t)(at + k) + (k == 0 ? 1 : 0)) * p.dim + c, nc, v[b]);
             }
 #pragma unroll
             for (int b = 0; b < B; ++b) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) acc[e] += k0 + b < to ? v[b][e] : 0.f;
+                for (int e = 0; e < COLS; ++e) acc[e] += k0 + b < to ? v[b][e] : 0.f;
             }
         }
     };
@@ -576,17 +619,17 @@ template <GemmStore OT, int S, int kJoinWaves> __global__ void __launch_bounds__
         if (m == 0) continue;
         const int per = (m + kJoinWaves - 1) / kJoinWaves, from = min(wave * per, m), to = min(from + per, m);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+        for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
         if (c < p.dim) add(blockIdx.x * kJoinWaves + w, from, to);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) lds[wave][lane][e] = acc[e];
+        for (int e = 0; e < COLS; ++e) lds[wave][lane][e] = acc[e];
         __syncthreads();
         if (wave == w && c < p.dim) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] = lds[0][lane][e];
+            for (int e = 0; e < COLS; ++e) acc[e] = lds[0][lane][e];
             for (int x = 1; x < kJoinWaves; ++x) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) acc[e] += lds[x][lane][e];
+                for (int e = 0; e < COLS; ++e) acc[e] += lds[x][lane][e];
             }
             put_row<OT>(p, end, c, acc);
         }
@@ -726,6 +769,13 @@ template <GemmStore ST, GemmStore OT> int launch_few(const FewArgs& f, hipStream
     return launch_status();
 }
 
+template <GemmStore OT, int S, int WAVES, int COLS> int launch_join(const SumArgs& p, hipStream_t stream)
+{
+    const dim3 grid((unsigned)ceil_div(p.chunks, WAVES), (unsigned)ceil_div(p.dim, kWave * COLS));
+    hipLaunchKernelGGL((join_runs<OT, S, WAVES, COLS>), grid, dim3(WAVES * kWave), 0, stream, p);
+    return launch_status();
+}
+
 template <GemmStore ST, GemmStore OT, int S> int launch_sums(SumArgs p, hipStream_t stream)
 {
     p.chunks = (int)ceil_div(p.n, S);
@@ -736,23 +786,25 @@ template <GemmStore ST, GemmStore OT, int S> int launch_sums(SumArgs p, hipStrea
     const int st = launch_status();
     if (st != HIMUON_OK || p.chunks < 2) return st;
     // (a block of 16 waves starts later than one of four: 1500 tokens 21.2 us and 18.5)
-    if (p.n <= 2048)
-        hipLaunchKernelGGL((join_runs<OT, S, 4>), dim3((unsigned)ceil_div(p.chunks, 4), (unsigned)p.slabs), dim3(4 * kWave), 0, stream, p);
-    else
-        hipLaunchKernelGGL((join_runs<OT, S, 16>), dim3((unsigned)ceil_div(p.chunks, 16), (unsigned)p.slabs), dim3(16 * kWave), 0, stream,
-                           p);
-    return launch_status();
+    if (p.n <= 2048) return p.dim <= 1024 ? launch_join<OT, S, 4, 4>(p, stream) : launch_join<OT, S, 4, 8>(p, stream);
+    return p.dim <= 1024 && p.n <= 32768 ? launch_join<OT, S, 16, 4>(p, stream) : launch_join<OT, S, 16, 8>(p, stream);
 }
 
 template <GemmStore ST, GemmStore OT> int launch_sums_t(const SumArgs& p, int s, hipStream_t stream)
 {
-    return s == 8 ? launch_sums<ST, OT, 8>(p, stream) : launch_sums<ST, OT, 32>(p, stream);
+    if (s == 8) return launch_sums<ST, OT, 8>(p, stream);
+    return s == 16 ? launch_sums<ST, OT, 16>(p, stream) : launch_sums<ST, OT, 32>(p, stream);
 }
 
-// Entries per chunk: short chunks while long ones would leave much of the chip idle.
-int chunk_size(int64_t n)
+// Entries per chunk: short chunks while long ones would leave much of the chip idle. A wave
+// has a chunk of 512 columns. Measured with 8, 16 and 32, Zipf's tokens (one token throughout):
+// 8192 x 947 35 us (46), 39 (40), 51 (44); 12000 x 947 40 (55), 43 (47), 52 (48); 5000 x 2560 41 (52), 41
+// (43), 44 (41); 8192 x 4096 78 (95), 75 (80), 72 (68); 32768 x 256 33 (76), 33 (53), 36 (42).
+int chunk_size(int64_t n, int64_t dim)
 {
-    return n <= 8192 ? 8 : 32;
+    const int64_t work = n * ceil_div(dim, kSlab);
+    if (n <= 8192 && work <= 16384) return 8;
+    return n <= 16384 && work <= 36864 ? 16 : 32;
 }
 
 int key_bits(int64_t rows)
@@ -791,7 +843,7 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
     // itself: 65536 x 64 into 50000 rows 52 us so and 50 not, 131072 x 64 61 and 67, 4 M x 64
     // 591 and 2507.
     g.scan = g.tiles > 96;
-    g.chunk = chunk_size(n);
+    g.chunk = chunk_size(n, dim);
     if (g.few || n == 0) return g;
     size_t at = 0;
     auto take = [&](size_t bytes) {
