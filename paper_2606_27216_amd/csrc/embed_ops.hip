@@ -441,19 +441,47 @@ struct SumArgs {
     float scale;
 };
 
-template <GemmStore OT> __device__ __forceinline__ void put_row(const SumArgs& p, uint32_t row, int c, float (&v)[8])
+// A lane's eight columns: the last lane's end with the last column, and begin with some of
+// the lane before it, which it sums up as well but does not store. (Of fewer columns than
+// eight loads would be made one by one, and each row's waited for: 32768 x 947 62 us a call, so 50.)
+struct Cols {
+    int first, n;  // fewer than eight only if there are no more
+    int skip;      // leading ones that are not stored: all of a lane past the last column
+};
+
+__device__ __forceinline__ Cols lane_cols(int lane_col, int dim)
 {
-    const int n = min(8, p.dim - c);
-    const int64_t i = (int64_t)row * p.ld_out + c;
+    Cols c;
+    const bool in = lane_col < dim;
+    c.first = in ? min(lane_col, max(dim - 8, 0)) : 0;
+    c.n = min(8, dim - c.first);
+    c.skip = in ? lane_col - c.first : 8;
+    return c;
+}
+
+template <GemmStore OT>
+__device__ __forceinline__ void put_cols(void* out, int64_t i, const Cols& c, bool accumulate, float (&v)[8])
+{
+    if (c.skip == 0) {
+        if (accumulate) {
+            float o[8];
+            load8<OT>(out, i, c.n, false, o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += o[e];
+        }
+        store8<OT>(out, i, c.n, false, v);
+    } else {
+#pragma unroll
+        for (int e = 1; e < 8; ++e)
+            if (e >= c.skip) put1<OT>(out, i + e, accumulate ? v[e] + get1<OT>(out, i + e) : v[e]);
+    }
+}
+
+template <GemmStore OT> __device__ __forceinline__ void put_row(const SumArgs& p, uint32_t row, const Cols& c, float (&v)[8])
+{
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= p.scale;
-    if (p.accumulate) {
-        float o[8];
-        load8<OT>(p.out, i, n, false, o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += o[e];
-    }
-    store8<OT>(p.out, i, n, false, v);
+    put_cols<OT>(p.out, (int64_t)row * p.ld_out + c.first, c, p.accumulate != 0, v);
 }
 
 __device__ __forceinline__ uint32_t lane_value(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
@@ -466,8 +494,7 @@ template <GemmStore ST, GemmStore OT, int S> __global__ void __launch_bounds__(k
     if (unit >= p.units) return;
     const int chunk = (int)(unit / p.slabs);
     const int lane_col = (int)(unit - (int64_t)chunk * p.slabs) * kSlab + lane * 8;
-    const bool col = lane_col < p.dim;  // (lanes past the last column read the first ones and store nothing)
-    const int c = col ? lane_col : 0;
+    const Cols c = lane_cols(lane_col, p.dim);
     // lane l holds entry chunk S - 1 + l: the one before the chunk, its S, the one after
     const int64_t i = (int64_t)chunk * S - 1 + lane;
     const bool there = i >= 0 && i < p.n && lane < S + 2;
@@ -475,7 +502,6 @@ template <GemmStore ST, GemmStore OT, int S> __global__ void __launch_bounds__(k
     const uint32_t pos = there ? p.pos[i] : 0u;
     if (key >= (uint32_t)p.rows) key = kNone;
     const int count = __popcll(__ballot(key != kNone && lane >= 1 && lane <= S));  // sorted: the first ones
-    const int nc = min(8, p.dim - c);
     float acc[8] = {};
     bool begun = count > 0 && lane_value(key, 0) != lane_value(key, 1);  // the current run began in this chunk
     // rows of B entries are in flight while those before them are summed
@@ -484,7 +510,7 @@ template <GemmStore ST, GemmStore OT, int S> __global__ void __launch_bounds__(k
     auto load = [&](Raw8<ST> (&v)[B], int e0) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < B; ++e)
-            v[e] = get_raw8<ST>(p.grad, (int64_t)lane_value(pos, min(e0 + e, count - 1) + 1) * p.ld_grad + c, nc);
+            v[e] = get_raw8<ST>(p.grad, (int64_t)lane_value(pos, min(e0 + e, count - 1) + 1) * p.ld_grad + c.first, c.n);
     };
     if (count == 0) return;
     load(next, 0);
@@ -501,9 +527,9 @@ template <GemmStore ST, GemmStore OT, int S> __global__ void __launch_bounds__(k
 #pragma unroll
             for (int x = 0; x < 8; ++x) acc[x] += raw_value<ST>(cur[e], x);
             if (last || e0 + e + 1 == S) {
-                if (col) {
+                if (c.skip < 8) {
                     if (begun && last) put_row<OT>(p, k, c, acc);
-                    else store8<GemmStore::F32>(p.part, (2 * (int64_t)chunk + (begun ? 1 : 0)) * p.dim + c, nc, false, acc);
+                    else put_cols<GemmStore::F32>(p.part, (2 * (int64_t)chunk + (begun ? 1 : 0)) * p.dim + c.first, c, false, acc);
                 }
 #pragma unroll
                 for (int x = 0; x < 8; ++x) acc[x] = 0.f;
@@ -531,6 +557,11 @@ template <int N> __device__ __forceinline__ void load_part(const float* p, int n
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = w[e];
     }
+}
+
+template <GemmStore OT> __device__ __forceinline__ void put_row(const SumArgs& p, uint32_t row, int c, float (&v)[8])
+{
+    put_row<OT>(p, row, Cols{c, min(8, p.dim - c), 0}, v);
 }
 
 template <GemmStore OT> __device__ __forceinline__ void put_row(const SumArgs& p, uint32_t row, int c, float (&v)[4])
@@ -712,9 +743,7 @@ template <GemmStore ST, GemmStore OT> __global__ void __launch_bounds__(kFewThre
     if (earliest < mine) return;
     const int slabs = (p.dim + kSlab - 1) / kSlab;
     for (int slab = blockIdx.y; slab < slabs; slab += gridDim.y) {
-        const int lane_col = slab * kSlab + lane * 8;
-        const bool col = lane_col < p.dim;  // (lanes past the last column read the first ones and store nothing)
-        const int c = col ? lane_col : 0, nc = min(8, p.dim - c);
+        const Cols c = lane_cols(slab * kSlab + lane * 8, p.dim);
         float acc[8] = {};
 #pragma unroll
         for (int g = 0; g < kFewParts; ++g) {
@@ -731,7 +760,7 @@ template <GemmStore ST, GemmStore OT> __global__ void __launch_bounds__(kFewThre
                         m &= m - 1;
                         ++n;
                     }
-                    v[b] = get_raw8<ST>(p.grad, (int64_t)at * p.ld_grad + c, nc);
+                    v[b] = get_raw8<ST>(p.grad, (int64_t)at * p.ld_grad + c.first, c.n);
                 }
 #pragma unroll
                 for (int b = 0; b < B; ++b) {
@@ -746,7 +775,7 @@ template <GemmStore ST, GemmStore OT> __global__ void __launch_bounds__(kFewThre
             for (int e = 0; e < 8; ++e) part[wave - 1][lane][e] = acc[e];
         }
         __syncthreads();
-        if (wave == 0 && col) {
+        if (wave == 0 && c.skip < 8) {
 #pragma unroll
             for (int w = 0; w < kFewWaves - 1; ++w) {
                 if (seen[w + 1] < p.n) {
