@@ -68,8 +68,11 @@ __global__ void __launch_bounds__(kThreads) act_pack(const void* x, int64_t ld, 
     u32x4* const mine = turn[threadIdx.x >> 6];
     const int64_t tb = unit / slabs;
     const int64_t c0 = (unit - tb * slabs) * (64 * N);
-    const int64_t c = min(c0 + lane * N, cols - 1);  // (lanes past the last column work on it in vain)
-    const int n = (int)min((int64_t)N, cols - c);
+    // The last lane's columns end with the last column, and begin with `skip` of the lane
+    // before it, which it does not store (nor does a lane past the last column any).
+    const int64_t c = min(c0 + lane * N, max(cols - N, (int64_t)0));
+    const int n = (int)min((int64_t)N, cols);
+    const int skip = (int)min(c0 + lane * N - c, (int64_t)N);
     const int64_t t0 = tb * kGroup;
     const int rows = (int)min((int64_t)kGroup, tokens - t0);
     u32x2 raw[kGroup];
@@ -122,12 +125,15 @@ __global__ void __launch_bounds__(kThreads) act_pack(const void* x, int64_t ld, 
                 q[r / 4] = d;
             }
         }
-        // piece h of column j: at 2 N lane + 2 j + h, moved within its lane's pieces so that
-        // the lanes of one access lie in different banks
+        // piece h of the lane's own column j: at 2 N lane + 2 j + h, moved within its lane's
+        // pieces so that the lanes of one access lie in different banks
+        if (j >= skip) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            mine[2 * N * lane + ((2 * j + h) ^ (lane & (2 * N - 1)))] = u32x4{q[4 * h], q[4 * h + 1], q[4 * h + 2], q[4 * h + 3]};
-        if (j < n && c0 + lane * N < cols) exps[tb * cols + c + j] = (uint8_t)code;
+            for (int h = 0; h < 2; ++h)
+                mine[2 * N * lane + ((2 * (j - skip) + h) ^ (lane & (2 * N - 1)))] =
+                    u32x4{q[4 * h], q[4 * h + 1], q[4 * h + 2], q[4 * h + 3]};
+            if (j < n) exps[tb * cols + c + j] = (uint8_t)code;
+        }
     }
     wave_exchange();
     u32x4* const dst = reinterpret_cast<u32x4*>(codes + (tb * cols + c0) * kGroup);

@@ -58,12 +58,13 @@ template <GemmStore ST, int LPR, int U> __global__ void __launch_bounds__(kThrea
     const bool in = t >= 0 && t < p.rows;
     const int64_t src = (in ? t : 0) * p.ld_table, dst = row * p.ld_out;
     const int c0 = seg * (LPR * U * 8) + (lane % LPR) * 8;
+    const int last = max(p.dim - 8, 0);  // (a row's last chunk ends with it, and has columns of the one before it too)
     float v[U][8];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int c = c0 + u * LPR * 8;
         if (c < p.dim && in) {
-            load8<ST>(p.table, src + c, min(8, p.dim - c), false, v[u]);
+            load8<ST>(p.table, src + min(c, last), min(8, p.dim), false, v[u]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[u][e] *= p.scale;
         } else {
@@ -74,7 +75,7 @@ template <GemmStore ST, int LPR, int U> __global__ void __launch_bounds__(kThrea
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int c = c0 + u * LPR * 8;
-        if (c < p.dim) store8<ST>(p.out, dst + c, min(8, p.dim - c), false, v[u]);
+        if (c < p.dim) store8<ST>(p.out, dst + min(c, last), min(8, p.dim), false, v[u]);
     }
 }
 
