@@ -59,9 +59,15 @@ template <int L> __device__ __forceinline__ float head_sum(float v)
     return v;
 }
 
-// The pairs of a head: the rotated ones first, then the others, each kind in runs of eight;
-// the last run of a kind ends with its last pair and repeats pairs of the run before it
-// where their number is no multiple of eight.
+// The pairs of a head: the rotated ones first, then the others, each kind in runs of eight
+// (side by side, INTER, the two kinds in the same runs); the last run of a kind ends with its
+// last pair and repeats pairs of the run before it where their number is no multiple of eight.
+enum class Runs : int {
+    EXACT,  // whole runs of one kind, none of which repeats pairs
+    WHOLE,  // whole runs
+    SHORT   // a kind may have fewer than eight pairs
+};
+
 struct Place {
     int pair;     // the run's first pair
     int n;        // pairs that exist: 8, fewer if there are no eight of the kind, 0 for an idle lane
@@ -86,7 +92,7 @@ template <bool INTER> __device__ __forceinline__ void pair_elements(int pair, in
 
 template <bool INTER> __device__ __forceinline__ Place place(int l, int dim, int rot)
 {
-    const int turned = rot / 2, rest = (dim - rot) / 2, runs = (turned + 7) / 8;
+    const int turned = INTER ? dim / 2 : rot / 2, rest = dim / 2 - turned, runs = (turned + 7) / 8;
     const bool second = l >= runs;
     const int r = second ? l - runs : l, first = second ? turned : 0, count = second ? rest : turned;
     Place w;
@@ -104,15 +110,14 @@ struct Pairs {
     f32x8 u, v;
 };
 
-// The lane's pairs of the vector at base + i. VEC: whole runs (idle lanes read the first
-// one); otherwise runs may be short.
-template <GemmStore ST, bool INTER, bool VEC> __device__ __forceinline__ Pairs load_pairs(const void* base, int64_t i, const Place& w)
+// The lane's pairs of the vector at base + i. (Idle lanes read the first run, if it is whole.)
+template <GemmStore ST, bool INTER, Runs R> __device__ __forceinline__ Pairs load_pairs(const void* base, int64_t i, const Place& w)
 {
     Pairs x;
-    if (VEC || w.n == 8 || w.n == 0) {
+    if (R != Runs::SHORT || w.n == 8 || w.n == 0) {
         if constexpr (INTER) {
             // (a head of fewer than eight pairs has no whole run: its idle lanes read nothing)
-            if (!VEC && w.n == 0) {
+            if (R == Runs::SHORT && w.n == 0) {
                 x.u = x.v = f32x8{};
                 return x;
             }
@@ -120,7 +125,7 @@ template <GemmStore ST, bool INTER, bool VEC> __device__ __forceinline__ Pairs l
             x.u = f32x8{lo[0], lo[2], lo[4], lo[6], hi[0], hi[2], hi[4], hi[6]};
             x.v = f32x8{lo[1], lo[3], lo[5], lo[7], hi[1], hi[3], hi[5], hi[7]};
         } else {
-            if (!VEC && w.n == 0) {
+            if (R == Runs::SHORT && w.n == 0) {
                 x.u = x.v = f32x8{};
                 return x;
             }
@@ -140,11 +145,11 @@ template <GemmStore ST, bool INTER, bool VEC> __device__ __forceinline__ Pairs l
     return x;
 }
 
-template <GemmStore ST, bool INTER, bool VEC>
+template <GemmStore ST, bool INTER, Runs R>
 __device__ __forceinline__ void store_pairs(void* base, int64_t i, const Place& w, const Pairs& x)
 {
     if (w.n == 0) return;
-    if (VEC || w.n == 8) {
+    if (R != Runs::SHORT || w.n == 8) {
         if constexpr (INTER) {
             put8<ST>(base, i + w.a, f32x8{x.u[0], x.v[0], x.u[1], x.v[1], x.u[2], x.v[2], x.u[3], x.v[3]});
             put8<ST>(base, i + w.a + 8, f32x8{x.u[4], x.v[4], x.u[5], x.v[5], x.u[6], x.v[6], x.u[7], x.v[7]});
@@ -164,34 +169,35 @@ __device__ __forceinline__ void store_pairs(void* base, int64_t i, const Place& 
     }
 }
 
-// Whether pair e of the lane counts in sums over the head. (VEC: all of a lane's do, or none.)
-template <bool VEC> __device__ __forceinline__ bool counts(const Place& w, int e)
+// Whether pair e of the lane counts in sums over the head. (EXACT: all of a lane's do, or none.)
+template <Runs R> __device__ __forceinline__ bool counts(const Place& w, int e)
 {
-    return VEC ? w.n > 0 : e >= w.skip && e < w.n;
+    return R == Runs::EXACT ? w.n > 0 : e >= w.skip && e < w.n;
 }
 
-template <bool INTER, bool VEC> __device__ __forceinline__ Pairs load_gains(const QkArgs& p, const void* gain, const Place& w)
+template <bool INTER, Runs R> __device__ __forceinline__ Pairs load_gains(const QkArgs& p, const void* gain, const Place& w)
 {
-    if (p.gain_bf16) return load_pairs<GemmStore::BF16, INTER, VEC>(gain, 0, w);
-    return load_pairs<GemmStore::F32, INTER, VEC>(gain, 0, w);
+    if (p.gain_bf16) return load_pairs<GemmStore::BF16, INTER, R>(gain, 0, w);
+    return load_pairs<GemmStore::F32, INTER, R>(gain, 0, w);
 }
 
 // The lane's cosines (u) and sines (v) of position t: 1 and 0 for what is not rotated.
-template <bool VEC> __device__ __forceinline__ Pairs load_turn(const QkArgs& p, int64_t t, const Place& w, bool used = true)
+template <bool INTER, Runs R> __device__ __forceinline__ Pairs load_turn(const QkArgs& p, int64_t t, const Place& w, bool used = true)
 {
     const int half = p.rot / 2;
     const int64_t i = t * half + w.pair;
     Pairs x;
     x.u = f32x8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
     x.v = f32x8{};
-    if (w.pair >= half || !used) return x;  // (a run lies in one part)
-    if (VEC || w.n == 8) {
+    if (w.pair >= half || !used) return x;
+    constexpr bool CUT = R == Runs::SHORT || (INTER && R == Runs::WHOLE);  // (a run that is not all rotated)
+    if (!CUT || w.pair + 8 <= half) {
         x.u = get8<GemmStore::F32>(p.cs, i);
         x.v = get8<GemmStore::F32>(p.sn, i);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if (e < w.n) {
+            if (w.pair + e < half) {
                 x.u[e] = p.cs[i + e];
                 x.v[e] = p.sn[i + e];
             }
@@ -210,12 +216,12 @@ __device__ __forceinline__ bool token_position(const QkArgs& p, int64_t token, i
 }
 
 // x -> R (r x w), the head's sum over L lanes.
-template <bool VEC, int L>
+template <Runs R, int L>
 __device__ __forceinline__ void forward_head(const QkArgs& p, const Place& w, const Pairs& g, const Pairs& turn, bool used, Pairs& x)
 {
     float sq = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sq += counts<VEC>(w, e) ? x.u[e] * x.u[e] + x.v[e] * x.v[e] : 0.f;
+    for (int e = 0; e < 8; ++e) sq += counts<R>(w, e) ? x.u[e] * x.u[e] + x.v[e] * x.v[e] : 0.f;
     const float r = rsqrtf(head_sum<L>(sq) * p.inv_dim + p.eps);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -226,7 +232,7 @@ __device__ __forceinline__ void forward_head(const QkArgs& p, const Place& w, co
 }
 
 // x, y = dL/d(output) -> x = dL/dx, d += the gain's terms.
-template <bool VEC, int L>
+template <Runs R, int L>
 __device__ __forceinline__ void backward_head(const QkArgs& p, const Place& w, const Pairs& g, const Pairs& turn, bool used, Pairs& x,
                                               Pairs& y, Pairs& d)
 {
@@ -236,8 +242,8 @@ __device__ __forceinline__ void backward_head(const QkArgs& p, const Place& w, c
         const float a = y.u[e] * turn.u[e] + y.v[e] * turn.v[e], c = y.v[e] * turn.u[e] - y.u[e] * turn.v[e];
         y.u[e] = a;  // dz
         y.v[e] = c;
-        sq += counts<VEC>(w, e) ? x.u[e] * x.u[e] + x.v[e] * x.v[e] : 0.f;
-        dot += counts<VEC>(w, e) ? a * g.u[e] * x.u[e] + c * g.v[e] * x.v[e] : 0.f;
+        sq += counts<R>(w, e) ? x.u[e] * x.u[e] + x.v[e] * x.v[e] : 0.f;
+        dot += counts<R>(w, e) ? a * g.u[e] * x.u[e] + c * g.v[e] * x.v[e] : 0.f;
     }
     sq = head_sum<L>(sq);
     dot = head_sum<L>(dot);
@@ -254,22 +260,22 @@ __device__ __forceinline__ void backward_head(const QkArgs& p, const Place& w, c
 
 // ------------------------------------------------------- many heads: a wave, one token
 
-template <GemmStore ST, bool INTER, bool VEC, int L>
+template <GemmStore ST, bool INTER, Runs R, int L>
 __device__ __forceinline__ void forward_heads(const QkArgs& p, const Strided& in, const Strided& out, const void* gain, int heads,
                                               int part, int64_t b, int64_t s, bool used, const Place& w, const Pairs& turn)
 {
     constexpr int G = 64 / L;
     const int lane = threadIdx.x & 63;
-    const Pairs g = load_gains<INTER, VEC>(p, gain, w);
+    const Pairs g = load_gains<INTER, R>(p, gain, w);
     const int64_t bi = b * in.sb + s * in.ss, bo = b * out.sb + s * out.ss;
     for (int h = part * G + lane / L; h < heads; h += p.parts * G) {
-        Pairs x = load_pairs<ST, INTER, VEC>(in.ptr, bi + h * in.sh, w);
-        forward_head<VEC, L>(p, w, g, turn, used, x);
-        store_pairs<ST, INTER, VEC>(out.ptr, bo + h * out.sh, w, x);
+        Pairs x = load_pairs<ST, INTER, R>(in.ptr, bi + h * in.sh, w);
+        forward_head<R, L>(p, w, g, turn, used, x);
+        store_pairs<ST, INTER, R>(out.ptr, bo + h * out.sh, w, x);
     }
 }
 
-template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bounds__(kThreads) qk_forward(const QkArgs p)
+template <GemmStore ST, bool INTER, Runs R, int L> __global__ void __launch_bounds__(kThreads) qk_forward(const QkArgs p)
 {
     const int64_t unit = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (unit >= p.units) return;
@@ -280,12 +286,12 @@ template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bo
     int64_t t;
     const bool used = token_position(p, token, s, t);
     Pairs turn{};
-    if (used) turn = load_turn<VEC>(p, t, w);
-    forward_heads<ST, INTER, VEC, L>(p, p.q, p.qo, p.wq, p.hq, part, b, s, used, w, turn);
-    forward_heads<ST, INTER, VEC, L>(p, p.k, p.ko, p.wk, p.hk, part, b, s, used, w, turn);
+    if (used) turn = load_turn<INTER, R>(p, t, w);
+    forward_heads<ST, INTER, R, L>(p, p.q, p.qo, p.wq, p.hq, part, b, s, used, w, turn);
+    forward_heads<ST, INTER, R, L>(p, p.k, p.ko, p.wk, p.hk, part, b, s, used, w, turn);
 }
 
-template <GemmStore ST, bool INTER, bool VEC, int L>
+template <GemmStore ST, bool INTER, Runs R, int L>
 __device__ __forceinline__ void backward_heads(const QkArgs& p, const Strided& in, const Strided& grad, const Strided& out,
                                                const Pairs& g, int heads, int64_t b, int64_t s, bool used, const Place& w,
                                                const Pairs& turn, Pairs& d)
@@ -294,10 +300,10 @@ __device__ __forceinline__ void backward_heads(const QkArgs& p, const Strided& i
     const int lane = threadIdx.x & 63;
     const int64_t bi = b * in.sb + s * in.ss, bg = b * grad.sb + s * grad.ss, bo = b * out.sb + s * out.ss;
     for (int h = lane / L; h < heads; h += G) {
-        Pairs x = load_pairs<ST, INTER, VEC>(in.ptr, bi + h * in.sh, w);
-        Pairs y = load_pairs<ST, INTER, VEC>(grad.ptr, bg + h * grad.sh, w);
-        backward_head<VEC, L>(p, w, g, turn, used, x, y, d);
-        store_pairs<ST, INTER, VEC>(out.ptr, bo + h * out.sh, w, x);
+        Pairs x = load_pairs<ST, INTER, R>(in.ptr, bi + h * in.sh, w);
+        Pairs y = load_pairs<ST, INTER, R>(grad.ptr, bg + h * grad.sh, w);
+        backward_head<R, L>(p, w, g, turn, used, x, y, d);
+        store_pairs<ST, INTER, R>(out.ptr, bo + h * out.sh, w, x);
     }
 }
 
@@ -312,7 +318,7 @@ template <bool INTER> __device__ __forceinline__ void put_gain(const QkArgs& p, 
 // Blocks (.., 0) have the queries, (.., 1) the keys: one gain and one set of sums in
 // registers. A wave takes tokens `units` apart; its sums stay in registers until the
 // end, when the block adds its own up in LDS and leaves a row of partial sums.
-template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bounds__(kThreads) qk_backward(const QkArgs p)
+template <GemmStore ST, bool INTER, Runs R, int L> __global__ void __launch_bounds__(kThreads) qk_backward(const QkArgs p)
 {
     __shared__ float sums[kWaves][L * 16];
     const int lane = threadIdx.x & 63;
@@ -321,14 +327,14 @@ template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bo
     const Place w = place<INTER>(threadIdx.x & (L - 1), p.dim, p.rot);
     const Strided in = key ? p.k : p.q, grad = key ? p.gk : p.gq, out = key ? p.ko : p.qo;
     const int heads = key ? p.hk : p.hq;
-    const Pairs g = load_gains<INTER, VEC>(p, key ? p.wk : p.wq, w);
+    const Pairs g = load_gains<INTER, R>(p, key ? p.wk : p.wq, w);
     Pairs d{};
     for (int64_t token = (int64_t)blockIdx.x * kWaves + wave; token < p.tokens; token += p.units) {
         const int64_t b = token / p.seq, s = token - b * p.seq;
         int64_t t;
         const bool used = token_position(p, token, s, t);
-        const Pairs turn = load_turn<VEC>(p, t, w, used);
-        backward_heads<ST, INTER, VEC, L>(p, in, grad, out, g, heads, b, s, used, w, turn, d);
+        const Pairs turn = load_turn<INTER, R>(p, t, w, used);
+        backward_heads<ST, INTER, R, L>(p, in, grad, out, g, heads, b, s, used, w, turn, d);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -338,7 +344,7 @@ template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bo
             u += __shfl_xor(u, o);
             v += __shfl_xor(v, o);
         }
-        if (lane < L && counts<VEC>(w, e)) {
+        if (lane < L && counts<R>(w, e)) {
             sums[wave][2 * (w.pair + e)] = u;
             sums[wave][2 * (w.pair + e) + 1] = v;
         }
@@ -366,7 +372,7 @@ __device__ __forceinline__ int token_of(const QkArgs& p, int64_t first, int in_w
     return (int)t;
 }
 
-template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bounds__(kThreads) qk_forward_few(const QkArgs p)
+template <GemmStore ST, bool INTER, Runs R, int L> __global__ void __launch_bounds__(kThreads) qk_forward_few(const QkArgs p)
 {
     const int lane = threadIdx.x & 63, group = lane / L, slot = group & (p.slots - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -374,7 +380,7 @@ template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bo
     const Place w = place<INTER>(threadIdx.x & (L - 1), p.dim, p.rot);
     const bool head = slot < p.hq + p.hk, key = head && slot >= p.hq;
     const int h = !head ? 0 : key ? slot - p.hq : slot;
-    const Pairs g = load_gains<INTER, VEC>(p, key ? p.wk : p.wq, w);
+    const Pairs g = load_gains<INTER, R>(p, key ? p.wk : p.wq, w);
     uint8_t* const src = key ? p.k.ptr : p.q.ptr;
     uint8_t* const dst = key ? p.ko.ptr : p.qo.ptr;
     const int64_t ib = key ? p.k.sb : p.q.sb, is = key ? p.k.ss : p.q.ss, i0 = h * (key ? p.k.sh : p.q.sh);
@@ -384,14 +390,14 @@ template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bo
         int64_t b, s, t;
         const int token = token_of(p, first, group / p.slots, live, b, s);
         const bool used = token_position(p, token, s, t);
-        Pairs x = load_pairs<ST, INTER, VEC>(src, b * ib + s * is + i0, w);
-        const Pairs turn = load_turn<VEC>(p, t, w, used);
-        forward_head<VEC, L>(p, w, g, turn, used, x);
-        if (live && head) store_pairs<ST, INTER, VEC>(dst, b * ob + s * os + o0, w, x);
+        Pairs x = load_pairs<ST, INTER, R>(src, b * ib + s * is + i0, w);
+        const Pairs turn = load_turn<INTER, R>(p, t, w, used);
+        forward_head<R, L>(p, w, g, turn, used, x);
+        if (live && head) store_pairs<ST, INTER, R>(dst, b * ob + s * os + o0, w, x);
     }
 }
 
-template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bounds__(kThreads) qk_backward_few(const QkArgs p)
+template <GemmStore ST, bool INTER, Runs R, int L> __global__ void __launch_bounds__(kThreads) qk_backward_few(const QkArgs p)
 {
     constexpr int G = 64 / L;
     __shared__ float sums[kWaves * G][L * 16 + 1];
@@ -401,7 +407,7 @@ template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bo
     const Place w = place<INTER>(threadIdx.x & (L - 1), p.dim, p.rot);
     const bool head = slot < p.hq + p.hk, key = head && slot >= p.hq;
     const int h = !head ? 0 : key ? slot - p.hq : slot;
-    const Pairs g = load_gains<INTER, VEC>(p, key ? p.wk : p.wq, w);
+    const Pairs g = load_gains<INTER, R>(p, key ? p.wk : p.wq, w);
     uint8_t* const src = key ? p.k.ptr : p.q.ptr;
     uint8_t* const ups = key ? p.gk.ptr : p.gq.ptr;
     uint8_t* const dst = key ? p.ko.ptr : p.qo.ptr;
@@ -414,15 +420,15 @@ template <GemmStore ST, bool INTER, bool VEC, int L> __global__ void __launch_bo
         int64_t b, s, t;
         const int token = token_of(p, first, group / p.slots, live, b, s);
         const bool used = token_position(p, token, s, t) && live && head;
-        Pairs x = load_pairs<ST, INTER, VEC>(src, b * ib + s * is + i0, w);
-        Pairs y = load_pairs<ST, INTER, VEC>(ups, b * gb + s * gs + g0, w);
-        const Pairs turn = load_turn<VEC>(p, t, w, used);
-        backward_head<VEC, L>(p, w, g, turn, used, x, y, d);
-        if (live && head) store_pairs<ST, INTER, VEC>(dst, b * ob + s * os + o0, w, x);
+        Pairs x = load_pairs<ST, INTER, R>(src, b * ib + s * is + i0, w);
+        Pairs y = load_pairs<ST, INTER, R>(ups, b * gb + s * gs + g0, w);
+        const Pairs turn = load_turn<INTER, R>(p, t, w, used);
+        backward_head<R, L>(p, w, g, turn, used, x, y, d);
+        if (live && head) store_pairs<ST, INTER, R>(dst, b * ob + s * os + o0, w, x);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        if (counts<VEC>(w, e)) {
+        if (counts<R>(w, e)) {
             sums[wave * G + group][2 * (w.pair + e)] = d.u[e];
             sums[wave * G + group][2 * (w.pair + e) + 1] = d.v[e];
         }
@@ -476,7 +482,7 @@ template <GemmStore GT> __global__ void __launch_bounds__(kSumThreads) gain_sums
 // Blocks of the backward pass, and rows of partial sums.
 int64_t grad_blocks(int64_t tokens) { return std::max<int64_t>(1, std::min<int64_t>(ceil_div(tokens, kWaves), 1024)); }
 
-template <bool BWD, GemmStore ST, bool INTER, bool VEC, int L> int launch_l(QkArgs p, hipStream_t stream)
+template <bool BWD, GemmStore ST, bool INTER, Runs R, int L> int launch_l(QkArgs p, hipStream_t stream)
 {
     constexpr int G = 64 / L;
     if constexpr (L <= 16) {
@@ -487,16 +493,16 @@ template <bool BWD, GemmStore ST, bool INTER, bool VEC, int L> int launch_l(QkAr
             const int64_t blocks = BWD ? grad_blocks(p.tokens) : std::min<int64_t>(ceil_div(p.tokens * p.slots, G * kWaves), 4096);
             p.units = blocks * kWaves;
             if constexpr (BWD)
-                hipLaunchKernelGGL((qk_backward_few<ST, INTER, VEC, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
+                hipLaunchKernelGGL((qk_backward_few<ST, INTER, R, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
             else
-                hipLaunchKernelGGL((qk_forward_few<ST, INTER, VEC, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
+                hipLaunchKernelGGL((qk_forward_few<ST, INTER, R, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
             return launch_status();
         }
     }
     if constexpr (BWD) {
         const int64_t blocks = grad_blocks(p.tokens);
         p.units = blocks * kWaves;
-        hipLaunchKernelGGL((qk_backward<ST, INTER, VEC, L>), dim3((unsigned)blocks, 2), dim3(kThreads), 0, stream, p);
+        hipLaunchKernelGGL((qk_backward<ST, INTER, R, L>), dim3((unsigned)blocks, 2), dim3(kThreads), 0, stream, p);
     } else {
         // few tokens: a token's heads are shared out over several waves
         const int64_t groups = ceil_div(std::max(p.hq, p.hk), G);
@@ -504,36 +510,40 @@ template <bool BWD, GemmStore ST, bool INTER, bool VEC, int L> int launch_l(QkAr
         p.units = p.tokens * p.parts;
         const int64_t blocks = ceil_div(p.units, kWaves);
         if (!launchable(blocks, kThreads)) return HIMUON_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL((qk_forward<ST, INTER, VEC, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
+        hipLaunchKernelGGL((qk_forward<ST, INTER, R, L>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
     }
     return launch_status();
 }
 
-template <bool BWD, GemmStore ST, bool INTER, bool VEC> int launch_vec(const QkArgs& p, hipStream_t stream)
+template <bool BWD, GemmStore ST, bool INTER, Runs R> int launch_runs(const QkArgs& p, int lanes, hipStream_t stream)
 {
-    // lanes to a head: one for each run of eight pairs
-    const int lanes = (int)(ceil_div(p.rot / 2, 8) + ceil_div((p.dim - p.rot) / 2, 8));
-    if (lanes <= 4) return launch_l<BWD, ST, INTER, VEC, 4>(p, stream);
-    if (lanes <= 8) return launch_l<BWD, ST, INTER, VEC, 8>(p, stream);
-    if (lanes <= 16) return launch_l<BWD, ST, INTER, VEC, 16>(p, stream);
-    if (lanes <= 32) return launch_l<BWD, ST, INTER, VEC, 32>(p, stream);
-    if constexpr (!VEC) return launch_l<BWD, ST, INTER, VEC, 64>(p, stream);
+    if (lanes <= 4) return launch_l<BWD, ST, INTER, R, 4>(p, stream);
+    if (lanes <= 8) return launch_l<BWD, ST, INTER, R, 8>(p, stream);
+    if (lanes <= 16) return launch_l<BWD, ST, INTER, R, 16>(p, stream);
+    if (lanes <= 32) return launch_l<BWD, ST, INTER, R, 32>(p, stream);
+    // (32 runs hold the largest head unless both kinds have a cut one)
+    if constexpr (!INTER && R != Runs::EXACT) return launch_l<BWD, ST, INTER, R, 64>(p, stream);
     return HIMUON_ERR_UNSUPPORTED;
 }
 
-template <bool BWD, GemmStore ST> int launch_st(const QkArgs& p, bool inter, hipStream_t stream)
+// 7 x 182 tokens, 48 + 8 heads of 256 bf16, backward: EXACT 26 us, WHOLE (148 elements rotated,
+// 17 lanes of 32 in use) 40, SHORT for the same 51.
+template <bool BWD, GemmStore ST, bool INTER> int launch_st(const QkArgs& p, hipStream_t stream)
 {
-    // whole runs, none of which repeats pairs (VEC)
-    const bool vec = p.dim % 16 == 0 && p.rot % 16 == 0;
-    if (inter) return vec ? launch_vec<BWD, ST, true, true>(p, stream) : launch_vec<BWD, ST, true, false>(p, stream);
-    return vec ? launch_vec<BWD, ST, false, true>(p, stream) : launch_vec<BWD, ST, false, false>(p, stream);
+    const int turned = INTER ? p.dim / 2 : p.rot / 2, rest = p.dim / 2 - turned;
+    // lanes to a head: one for each run of eight pairs
+    const int lanes = (int)(ceil_div(turned, 8) + ceil_div(rest, 8));
+    if (p.dim % 16 == 0 && p.rot % 16 == 0) return launch_runs<BWD, ST, INTER, Runs::EXACT>(p, lanes, stream);
+    if ((turned == 0 || turned >= 8) && (rest == 0 || rest >= 8)) return launch_runs<BWD, ST, INTER, Runs::WHOLE>(p, lanes, stream);
+    if constexpr (INTER) return launch_l<BWD, ST, INTER, Runs::SHORT, 4>(p, stream);  // (a head of fewer than eight pairs)
+    else return launch_runs<BWD, ST, INTER, Runs::SHORT>(p, lanes, stream);
 }
 
 template <bool BWD> int launch_qk(const QkArgs& p, const himuon_qk_t* a, hipStream_t stream)
 {
-    const bool inter = a->interleaved != 0;
-    return a->dtype == HIMUON_BF16 ? launch_st<BWD, GemmStore::BF16>(p, inter, stream)
-                                   : launch_st<BWD, GemmStore::F32>(p, inter, stream);
+    if (a->dtype == HIMUON_BF16)
+        return a->interleaved ? launch_st<BWD, GemmStore::BF16, true>(p, stream) : launch_st<BWD, GemmStore::BF16, false>(p, stream);
+    return a->interleaved ? launch_st<BWD, GemmStore::F32, true>(p, stream) : launch_st<BWD, GemmStore::F32, false>(p, stream);
 }
 
 int check_args(const himuon_qk_t* a)
