@@ -60,10 +60,10 @@ _device = _raw_stream = None
 def _torch():
     global _device, _raw_stream
     import torch
-    if not _INDEX:
+    if not _INDEX:  # (filled last: another thread that finds it filled finds all of this)
+        _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         _TYPES.update({torch.float32: F32, torch.bfloat16: BF16})
         _INDEX.update({torch.int32: I32, torch.int64: I64})
-        _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     return torch
 
 
