@@ -492,7 +492,8 @@ int himuon_select_compute(int dtype, int compute, int K, float a, float b, float
  * Leading dimensions and strides count elements. Empty batches (no token) are
  * valid. Sizes that a kernel's indexes or a launch cannot hold are
  * HIMUON_ERR_UNSUPPORTED: 2^31 rows, columns or tokens (2^30 tokens of a table's
- * gradient, 2^29 of an activation, 2^26 columns), 2^32 threads.
+ * gradient, 2^29 of an activation, 2^26 columns), more than 2^30 heads of queries
+ * and keys together, 2^32 threads.
  */
 
 /* Integer type of token and position arrays. */

@@ -27,6 +27,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
+constexpr int64_t kMostHeads = INT64_C(1) << 30;  // queries' and keys' (the kernels count them in 32 bits, 65536 ahead)
 
 struct Strided {
     uint8_t* ptr;
@@ -557,7 +558,7 @@ int check_args(const himuon_qk_t* a)
     if (a->rot_dim > 0 && a->table_rows > 0 && (!a->cos_table || !a->sin_table)) return HIMUON_ERR_INVALID_ARG;
     if (a->head_dim > HIMUON_MAX_HEAD_DIM) return HIMUON_ERR_UNSUPPORTED;
     if (a->batch > INT32_MAX || a->seq > INT32_MAX || a->table_rows > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
-    if (a->batch * a->seq > INT32_MAX) return HIMUON_ERR_UNSUPPORTED;
+    if (a->batch * a->seq > INT32_MAX || (int64_t)a->q_heads + a->k_heads > kMostHeads) return HIMUON_ERR_UNSUPPORTED;
     return HIMUON_OK;
 }
 
