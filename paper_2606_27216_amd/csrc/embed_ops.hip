@@ -811,7 +811,6 @@ template <GemmStore ST, GemmStore OT, int S> int launch_sums(SumArgs p, hipStrea
     p.chunks = (int)ceil_div(p.n, S);
     p.units = (int64_t)p.chunks * p.slabs;
     const int64_t blocks = ceil_div(p.units, kThreads / kWave);
-    if (!launchable(blocks, kThreads) || p.slabs > 65535) return HIMUON_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((sum_runs<ST, OT, S>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
     const int st = launch_status();
     if (st != HIMUON_OK || p.chunks < 2) return st;
@@ -837,6 +836,18 @@ int chunk_size(int64_t n, int64_t dim)
     return n <= 16384 && work <= 36864 ? 16 : 32;
 }
 
+// Whether the sums of a sorted batch are launches that can be made.
+bool sums_launchable(int64_t n, int64_t dim)
+{
+    const int64_t slabs = ceil_div(dim, kSlab), units = ceil_div(n, chunk_size(n, dim)) * slabs;
+    return slabs <= 65535 && launchable(ceil_div(units, kThreads / kWave), kThreads);
+}
+
+// Short batches are not sorted. One launch against the sort's three: 100 tokens into 32000 x 256
+// 10.0 us and 16.9, 600 into 5003 x 1000 10.1 and 17.2; but 600 into 32000 x 4096 49 and 44, 1500 of
+// one token 35 and 22.
+bool few_tokens(int64_t n, int64_t dim) { return n > 0 && n <= (dim <= 2 * kSlab ? kFewMost : kFewMost / 2); }
+
 int key_bits(int64_t rows)
 {
     int b = 1;
@@ -860,9 +871,7 @@ GradPlan plan_grad(int64_t n, int64_t rows, int64_t dim)
     const int kb = key_bits(rows);
     g.digits = (kb + 9) / 10;
     g.bits = std::max(2, (kb + g.digits - 1) / g.digits);  // (bins in groups of four)
-    // One launch against the sort's three: 100 tokens into 32000 x 256 10.0 us and 16.9, 600 into
-    // 5003 x 1000 10.1 and 17.2; but 600 into 32000 x 4096 49 and 44, 1500 of one token 35 and 22.
-    g.few = n > 0 && n <= (dim <= 2 * kSlab ? kFewMost : kFewMost / 2);
+    g.few = few_tokens(n, dim);
     g.tiles = (int)ceil_div(n, kTile);
     // One launch, two, or two to three for each digit. Measured, x 64 into 50000 rows: 4096
     // tokens RANK 23.3 us, MERGE 20.5; 6144 29.1 and 22.3; MERGE and RADIX: 16384 30 and 40, 32768 37
@@ -895,6 +904,7 @@ int embed_grad_sizes(int64_t n, int64_t rows, int64_t dim)
 {
     if (n < 0 || rows < 1 || dim < 1) return HIMUON_ERR_INVALID_ARG;
     if (n > INT32_MAX / 2 || rows >= INT32_MAX || dim > INT32_MAX - 1024) return HIMUON_ERR_UNSUPPORTED;
+    if (n > 0 && !few_tokens(n, dim) && !sums_launchable(n, dim)) return HIMUON_ERR_UNSUPPORTED;
     return HIMUON_OK;
 }
 
