@@ -832,6 +832,13 @@ WgradPlan plan_wgrad(int64_t tokens, int64_t out, int64_t cols, const void* grad
     return g;
 }
 
+// Whether the plan's workgroups are a launch that can be made.
+bool tiles_launchable(const WgradPlan& g, int64_t out, int64_t cols)
+{
+    const int64_t edge = g.tile == Tile::DIRECT ? 64 : g.tile == Tile::B256 ? 256 : 128;
+    return launchable(ceil_div(out, edge) * ceil_div(cols, edge) * g.splits, g.tile == Tile::B128 ? 256 : 512);
+}
+
 template <GemmStore OT> int join_splits(const WgradArgs& p, hipStream_t stream)
 {
     const int st = launch_status();
@@ -846,7 +853,7 @@ template <GemmStore OT, int BM, int BN, int WGM, int WGN, int KG, int NS, int MI
     p.ti = (int32_t)ceil_div(p.rows, BM);
     p.tj = (int32_t)ceil_div(p.cols, BN);
     const int64_t total = (int64_t)p.ti * p.tj * p.splits;
-    if (!launchable(total, 64 * WGM * WGN * KG)) return HIMUON_ERR_UNSUPPORTED;
+    static_assert(64 * WGM * WGN * KG == (BM == 128 && KG == 1 ? 256 : 512), "tiles_launchable's threads");
     hipLaunchKernelGGL((wgrad_blocks<OT, BM, BN, WGM, WGN, KG, NS, MINW>), dim3((unsigned)total), dim3(64 * WGM * WGN * KG), 0,
                        stream, p);
     return join_splits<OT>(p, stream);
@@ -928,7 +935,8 @@ extern "C" size_t himuon_weight_grad_workspace_size(int64_t n_tokens, int64_t ou
 {
     using namespace himuon;
     if (wgrad_sizes(n_tokens, out, cols) != HIMUON_OK || !known_dtype(dtype) || ld_grad < out) return 0;
-    return plan_wgrad(n_tokens, out, cols, grad, ld_grad, dtype).total;
+    const WgradPlan g = plan_wgrad(n_tokens, out, cols, grad, ld_grad, dtype);
+    return tiles_launchable(g, out, cols) ? g.total : 0;
 }
 
 extern "C" int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, const void* grad, int64_t ld_grad, int dtype,
@@ -941,7 +949,8 @@ extern "C" int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, c
     if (!known_dtype(dtype) || !known_dtype(out_dtype) || ld_grad < out || ld_dweight < cols) return HIMUON_ERR_INVALID_ARG;
     if (!small_product(n_tokens, ld_grad) || !small_product(out, ld_dweight)) return HIMUON_ERR_INVALID_ARG;
     if (!dweight || (n_tokens && (!grad || !codes || !exponents || ((uintptr_t)codes & 15)))) return HIMUON_ERR_INVALID_ARG;
-    WgradPlan g = plan_wgrad(n_tokens, out, cols, grad, ld_grad, dtype);
+    const WgradPlan g = plan_wgrad(n_tokens, out, cols, grad, ld_grad, dtype);
+    if (!tiles_launchable(g, out, cols)) return HIMUON_ERR_UNSUPPORTED;
     if (g.total > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < g.total)) return HIMUON_ERR_WORKSPACE;
     if (n_tokens == 0 && accumulate) return HIMUON_OK;
     StreamDevice on(stream);

@@ -1,7 +1,7 @@
 """Sizes that a launch or a kernel's indexes cannot hold: refused before anything is
 enqueued. (No call may follow a pointer here, nor reach a device.)"""
 import pytest
-from test_train_ops_cpu import GRAD, HEADS, P, _call, _qk
+from test_train_ops_cpu import GRAD, HEADS, P, WGRAD, _call, _qk
 
 import paper_2606_27216_amd as hm
 
@@ -24,3 +24,13 @@ def test_sums_of_a_tables_gradient(n, dim):
     assert _call("embed_grad", GRAD, n=n, dim=dim, ld_grad=dim, ld_out=dim, ws_bytes=1 << 60) == hm.ERR_UNSUPPORTED
     assert L.himuon_embed_grad_workspace_size(n, 10, dim) == 0
     assert L.himuon_embed_grad_workspace_size(600, 10, 65535 * 512) > 0
+
+
+@pytest.mark.parametrize("dtype", [hm.F32, hm.BF16])
+@pytest.mark.parametrize("n", [0, 64, 100000])
+def test_tiles_of_a_weight_gradient(n, dtype):
+    """More tiles than a launch holds: known before the gradient is laid out."""
+    rows, cols = (1 << 26) - 8192, (1 << 26) - 8191
+    assert _call("weight_grad", WGRAD, n=n, out=rows, cols=cols, ld_grad=rows, ld_dw=cols, dtype=dtype,
+                 ws_bytes=1 << 60) == hm.ERR_UNSUPPORTED
+    assert hm.lib().himuon_weight_grad_workspace_size(n, rows, cols, P, rows, dtype) == 0
