@@ -141,8 +141,8 @@ def _workspace(need, given, like):
         torch = _torch()
         given = torch.empty(need, dtype=torch.uint8, device=like.device)
         return given, given.data_ptr(), need
-    if given.device != like.device:
-        raise ValueError("the workspace must be on the tensors' device")
+    if given.device != like.device or not given.is_contiguous():  # (its bytes are counted by its elements)
+        raise ValueError("the workspace must be a contiguous tensor on the tensors' device")
     return given, given.data_ptr(), given.numel() * given.element_size()
 
 
