@@ -6,8 +6,8 @@ Tokens are looked up in a scaled table (``embed``); queries and keys are normali
 head and rotated (``qk_norm_rope``); every projection keeps its input in 8 bits for the
 backward pass (``act_pack``) and forms its weight gradient from it (``weight_grad``) in the
 buffer that ``HiMuon`` steps on; the table's gradient comes from the sorted tokens
-(``embed_grad``). The operators join autograd through the three functions below; attention
-itself, the loss and the residual's norms are torch's.
+(``embed_grad``). Lookup and norms join autograd by themselves, the projections through the
+function below; attention itself, the loss and the residual's norms are torch's.
 
 The task: every token has one successor, and a sequence walks from a random one on.
 """
@@ -26,30 +26,6 @@ import paper_2606_27216_amd as hm
 VOCAB, WIDTH, HEADS, KV_HEADS, HEAD, HIDDEN = 1000, 256, 8, 4, 64, 1024
 BATCH, SEQ = 16, 128
 EPS = 1e-6
-
-
-class Embed(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, tokens, table, scale):
-        ctx.save_for_backward(tokens)
-        ctx.rows, ctx.scale = table.shape[0], scale
-        return hm.embed(tokens, table, scale=scale)
-
-    @staticmethod
-    def backward(ctx, g):
-        (tokens,) = ctx.saved_tensors
-        return None, hm.embed_grad(tokens, g.contiguous(), ctx.rows, scale=ctx.scale), None
-
-
-class QkNormRope(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, q, k, q_gain, k_gain, cos, sin):
-        ctx.save_for_backward(q, k, q_gain, k_gain, cos, sin)
-        return hm.qk_norm_rope(q, k, q_gain, k_gain, cos, sin, eps=EPS)
-
-    @staticmethod
-    def backward(ctx, gq, gk):
-        return (*hm.qk_norm_rope_grad(gq, gk, *ctx.saved_tensors, eps=EPS), None, None)
 
 
 class Linear8(torch.autograd.Function):
@@ -91,10 +67,10 @@ class Block:
         return Linear8.apply(x, self.weights[name], self.grads[name])
 
     def embed(self, tokens):
-        return Embed.apply(tokens, self.table, math.sqrt(WIDTH))
+        return hm.embed(tokens, self.table, scale=math.sqrt(WIDTH))
 
     def norm_rope(self, q, k):
-        return QkNormRope.apply(q, k, *self.gains, self.cos, self.sin)
+        return hm.qk_norm_rope(q, k, *self.gains, self.cos, self.sin, eps=EPS)
 
     def loss(self, tokens):
         def norm(x):

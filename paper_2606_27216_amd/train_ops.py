@@ -10,6 +10,10 @@ As in the rest of the binding: argument checks and marshalling only, the work is
 the native library's; calls are asynchronous on ``stream`` (default: torch's
 current stream), results are fresh tensors unless ``out`` is given, and an error
 of the library raises HimuonError. Tensors are float32 or bfloat16.
+
+``embed`` and ``qk_norm_rope`` join autograd where it records: gradients reach the table,
+queries, keys and gains (not the cosines and sines). Results written to ``out``, and the
+other operators' results, carry no graph.
 """
 from __future__ import annotations
 
@@ -146,6 +150,11 @@ def _workspace(need, given, like):
     return given, given.data_ptr(), given.numel() * given.element_size()
 
 
+def _functions():
+    from . import train_autograd  # (torch itself is imported by the first call)
+    return train_autograd
+
+
 def _done(status, what):
     if status != OK:
         raise HimuonError(status, what)
@@ -157,14 +166,17 @@ def embed(tokens, table, scale=1.0, out=None, stream=None):
     """``scale * table[tokens]``: a tensor of ``tokens.shape + (width,)`` in the
     table's type. ``tokens`` is a contiguous int32 or int64 tensor; a token
     outside the table (such as -1 for padding) gives zeros. Rows of ``table`` and
-    of a 2-D ``out`` (one row per token) may be strided."""
-    _torch()
+    of a 2-D ``out`` (one row per token) may be strided. The table's gradient is
+    ``embed_grad``'s."""
+    torch = _torch()
     rows, width, ld = _matrix(table, "table")
     if not tokens.is_cuda or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous CUDA tensor")
     dev, n = table.device, tokens.numel()
     if _away(dev, stream):
         return _on(dev, stream, embed, tokens, table, scale, out)
+    if table.requires_grad and out is None and torch.is_grad_enabled():
+        return _functions().Embed.apply(tokens, table, scale)
     code, index = _type_code(table), _index_code(tokens)
     if out is None:
         out = table.new_empty((*tokens.shape, width))
@@ -294,11 +306,16 @@ def qk_norm_rope(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, inter
                     sequence). A position outside the table marks a token that is
                     not in use: zeros come out.
     ``interleaved`` pairs (2i, 2i+1) instead of (i, i + width).
-    ``out``         the two tensors to write (q and k themselves are allowed)."""
+    ``out``         the two tensors to write (q and k themselves are allowed).
+
+    The gradients of ``q``, ``k`` and the gains are ``qk_norm_rope_grad``'s."""
     sq, sk, args, hq, hk = _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
     dev = q.device
     if _away(dev, stream):
         return _on(dev, stream, qk_norm_rope, q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, out)
+    if out is None and (q.requires_grad or k.requires_grad or q_gain.requires_grad or k_gain.requires_grad) and \
+            _torch().is_grad_enabled():
+        return _functions().QkNormRope.apply(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
     oq, ok, ho, hp = _outputs(out, q, k, sq, sk)
     _done(lib().himuon_qk_norm_rope(args, hq, hk, ho, hp, _stream_of(dev.index)), "himuon_qk_norm_rope")
     return oq, ok
