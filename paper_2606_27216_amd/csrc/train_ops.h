@@ -5,6 +5,7 @@
 #include "elementwise8.h"
 #include "himuon_internal.h"
 #include "ns_gemm_path.h"
+#include "sizes.h"
 
 namespace himuon {
 
@@ -21,8 +22,6 @@ struct StreamDevice {
 inline bool known_dtype(int d) { return d == HIMUON_F32 || d == HIMUON_BF16; }
 inline bool known_index(int i) { return i == HIMUON_I32 || i == HIMUON_I64; }
 inline int64_t dtype_size(int d) { return d == HIMUON_BF16 ? 2 : 4; }
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline size_t round_up(size_t v, size_t to) { return (v + to - 1) / to * to; }
 inline int launch_status()
 {
     const hipError_t e = hipGetLastError();
@@ -105,9 +104,6 @@ template <GemmStore ST> __device__ __forceinline__ void put1(void* base, int64_t
     else static_cast<float*>(base)[i] = v;
 }
 
-// Whether a launch of this many blocks (of `threads` each, in x) stays below 2^32 threads.
-inline bool launchable(int64_t blocks, int threads) { return blocks <= (int64_t)(UINT32_MAX / (uint32_t)threads); }
-
 // Between a wave's writes to LDS and reads of what its other lanes wrote: they are carried out
 // in order, so only the compiler has to keep it.
 __device__ __forceinline__ void wave_exchange()
@@ -116,8 +112,5 @@ __device__ __forceinline__ void wave_exchange()
     __builtin_amdgcn_wave_barrier();
     asm volatile("" ::: "memory");
 }
-
-// True if the product of two non-negative values stays below 2^62.
-inline bool small_product(int64_t a, int64_t b) { return a == 0 || b <= (INT64_C(1) << 62) / a; }
 
 }  // namespace himuon
