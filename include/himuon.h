@@ -622,7 +622,8 @@ int himuon_act_unpack(int64_t n_tokens, int64_t cols, const void* codes, const v
  * its inputs held in 8 bits:
  *     dweight[o, i] (+)= sum over tokens t of grad[t, o] * x[t, i],
  * added to dweight if accumulate != 0. bf16 gradients are exact operands of the
- * matrix cores; fp32 ones are taken as three bf16 terms, which hold all 24 bits.
+ * matrix cores; fp32 ones are taken as three bf16 terms, which hold all 24 bits of
+ * values from 2^-110 on, and of smaller ones those from 2^-133, bf16's last, on.
  * Products are exact and accumulated in fp32. (Codes as himuon_act_pack writes
  * them: the places behind the last token are zeros.)
  *

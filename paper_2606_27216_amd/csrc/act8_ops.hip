@@ -709,8 +709,8 @@ struct StageArgs {
 };
 
 // What a product cannot read where it lies. The gradient: [slice][32][pitch], fp32 as three
-// terms of 8 bits each (x = h + m + l, cut, not rounded: all 24 bits; infinities and NaN in
-// the first alone); rows past the last token and columns past the last are zeros.
+// terms of 8 bits each (x = h + m + l, cut, not rounded: all 24 bits, but none below 2^-133, the last
+// one of bf16; infinities and NaN in the first alone); rows past the last token and columns past the last are zeros.
 template <GemmStore ST> __global__ void __launch_bounds__(kThreads) stage_operands(const StageArgs p)
 {
     if ((int)blockIdx.x >= p.grad_blocks) {
