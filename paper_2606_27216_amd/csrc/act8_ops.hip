@@ -211,9 +211,9 @@ __global__ void __launch_bounds__(kThreads) act_unpack(const uint8_t* codes, con
 // workspace as slices of bf16 rows, fp32 as three terms that follow each other (the
 // codes' slice is then read three times in a row, from cache).
 //
-// Bound by the matrix cores under the board's power cap: 8192 x 11008 x 4096 takes 551 us,
-// 1.34 PFLOP/s (a large library product reaches 1.25 to 1.40 on the card, the library's
-// bf16 product of this shape 0.9). The cores are busy for 68% of the launch's cycles: 688
+// Bound by the matrix cores under the board's power cap: 8192 x 11008 x 4096 takes 551 to 578
+// us, 1.28 to 1.34 PFLOP/s (a large library product reaches 1.25 to 1.40 on the card, the
+// library's bf16 product of this shape 0.9). The cores are busy for 68% of the launch's cycles: 688
 // tiles of 256 are 2.7 rounds of the chip, and a slice takes longer than its 1024 cycles of
 // products. Eight waves of 128 x 64 to a tile against four of 128 x 128 (560) and of 256 x 64,
 // which widen each code once instead of twice (556); a ring of four or six slices 557.

@@ -14,6 +14,9 @@ of the library raises HimuonError. Tensors are float32 or bfloat16.
 ``embed`` and ``qk_norm_rope`` join autograd where it records: gradients reach the table,
 queries, keys and gains (not the cosines and sines). Results written to ``out``, and the
 other operators' results, carry no graph.
+
+Inputs of a call for another stream are the caller's to keep until it has read them
+(``record_stream``), as with torch's own operations.
 """
 from __future__ import annotations
 
@@ -302,7 +305,7 @@ def qk_norm_rope(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, inter
                     for adjacent elements of a head (slices of a fused projection).
     ``cos``, ``sin``  float32, row p the cosines and sines of position p's angles; twice
                     their width is the part of a head that is rotated.
-    ``positions``   int32 or int64, one per token (default: the index in the
+    ``positions``   contiguous int32 or int64, one per token (default: the index in the
                     sequence). A position outside the table marks a token that is
                     not in use: zeros come out.
     ``interleaved`` pairs (2i, 2i+1) instead of (i, i + width).
