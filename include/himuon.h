@@ -642,6 +642,141 @@ int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, const void* 
                        const void* codes, const void* exponents, void* dweight, int64_t ld_dweight, int out_dtype,
                        int accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * The rest of a decoder block's training step: the residual's addition with the norm of
+ * the sum, attention, and the log probabilities of tokens, each with its backward
+ * pass. The rules of the calls above hold for them too. Integer arrays that these
+ * calls read on the device are not checked on the host: starts and lengths are cut to the
+ * tokens there are.
+ */
+
+/*
+ * h = x + residual (NULL: h is x, and nothing is written to h), and
+ *     y = h * gain / sqrt(mean(h^2) + eps)
+ * over each of n_tokens rows of `width` elements. The norm is that of the sum in
+ * fp32, before h is rounded on store. With codes and exponents (both or neither) y is
+ * kept in 8 bits too, as himuon_act_pack of the stored y gives them.
+ *
+ * x, residual, h, y  storage `dtype`, ld >= width. h may be x or residual, y any of
+ *                    the three inputs' buffers (same ld) unless h is it too.
+ * gain               width elements, storage `gain_dtype`.
+ * codes              16-byte aligned.
+ * width              at most 2^26; n_tokens below 2^31 (2^29 with codes).
+ */
+int himuon_add_norm(int64_t n_tokens, int64_t width, const void* x, int64_t ld_x, const void* residual, int64_t ld_residual,
+                    const void* gain, int gain_dtype, void* h, int64_t ld_h, void* y, int64_t ld_y, void* codes, void* exponents,
+                    float eps, int dtype, void* stream);
+
+/*
+ * Its backward pass, from the gradients g_y of y and g_h of h (NULL: none) and from
+ * h: dh, the gradient of x and of the residual alike, and dgain (width elements of
+ * gain_dtype, overwritten, summed over rows in an order that depends on the sizes
+ * alone). dh may be g_y or g_h (same ld).
+ * workspace  himuon_add_norm_grad_workspace_size(n_tokens, width) bytes, 16-byte
+ *            aligned.
+ */
+size_t himuon_add_norm_grad_workspace_size(int64_t n_tokens, int64_t width);
+
+int himuon_add_norm_grad(int64_t n_tokens, int64_t width, const void* g_y, int64_t ld_g_y, const void* g_h, int64_t ld_g_h,
+                         const void* h, int64_t ld_h, const void* gain, int gain_dtype, void* dh, int64_t ld_dh, void* dgain,
+                         float eps, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Largest head of attention. */
+#define HIMUON_MAX_ATTN_DIM 256
+
+/*
+ * What himuon_attention and its gradient share. Arrays are [batch, tokens, heads, dim]
+ * as in himuon_heads_t; heads q_heads / k_heads in number share a key head.
+ *
+ * Sequences are the rows of the batch, or packed: token starts[s] .. starts[s + 1] - 1
+ * of one array of q_len (k_len) tokens is sequence s, batch + 1 starts that do not
+ * decrease. Of a sequence's tokens the first lengths[s] are in use (NULL: all of
+ * them). Tokens that are not, and those of no sequence, are not read: their
+ * results are zeros (lse: minus infinity), whatever they hold.
+ *
+ * With `causal`, query i of n_q in use sees the keys j <= i + n_k - n_q of the n_k
+ * in use (the last query lies on the last key), else all of them. A query that
+ * sees no key has the result zero, lse minus infinity, and gives no gradient. A value that
+ * is not finite at a key that a query does not see, within a sequence's tokens in use,
+ * may reach the query's result (as 0 times it), as a query's may the gradients of keys that
+ * do not see it.
+ */
+typedef struct himuon_attn {
+    int64_t batch;           /* rows of the batch; packed: sequences            */
+    int64_t q_len, k_len;    /* tokens of a row; packed: of the arrays          */
+    int32_t q_heads, k_heads;/* q_heads a multiple of k_heads                   */
+    int32_t head_dim;        /* 1 .. HIMUON_MAX_ATTN_DIM                        */
+    int32_t causal;
+    int32_t dtype;           /* storage of every array but lse                  */
+    int32_t index;           /* himuon_index_t of starts and lengths            */
+    const void* q_starts;    /* batch + 1 (device); both NULL: not packed       */
+    const void* k_starts;
+    const void* q_lengths;   /* batch (device), or NULL                         */
+    const void* k_lengths;
+    float scale;             /* of the scores, > 0                              */
+} himuon_attn_t;
+
+/*
+ * out = softmax(scale * q k^T) v over the keys that each query sees, and lse, the
+ * natural logarithm of the sum of the scores' exponentials: [batch, q_len, q_heads] fp32,
+ * contiguous. Products of bf16 arrays are exact, the softmax's statistics fp32, its
+ * values rounded to bf16 for their product with v; fp32 arrays are multiplied in fp32.
+ * out must not overlap the inputs.
+ * workspace  himuon_attention_workspace_size(args) bytes, 16-byte aligned (0: none is
+ *            needed, or the arguments are invalid; NULL will do).
+ */
+size_t himuon_attention_workspace_size(const himuon_attn_t* args);
+
+int himuon_attention(const himuon_attn_t* args, const himuon_heads_t* q, const himuon_heads_t* k, const himuon_heads_t* v,
+                     const himuon_heads_t* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its backward pass: from the gradient g of out, and the inputs and results of the
+ * forward call, the gradients dq, dk, dv (summed over the heads that share a key head).
+ * They must not overlap the inputs.
+ * workspace  himuon_attention_grad_workspace_size(args) bytes, 16-byte aligned.
+ */
+size_t himuon_attention_grad_workspace_size(const himuon_attn_t* args);
+
+int himuon_attention_grad(const himuon_attn_t* args, const himuon_heads_t* g, const himuon_heads_t* q, const himuon_heads_t* k,
+                          const himuon_heads_t* v, const himuon_heads_t* out, const float* lse, const himuon_heads_t* dq,
+                          const himuon_heads_t* dk, const himuon_heads_t* dv, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* Most alternatives of a call below. */
+#define HIMUON_MAX_TOP 64
+
+/*
+ * Of the distributions softmax(scale * logits[i, :]) over `vocab` tokens:
+ *     logprob[i]  the logarithm of tokens[i]'s probability
+ *     entropy[i]  - sum of p log p
+ *     lse[i]      the logarithm of the sum of exponentials
+ *     top_logprob, top_index [n_tokens, top]  the `top` largest of its log probabilities and their
+ *                 tokens, the largest first, equal logits by index (NaN counts as largest)
+ * A token outside [0, vocab) (such as -1) marks a row that is not in use: it is not
+ * read, its results are zeros and its top_index -1. A row whose logits are all
+ * minus infinity has the log probabilities and lse minus infinity and entropy zero.
+ * Sums are fp32, relative to the row's maximum.
+ *
+ * logits     n_tokens x vocab, storage `dtype`, ld >= vocab; vocab below 2^31.
+ * tokens     n_tokens integers of type `index`.
+ * scale      > 0. top: 0 .. min(vocab, HIMUON_MAX_TOP); 0: top_logprob, top_index are unused.
+ */
+int himuon_token_logprob(int64_t n_tokens, int64_t vocab, const void* logits, int64_t ld, int dtype, const void* tokens, int index,
+                         float scale, int top, float* logprob, float* entropy, float* lse, float* top_logprob, int64_t* top_index,
+                         void* stream);
+
+/*
+ * The logits' gradient from those of logprob and entropy (each may be NULL: none):
+ *     d[i, j] = scale * (g_logprob[i] (delta(j, tokens[i]) - p) - g_entropy[i] p (log p + entropy[i]))
+ * with p from the logits and lse. Rows that are not in use, and rows whose lse is minus
+ * infinity, get zeros; so do logits of minus infinity but for the token's own. d: storage
+ * `dtype`, ld_d >= vocab; may be the logits (same ld).
+ */
+int himuon_token_logprob_grad(int64_t n_tokens, int64_t vocab, const float* g_logprob, const float* g_entropy, const void* logits,
+                              int64_t ld, int dtype, const void* tokens, int index, const float* lse, const float* entropy,
+                              float scale, void* d, int64_t ld_d, void* stream);
+
 /* Static English text for a status code. */
 const char* himuon_status_string(int status);
 

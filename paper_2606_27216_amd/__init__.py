@@ -119,6 +119,7 @@ def lib():
         L.himuon_calib_mfma.argtypes = [ctypes.c_int, vp, vp, ctypes.c_int, ctypes.c_int, vp]
         L.himuon_calib_mfma.restype = ctypes.c_int
         train_ops.declare(L)
+        block_ops.declare(L)
         _lib = L
     return _lib
 
@@ -774,3 +775,6 @@ class HiMuon:
 from . import train_ops  # noqa: E402  (takes the error type and the checks above)
 from .train_ops import (act_pack, act_unpack, embed, embed_grad, qk_norm_rope,  # noqa: E402,F401
                         qk_norm_rope_grad, weight_grad)
+from . import block_ops  # noqa: E402
+from .block_ops import (add_norm, add_norm_grad, attention, attention_grad, token_logprob,  # noqa: E402,F401
+                        token_logprob_grad)

@@ -30,6 +30,8 @@ COMMON = [
 # accumulators in architectural VGPRs, where the vector ALU converts or sums
 # them after each product (fp32, T = 64: 1493 us without the flag, 1383 with it;
 # bf16 operands, T = 32 / 64 / 128 on 12 x 2048^2: 149 / 194 / 299 and 118 / 128 / 264).
+# So do the attention kernels, whose scores turn from a result into an operand: with it two waves
+# share a SIMD at a head of 128 (242 registers, 258 without it in the queries' gradient).
 SOURCES = [
     ("ns_tiled_kernels.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
     ("ns_tiled_f16.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
@@ -41,6 +43,10 @@ SOURCES = [
     ("embed_ops.hip", []),
     ("qk_norm_rope.hip", []),
     ("act8_ops.hip", []),
+    ("add_norm.hip", []),
+    ("attention.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
+    ("attention_grad.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
+    ("token_logprob.hip", []),
     ("himuon_api.cpp", []),
     ("ns_gemm_path.cpp", []),
     ("himuon_step.cpp", []),

@@ -1,0 +1,280 @@
+"""attention and its gradient against the definition in 64 bits, sequence by sequence.
+
+Tolerances. A score is off by at most (dim + 4) U of |q| |k| scale (U = 2^-24), a probability
+by that twice (the sum shares it), 16 U and U of the exponent's size; a sum of n terms by n U. bf16: the
+probabilities (in the gradient also ds) round by half a step, 2^-8, before their product, and
+every result does on store.
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2606_27216_amd as hm
+
+pytestmark = pytest.mark.gpu
+T = {"f32": torch.float32, "bf16": torch.bfloat16}
+U = 2.0 ** -24
+
+
+def heads(gen, lead, rows, n, dim, dtype, layout):
+    if layout == "heads":
+        return torch.randn(*lead, n, rows, dim, generator=gen, device="cuda").to(T[dtype]).transpose(-3, -2)
+    if layout == "fused":  # a slice of a wider projection
+        return torch.randn(*lead, rows, n + 3, dim, generator=gen, device="cuda").to(T[dtype])[..., 1:n + 1, :]
+    if layout == "odd":    # rows at odd addresses
+        return torch.randn(*lead, rows, n, dim + 3, generator=gen, device="cuda").to(T[dtype])[..., 1:dim + 1]
+    return torch.randn(*lead, rows, n, dim, generator=gen, device="cuda").to(T[dtype])
+
+
+def make(lead, nq, nk, hq, hk, dim, dtype, layout="tokens", seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    q, k, v, g = (heads(gen, lead, n, h, dim, dtype, layout) for n, h in ((nq, hq), (nk, hk), (nk, hk), (nq, hq)))
+    return q, k, v, g
+
+
+def pieces(q, k, where):
+    """(queries, keys) of each sequence as slices of the flattened tokens."""
+    if "q_starts" in where:
+        a, b = where["q_starts"].tolist(), where.get("k_starts", where["q_starts"]).tolist()
+        n = len(a) - 1
+        caps = [(a[i], a[i + 1] - a[i], b[i], b[i + 1] - b[i]) for i in range(n)]
+    else:
+        B, S, K = (q.shape[0], q.shape[1], k.shape[1]) if q.dim() == 4 else (1, q.shape[0], k.shape[0])
+        caps = [(i * S, S, i * K, K) for i in range(B)]
+    ql, kl = (where[x].tolist() if x in where else [None] * len(caps) for x in ("q_lengths", "k_lengths"))
+    return [(slice(a, a + (n if x is None else x)), slice(b, b + (m if y is None else y))) for (a, n, b, m), x, y in zip(caps, ql, kl)]
+
+
+def reference(q, k, v, g, where, causal, scale, out=None, lse=None):
+    """Results in 64 bits with their tolerances' parts: forward (out, lse), or backward where the
+    call's out and lse are given."""
+    D, H, G = q.shape[-1], q.shape[-2], k.shape[-2]
+    f = [t.reshape(-1, t.shape[-2], D).double() for t in (q, k, v)] + [g.reshape(-1, H, D).double()]
+    zeros = [torch.zeros_like(t) for t in f[:3]]
+    res = {n: torch.zeros_like(t) for n, t in zip(("out", "dk", "dv", "dq"), (f[0], f[1], f[2], f[0]))}
+    tol = {n: torch.zeros_like(t) for n, t in res.items()}
+    res["lse"], tol["lse"] = torch.full(f[0].shape[:2], -math.inf, device="cuda", dtype=torch.float64), torch.zeros(f[0].shape[:2], device="cuda", dtype=torch.float64)
+    h = torch.finfo(q.dtype).eps / 2 if q.dtype == torch.bfloat16 else 0.0
+    del zeros
+    for rows, keys in pieces(q, k, where):
+        n, m = rows.stop - rows.start, keys.stop - keys.start
+        if n <= 0 or m <= 0:
+            continue
+        hide = torch.ones(n, m, dtype=torch.bool, device="cuda").triu(m - n + 1) if causal else torch.zeros(n, m, dtype=torch.bool, device="cuda")
+        for i in range(H):
+            j = i * G // H
+            a, b, c, e = f[0][rows, i], f[1][keys, j], f[2][keys, j], f[3][rows, i]
+            s = (a @ b.t().contiguous()) * scale
+            err = 2 * (D + 4) * U * scale * a.norm(dim=1, keepdim=True) * b.norm(dim=1).max() + 16 * U + 4 * U * s.abs().amax(1, keepdim=True)
+            s = s.masked_fill(hide, -math.inf)
+            if out is None:
+                l = torch.logsumexp(s, 1, keepdim=True)
+                p = torch.where(hide, 0.0, (s - l.clamp_min(-1e300)).exp())
+                o = p @ c
+                res["out"][rows, i], res["lse"][rows, i] = o, l[:, 0]
+                tol["out"][rows, i] = (p @ c.abs()) * (h + 2 * err + m * U)
+                tol["lse"][rows, i] = err[:, 0] + m * U + 4 * U * l[:, 0].abs().nan_to_num(0, 0, 0)
+                continue
+            L = lse.reshape(-1, H)[rows, i].double()[:, None]
+            O = out.reshape(-1, H, D)[rows, i].double()
+            dead = hide | (L == -math.inf)
+            p = torch.where(dead, 0.0, (s - L.clamp_min(-1e300)).exp())
+            err = err + 4 * U * L.abs().nan_to_num(0, 0, 0)
+            dp, d = e @ c.t().contiguous(), (e * O).sum(1, keepdim=True)
+            ds = p * (dp - d)
+            rough = p * ((e.abs() @ c.abs().t().contiguous()) + (e * O).abs().sum(1, keepdim=True)) * (err + (2 * D + 8) * U)
+            res["dv"][keys, j] += p.t().contiguous() @ e
+            tol["dv"][keys, j] += (p * (h + err + (n * H // G) * U)).t().contiguous() @ e.abs()
+            res["dq"][rows, i] = scale * (ds @ b)
+            tol["dq"][rows, i] = scale * ((ds.abs() * (h + m * U) + rough) @ b.abs())
+            res["dk"][keys, j] += scale * (ds.t().contiguous() @ a)
+            tol["dk"][keys, j] += scale * ((ds.abs() * (h + (n * H // G) * U) + rough).t().contiguous() @ a.abs())
+    return res, tol
+
+
+def close(name, got, res, tol, dtype):
+    want = res[name].reshape(got.shape)
+    room = 1.05 * tol[name].reshape(got.shape) + (0.0 if name == "lse" else want.abs().nan_to_num(0, 0, 0) * torch.finfo(dtype).eps / 2) + 1e-30
+    inf = want == -math.inf
+    assert torch.equal(got == -math.inf, inf), name
+    off = torch.where(inf, 0.0, (got.double() - want).abs())
+    assert bool(off.isfinite().all()), name
+    assert bool((off <= room).all()), f"{name}: {int((off > room).sum())} of {off.numel()} off, worst {float((off / room).max()):.3g} times the tolerance"
+
+
+def check(q, k, v, g, causal=True, scale=None, **where):
+    dtype, c = q.dtype, q.shape[-1] ** -0.5 if scale is None else scale
+    out, lse = hm.attention(q, k, v, causal=causal, scale=scale, **where)
+    res, tol = reference(q, k, v, g, where, causal, c)
+    close("out", out, res, tol, dtype)
+    close("lse", lse, res, tol, dtype)
+    o, l = res["out"].to(dtype).view(q.shape), res["lse"].float().view(lse.shape)
+    grads = hm.attention_grad(g, q, k, v, o, l, causal=causal, scale=scale, **where)
+    res, tol = reference(q, k, v, g, where, causal, c, o, l)
+    for name, got in zip(("dq", "dk", "dv"), grads):
+        close(name, got, res, tol, dtype)
+    return out, lse, grads
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [1, 8, 20, 33, 64, 72, 80, 127, 128, 136, 200, 256])
+def test_heads_sizes(dim, dtype):
+    print("[gpu-case] attention dim", dim, dtype, flush=True)
+    for hq, hk, n, layout in ((2, 2, 70, "tokens"), (6, 2, 150, "heads"), (5, 1, 33, "odd")):
+        check(*make((2,), n, n, hq, hk, dim, dtype, layout, dim))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,nk", [(1, 1), (1, 31), (2, 64), (3, 65), (31, 31), (32, 32), (33, 33), (64, 64), (127, 127), (128, 128), (129, 129),
+                                   (200, 333), (257, 257), (300, 40), (1, 1000), (4, 777), (16, 2049)])
+def test_lengths(nq, nk, dtype):
+    print("[gpu-case] attention lengths", nq, nk, dtype, flush=True)
+    for causal in (True, False):
+        check(*make((1,), nq, nk, 4, 2, 64, dtype, "fused", nq + nk), causal=causal)
+        check(*make((3,), nq, nk, 3, 1, 128, dtype, "tokens", nq + nk), causal=causal, scale=0.3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_long_rows(dtype):
+    print("[gpu-case] attention long", dtype, flush=True)
+    check(*make((1,), 1500, 1500, 2, 1, 128, dtype, "heads", 1))
+    check(*make((2,), 1, 9001, 8, 2, 128, dtype, "heads", 2))
+    check(*make((1,), 1, 5000, 1, 1, 256, dtype, "tokens", 3))
+    check(*make((1,), 2, 5000, 16, 1, 64, dtype, "tokens", 3))
+
+
+@pytest.mark.parametrize("dtype,index", [("bf16", torch.int32), ("f32", torch.int64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_packed(causal, dtype, index):
+    print("[gpu-case] attention packed", causal, dtype, flush=True)
+    for starts, total in (([0, 5, 5, 140, 141, 300], 300), ([0, 0, 200], 260), ([3, 64, 96], 128), ([0], 40), ([0, 1], 1), ([10, 10], 10)):
+        s = torch.tensor(starts, dtype=index, device="cuda")
+        q, k, v, g = make((), total, total, 6, 3, 64, dtype, "tokens", total)
+        off = torch.ones(total, dtype=torch.bool)
+        off[starts[0]:starts[-1]] = False
+        q[off.cuda()] = k[off.cuda()] = math.nan  # tokens of no sequence are not read
+        v[off.cuda()] = g[off.cuda()] = math.inf
+        out, lse, grads = check(q.nan_to_num(0), k.nan_to_num(0), v.nan_to_num(0, 0, 0), g.nan_to_num(0, 0, 0), causal=causal, q_starts=s)
+        again = hm.attention(q, k, v, q_starts=s, causal=causal)
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+        for t in (out, *grads):
+            assert not t[off.cuda()].any()
+    # keys of their own, and tokens in use of each sequence
+    qs = torch.tensor([0, 40, 41, 100, 170], dtype=index, device="cuda")
+    ks = torch.tensor([2, 30, 200, 260, 390], dtype=index, device="cuda")
+    q, k, v, g = make((), 180, 400, 8, 2, 80, dtype, "heads", 5)
+    check(q, k, v, g, causal=causal, q_starts=qs, k_starts=ks)
+    ql, kl = (torch.tensor(x, dtype=index, device="cuda") for x in ([40, 0, 33, 70], [0, 170, 60, 101]))
+    check(q, k, v, g, causal=causal, q_starts=qs, k_starts=ks, q_lengths=ql, k_lengths=kl)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_padded_batches_and_caches(dtype):
+    print("[gpu-case] attention padded", dtype, flush=True)
+    n = torch.tensor([77, 1, 0, 200, 130], dtype=torch.int32, device="cuda")
+    q, k, v, g = make((5,), 200, 200, 4, 2, 128, dtype, "tokens", 6)
+    pad = torch.arange(200, device="cuda")[None] >= n[:, None]
+    for t in (q, k, v, g):
+        t[pad] = 0
+    for causal in (True, False):
+        out, lse, grads = check(q, k, v, g, causal=causal, q_lengths=n, k_lengths=n)
+        dirty = [t.clone() for t in (q, k, v, g)]
+        for t, x in zip(dirty, (math.nan, math.inf, math.nan, -math.inf)):
+            t[pad] = x
+        a, b = hm.attention(*dirty[:3], causal=causal, q_lengths=n, k_lengths=n)
+        assert torch.equal(a, out) and torch.equal(b, lse)
+        o, l = out, lse
+        clean = hm.attention_grad(g, q, k, v, o, l, causal=causal, q_lengths=n, k_lengths=n)
+        o = o.clone()
+        o[pad] = math.nan
+        for x, y in zip(clean, hm.attention_grad(dirty[3], *dirty[:3], o, l, causal=causal, q_lengths=n, k_lengths=n)):
+            assert torch.equal(x, y) and not x[pad].any()
+    # one query (and three) of each sequence against keys held so far
+    for nq, hq in ((1, 8), (3, 8), (1, 3), (16, 2)):
+        kl = torch.tensor([1000, 1, 0, 517, 64], dtype=torch.int64, device="cuda")
+        q, k, v, g = make((5,), nq, 1000, hq, 1, 128, dtype, "heads", 7)
+        hidden = torch.arange(1000, device="cuda")[None] >= kl[:, None]
+        k[hidden] = math.nan
+        v[hidden] = math.inf
+        check(q, k.nan_to_num(0), v.nan_to_num(0, 0, 0), g, k_lengths=kl)
+        a, b = hm.attention(q, k, v, k_lengths=kl), hm.attention(q, k.nan_to_num(0), v.nan_to_num(0, 0, 0), k_lengths=kl)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_lengths_outside_are_cut():
+    """Starts and lengths beyond the tokens there are do not reach outside of them."""
+    q, k, v, g = make((2,), 50, 50, 2, 1, 64, "f32", "tokens", 8)
+    want = hm.attention(q, k, v)
+    n = torch.tensor([1000, 51], dtype=torch.int32, device="cuda")
+    got = hm.attention(q, k, v, q_lengths=n, k_lengths=n)
+    assert torch.equal(got[0], want[0])
+    assert not hm.attention(q, k, v, q_lengths=-n, k_lengths=n)[0].any()
+    s = torch.tensor([-5, 30, 1000], dtype=torch.int64, device="cuda")
+    got = hm.attention(q[0], k[0], v[0], q_starts=s)
+    want = hm.attention(q[0], k[0], v[0], q_starts=torch.tensor([0, 30, 50], device="cuda"))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_large_scores_and_equal_calls():
+    q, k, v, g = make((2,), 300, 300, 4, 2, 128, "bf16", "tokens", 9)
+    out, lse, grads = check(q * 12, k * 12, v, g)  # scores of some hundreds: near one-hot rows
+    again = hm.attention(q * 12, k * 12, v)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    a = hm.attention_grad(g, q, k, v, *hm.attention(q, k, v))
+    b = hm.attention_grad(g, q, k, v, *hm.attention(q, k, v))
+    for x, y in zip(a, b):
+        assert torch.equal(x, y)
+
+
+def test_outputs_strides_and_broadcast_keys():
+    q, k, v, g = make((2,), 90, 90, 4, 2, 64, "bf16", "tokens", 10)
+    out, lse = hm.attention(q, k, v)
+    room = torch.full((2, 4, 90, 64 + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    mine = room[..., :64].transpose(1, 2)
+    assert hm.attention(q, k, v, out=mine)[0] is mine and torch.equal(mine, out) and bool((room[..., 64:] == 7).all())
+    one = k[:, :, :1].expand(2, 90, 2, 64)  # the same keys for every head
+    a, b = hm.attention(q, one, v)[0], hm.attention(q, one.contiguous(), v)[0]
+    assert torch.equal(a, b)
+    grads = hm.attention_grad(g, q, k, v, out, lse)
+    rooms = [torch.zeros(2, 90, n, 67, dtype=torch.bfloat16, device="cuda")[..., 3:] for n in (4, 2, 2)]
+    for x, y in zip(hm.attention_grad(g, q, k, v, out, lse, grads=rooms), grads):
+        assert torch.equal(x, y)
+
+
+def test_empty_calls():
+    q, k, v, g = make((2,), 5, 0, 2, 1, 64, "f32", "tokens", 11)
+    out, lse = hm.attention(q, k, v)
+    assert not out.any() and bool((lse == -math.inf).all())
+    assert not hm.attention_grad(g, q, k, v, out, lse)[0].any()
+    q, k, v, g = make((2,), 0, 5, 2, 1, 64, "f32", "tokens", 11)
+    out, lse = hm.attention(q, k, v)
+    assert out.shape == (2, 0, 2, 64)
+    _, dk, dv = hm.attention_grad(g, q, k, v, out, lse)
+    assert not dk.any() and not dv.any()
+    q, k, v, g = make((0,), 5, 5, 2, 1, 64, "f32", "tokens", 11)
+    assert hm.attention(q, k, v)[0].shape == (0, 5, 2, 64)
+
+
+def test_autograd_and_differences():
+    q, k, v, g = (t.clone().requires_grad_(i < 3) for i, t in enumerate(make((2,), 40, 40, 4, 2, 24, "f32", "tokens", 12)))
+    n = torch.tensor([40, 23], device="cuda")
+    out, lse = hm.attention(q, k, v, q_lengths=n, k_lengths=n)
+    assert not lse.requires_grad
+    (out * g.detach()).sum().backward()
+
+    def loss(a, b, c):
+        b, c = (t.repeat_interleave(2, 2).transpose(1, 2) for t in (b, c))
+        i = torch.arange(40, device="cuda")
+        see = (i[None, :, None] < n[:, None, None]) & (i[None, None, :] <= i[None, :, None])
+        s = (a.transpose(1, 2) @ b.transpose(2, 3).contiguous() / 24 ** 0.5).masked_fill(~see[:, None], -1e300)
+        p = torch.softmax(s, -1) * see[:, None]
+        return ((p @ c).transpose(1, 2) * g.detach().double()).sum()
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    args, step = [t.detach().double() for t in (q, k, v)], 1e-5
+    for i, t in enumerate((q, k, v)):
+        d = torch.randn(args[i].shape, generator=gen, device="cuda", dtype=torch.float64)
+        up, down = list(args), list(args)
+        up[i], down[i] = args[i] + step * d, args[i] - step * d
+        want = float(loss(*up) - loss(*down)) / (2 * step)
+        assert abs(float((t.grad.double() * d).sum()) - want) < 1e-6 + 400 * U * float((t.grad.double() * d).abs().sum())
