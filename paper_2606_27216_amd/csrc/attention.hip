@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace himuon {
 namespace attn {
@@ -18,78 +19,93 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64, kTileRows = kRows * kWaves;
 
-// Keys of a tile: two buffers of keys and values leave room for two blocks to a CU where rows are short.
-template <GemmStore ST, int DP> constexpr int tile_keys() { return DP * (ST == GemmStore::BF16 ? 2 : 4) <= 256 ? 64 : 32; }
-
+// A row's softmax as far as it has come: o unnormalised, the maximum m that its exponentials are
+// relative to, their sum l (of this half's keys).
 template <GemmStore ST, int DP> struct Running {
     using L = Lay<ST, DP>;
     f32x16 o[L::DT];
-    float m, l;  // l: of this half's keys
+    float m, l, l2;  // l: in two parts
 
     HM_DEV void clear()
     {
 #pragma unroll
         for (int t = 0; t < L::DT; ++t) o[t] = f32x16{};
         m = -INFINITY;
-        l = 0.f;
+        l = l2 = 0.f;
     }
 
-    // KT tiles of 32 keys at `kt`, `vt`; `masked` (the same in all lanes): this lane's row sees the first `left` of them.
-    template <int KT> HM_DEV void keys(const uint8_t* kt, const uint8_t* vt, const Frag<ST> (&q)[L::NS], float c, bool masked, int left, int lane)
+    // This lane's row sees the first `left` of the keys.
+    static HM_DEV void hide(f32x16& s, int left, int lane)
     {
-        const int h = lane >> 5;
-        f32x16 s[KT];
+        left -= 4 * (lane >> 5);
 #pragma unroll
-        for (int k = 0; k < KT; ++k) s[k] = f32x16{};
-        ahead<KT * L::NS>([&](int i) { return L::row_frag(kt, 32 * (i / L::NS) + (lane & 31), i % L::NS, h); },
-                          [&](int i, const Frag<ST>& a) { mma<ST>(s[i / L::NS], a, q[i % L::NS]); });
-        if (masked) {
+        for (int i = 0; i < 16; ++i) s[i] = result_row(i, 0) < left ? s[i] : -INFINITY;
+    }
+    static HM_DEV float top(const f32x16& s, float t, int from, int to)
+    {
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[k][i] = 32 * k + result_row(i, h) < left ? s[k][i] : -INFINITY;
+        for (int i = from; i < to; i += 2) {
+            t = fmaxf(fmaxf(s[i], s[i + 1]), t);
+            settle(t);
         }
-        float top = s[0][0];
-#pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[k][i]);
-        top = max_halves(top);
-        // The maximum follows once it is left behind by 2^8: any value near it serves, and most
-        // tiles then leave o as it is.
-        if (__any(top * c > m * c + 8.f)) {
-            const float now = fmaxf(m, top);
+        return t;
+    }
+    // The maximum follows once the scores leave it behind by 2^8: any value near it serves, and
+    // most tiles then leave o as it is.
+    HM_DEV void follow(float t, float c)
+    {
+        t = max_halves(t);
+        if (__any(t * c > m * c + 8.f)) {
+            const float now = fmaxf(m, t);
             const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - now) * c);
             m = now;
             l *= f;
+            l2 *= f;
 #pragma unroll
-            for (int t = 0; t < L::DT; ++t)
+            for (int x = 0; x < L::DT; ++x)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[t][i] *= f;
+                for (int i = 0; i < 16; ++i) o[x][i] *= f;
         }
-        const float mc = m == -INFINITY ? 0.f : m * c;
-        float sum[2] = {};
+    }
+    // What the exponentials are relative to.
+    HM_DEV float base(float c) const { return m == -INFINITY ? 0.f : m * c; }
+    // Elements [from, to) of s, an even number, to the operand p.
+    HM_DEV void exponentials(const f32x16& s, Frag<ST> (&p)[2], float c, float mc, int from, int to)
+    {
 #pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[k][i] = __builtin_amdgcn_exp2f(fmaf(s[k][i], c, -mc));
-                sum[i & 1] += s[k][i];
-            }
-        l += sum[0] + sum[1];
-        Frag<ST> pr[2 * KT];
-#pragma unroll
-        for (int k = 0; k < 2 * KT; ++k) pr[k] = as_operand<ST>(s[k / 2], k % 2);
-        ahead<2 * KT * L::DT>([&](int i) { return L::col_frag(vt, 16 * (i / L::DT), 32 * (i % L::DT), lane); },
-                              [&](int i, const Frag<ST>& a) { mma<ST>(o[i % L::DT], a, pr[i / L::DT]); });
+        for (int i = from; i < to; i += 2) {
+            const float a = __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc)), b = __builtin_amdgcn_exp2f(fmaf(s[i + 1], c, -mc));
+            l += a;
+            l2 += b;
+            set_pair<ST>(p, i / 2, a, b);
+            settle_pair<ST>(p, i / 2);
+            settle(l);
+            settle(l2);
+        }
+    }
+    HM_DEV auto read_k(const uint8_t* kt, int lane) const
+    {
+        return [=](int i) __attribute__((always_inline)) { return L::row_frag(kt, lane & 31, i, lane >> 5); };
+    }
+    HM_DEV auto read_v(const uint8_t* vt, int lane) const
+    {
+        return [=](int i) __attribute__((always_inline)) { return L::col_frag(vt, 16 * (i / L::DT), 32 * (i % L::DT), lane); };
     }
 };
+template <GemmStore ST, int DP> using KeyFrags = Ahead<Frag<ST>, DP / 16, kDepth<ST, DP>>;
+template <GemmStore ST, int DP> using ValueFrags = Ahead<Frag<ST>, DP / 16, kDepth<ST, DP>>;
 
-template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThreads, (DP * (ST == GemmStore::BF16 ? 2 : 4) <= 256 ? 2 : 1)) attn_forward(const AttnArgs p)
+// Tiles of 32 keys lie in rings of LDS buffers; a wave multiplies a tile's keys beside the
+// exponentials of the tile before and that tile's values beside the next one's maximum, so that the
+// matrix cores work while the vector ALU does.
+template <GemmStore ST, int DP> constexpr int ring() { return Lay<ST, DP>::PITCH <= 512 ? 4 : 2; }
+
+template <GemmStore ST, int DP, bool DMA>
+__global__ void __launch_bounds__(kThreads, (Lay<ST, DP>::PITCH <= 256 ? 2 : 1)) attn_forward(const AttnArgs p)
 {
     using L = Lay<ST, DP>;
-    constexpr int BN = tile_keys<ST, DP>(), TILE = BN * L::PITCH;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TILE];  // [2][keys, values]
+    constexpr int R = ring<ST, DP>(), TILE = kRows * L::PITCH, VALUES = R * TILE;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * R * TILE];  // [R] keys, [R] values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
@@ -100,54 +116,123 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
     // (a sequence's last tiles, which see the most keys, first)
     const int64_t tile = p.packed ? items - 1 - at_item : at_item / p.slots * p.slots + (p.slots - 1 - at_item % p.slots);
     const Seq s = find_seq<false, kTileRows>(p, tile, G);
-    const int64_t rows = (int64_t)s.q_cap * G, r0 = (int64_t)s.tile * kTileRows;
+    const int rows = s.q_cap * G, r0 = s.tile * kTileRows;  // (a sequence's rows are counted in 32 bits)
     if (r0 >= rows) return;
 
-    const int64_t r = r0 + wave * kRows + (lane & 31);
+    const int r = r0 + wave * kRows + (lane & 31);
     const int query = (int)((uint32_t)r / (uint32_t)G);
     const int head = kh * G + (int)((uint32_t)r - (uint32_t)query * (uint32_t)G);
     const bool exists = r < rows, on = query < s.nq;
-    Frag<ST> q[L::NS];
-    load_row<ST, DP>(q, at(p.q, s.batch, s.q0 + query, head), on, p.dim, h);
 
-    // keys that the block's, the wave's and the lane's rows see
-    const int last = min((int)((r0 + kTileRows - 1) / G), s.nq - 1);
-    const int n_block = s.nq > 0 && r0 < (int64_t)s.nq * G ? visible(p, s, last) : 0;
-    const int64_t w0 = r0 + wave * kRows;
-    const int n_wave = w0 < (int64_t)s.nq * G ? visible(p, s, min((int)((w0 + kRows - 1) / G), s.nq - 1)) : 0;
-    const int n_all = visible(p, s, (int)(w0 / G));  // seen by all of the wave's rows
-    const int n_lane = on ? visible(p, s, query) : 0;
+    // tiles of keys that the block's and the wave's rows see; keys seen by all of the wave's
+    // rows, and by this lane's
+    const int w0 = r0 + wave * kRows, in_use = s.nq * G;
+    auto seen = [&](int row) { return row < in_use ? visible(p, s, (int)((uint32_t)row / (uint32_t)G)) : 0; };
+    const int tiles = (seen(min(r0 + kTileRows, in_use) - 1) + kRows - 1) / kRows * (r0 < in_use);
+    const int mine = (seen(min(w0 + kRows, in_use) - 1) + kRows - 1) / kRows * (w0 < in_use);
+    const int n_all = seen(w0), n_lane = on ? visible(p, s, query) : 0;
+    const int whole = min(tiles, s.nk / kRows);
+
+    const int row_bytes = p.dim * L::ES;
+    const uint8_t *kp = at(p.k, s.batch, s.k0, kh), *vp = at(p.v, s.batch, s.k0, kh);
+    const Share<ST, DP, kRows, kThreads> share{(int)threadIdx.x};
+    constexpr int NI = Share<ST, DP, kRows, kThreads>::NI;
+    // The next tile of keys and of values, to its place in the ring: a whole one, or any.
+    const bool exact = DMA && row_bytes == L::PITCH;
+    uint32_t k_off[NI], v_off[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        k_off[i] = share.offset(i, p.k.ss);
+        v_off[i] = share.offset(i, p.v.ss);
+    }
+    auto load = [&](const uint8_t* from, int64_t stride, uint8_t* to, int t) __attribute__((always_inline)) {
+        if (t >= tiles) return;
+        share.template stage<DMA>(to, from + t * kRows * stride, row_bytes, t < whole, [&](int i) { return share.row(i) * stride; },
+                                  [&](int i) { return t * kRows + share.row(i) < s.nk; });
+    };
+    auto load_k = [&](int t, int place) __attribute__((always_inline)) { load(kp, p.k.ss, lds + place * TILE, t); };
+    auto load_v = [&](int t, int place) __attribute__((always_inline)) { load(vp, p.v.ss, lds + VALUES + place * TILE, t); };
 
     Running<ST, DP> run;
     run.clear();
     const float c = p.scale * kLog2e;
-    const int row_bytes = p.dim * L::ES;
-    const uint8_t *kp = at(p.k, s.batch, s.k0, kh), *vp = at(p.v, s.batch, s.k0, kh);
-    const Share<ST, DP, BN, kThreads> share{(int)threadIdx.x};
-    auto load = [&](int buf, int j0) __attribute__((always_inline)) {
-        uint8_t* const t = lds + buf * 2 * TILE;
-        const bool whole = j0 + BN <= s.nk;
-        auto on = [&](int i) { return j0 + share.row(i) < s.nk; };
-        share.template stage<DMA>(t, kp + j0 * p.k.ss, row_bytes, whole, [&](int i) { return share.row(i) * p.k.ss; }, on);
-        share.template stage<DMA>(t + TILE, vp + j0 * p.v.ss, row_bytes, whole, [&](int i) { return share.row(i) * p.v.ss; }, on);
-    };
-    if (n_block > 0) {
+    if (tiles > 0) {
         if (DMA && p.dim < DP) {
-            clear_lds<kThreads>(lds, 4 * TILE);
+            clear_lds<kThreads>(lds, 2 * R * TILE);
             __syncthreads();
         }
-        load(0, 0);
-        int buf = 0;
-        for (int j0 = 0; j0 < n_block; j0 += BN, buf ^= 1) {
-            dev::dma_wait_barrier<0>();
-            if (j0 + BN < n_block) load(buf ^ 1, j0 + BN);
-            if (j0 >= n_wave) continue;
-            const uint8_t* const t = lds + buf * 2 * TILE;
-            run.template keys<BN / 32>(t, t + TILE, q, c, j0 + BN > n_all, n_lane - j0, lane);
+        // (values of tile t and keys of tile t + 1 travel together)
+        load_k(0, 0);
+#pragma unroll
+        for (int t = 0; t < R - 1; ++t) {
+            load_v(t, t);
+            load_k(t + 1, t + 1);
+        }
+        Frag<ST> q[L::NS];
+        load_row<DMA, ST, DP>(q, at(p.q, s.batch, s.q0 + query, head), on, p.dim, h);
+        dev::dma_wait_barrier<0>();
+        KeyFrags<ST, DP> fk;
+        ValueFrags<ST, DP> fv;
+        f32x16 x{};
+        auto first_k = run.read_k(lds, lane);
+        fk.fill(first_k);
+        fk.run(first_k, [&](int i, const Frag<ST>& a) { mma<ST>(x, a, q[i]); });
+        if (kRows > n_all) run.hide(x, n_lane, lane);
+        if (mine > 0) run.follow(run.top(x, -INFINITY, 0, 16), c);
+        // (a tile's place in the rings is known where it is used: its reads need no addresses of
+        // their own)
+        // (x: its scores, next: those of the tile behind it)
+        auto step = [&](int t, auto place, f32x16& x, f32x16& next) __attribute__((always_inline)) {
+            const int S = place;
+            if (exact && t + R < whole) {
+                dev::dma_wait_barrier<(R - 2) * 2 * NI>();
+                share.copy(lds + VALUES + (S + R - 1) % R * TILE, vp + (t + R - 1) * (kRows * p.v.ss), v_off);
+                share.copy(lds + S * TILE, kp + (t + R) * (kRows * p.k.ss), k_off);
+            } else {
+                dev::dma_wait_barrier<0>();
+                load_v(t + R - 1, (S + R - 1) % R);
+                load_k(t + R, S);
+            }
+            if (t >= mine) return;
+            // (behind the wave's last tile the next scores are nothing's, and not used)
+            const auto read_k = run.read_k(lds + (S + 1) % R * TILE, lane);
+            const auto read_v = run.read_v(lds + VALUES + S * TILE, lane);
+            const float mc = run.base(c);
+            constexpr int N = L::NS, E = 4;  // E: exponentials while the first keys are on their way
+            Frag<ST> pr[2];
+            next = f32x16{};
+            fk.fill(read_k);
+            run.exponentials(x, pr, c, mc, 0, E);
+            fk.run(read_k, [&](int i, const Frag<ST>& a) {
+                mma<ST>(next, a, q[i]);
+                run.exponentials(x, pr, c, mc, (E + (16 - E) * i / N) & ~1, (E + (16 - E) * (i + 1) / N) & ~1);
+            });
+            fv.fill(read_v);
+            if ((t + 2) * kRows > n_all) run.hide(next, n_lane - (t + 1) * kRows, lane);
+            float top = -INFINITY;
+            fv.run(read_v, [&](int i, const Frag<ST>& a) {
+                mma<ST>(run.o[i % L::DT], a, pr[i / L::DT]);
+                top = run.top(next, top, (16 * i / N) & ~1, (16 * (i + 1) / N) & ~1);
+            });
+            if (t + 1 < mine) run.follow(top, c);
+        };
+        f32x16 y;
+        if constexpr (ST == GemmStore::F32 || DP > 128) {  // (copies of the step cost registers)
+            for (int t = 0; t < tiles; ++t) {
+                step(t, t % R, x, y);
+                x = y;
+            }
+        } else {
+            for (int t = 0; t < tiles; t += R) {
+                step(t, std::integral_constant<int, 0>{}, x, y);
+                if (t + 1 < tiles) step(t + 1, std::integral_constant<int, 1>{}, y, x);
+                if (t + 2 < tiles) step(t + 2, std::integral_constant<int, 2>{}, x, y);
+                if (t + 3 < tiles) step(t + 3, std::integral_constant<int, 3>{}, y, x);
+            }
         }
     }
     if (!exists) return;
-    const float l = add_halves(run.l);
+    const float l = add_halves(run.l + run.l2);
     store_row<DMA, ST>(at(p.o, s.batch, s.q0 + query, head), run.o, on && l != 0.f, 1.f / l, p.dim, h);
     if (h == 0)
         p.lse[((int64_t)s.batch * p.q_len + s.q0 + query) * ((int64_t)p.hk * G) + head] =
@@ -181,7 +266,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     const int query = (lane & 31) / G, head = kh * G + (lane & 31) - query * G;
     const bool exists = (lane & 31) < rows, on = query < s.nq;
     Frag<ST> q[L::NS];
-    load_row<ST, DP>(q, at(p.q, s.batch, s.q0 + query, head), on && exists, p.dim, h);
+    load_row<DMA, ST, DP>(q, at(p.q, s.batch, s.q0 + query, head), on && exists, p.dim, h);
 
     const int n = s.nq > 0 ? visible(p, s, s.nq - 1) : 0, n_all = visible(p, s, 0), n_lane = on && exists ? visible(p, s, query) : 0;
     const int tiles = (n + kRows - 1) / kRows, turns = (tiles + p.splits * W - 1) / (p.splits * W);
@@ -206,6 +291,8 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
             for (int i = 16 * lane; i < 4 * TILE; i += 16 * 64) *reinterpret_cast<u32x4*>(mine + i) = u32x4{};
             wave_wait<0>();
         }
+        KeyFrags<ST, DP> fk;
+        ValueFrags<ST, DP> fv;
         load(0, first);
         int buf = 0;
         for (int t = first; t < end; ++t, buf ^= 1) {
@@ -220,10 +307,20 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
                 wave_wait<0>();
             }
             const uint8_t* const at_k = mine + buf * 2 * TILE;
-            run.template keys<1>(at_k, at_k + TILE, q, c, (t + 1) * kRows > n_all, n_lane - t * kRows, lane);
+            f32x16 x{};
+            const auto read_k = run.read_k(at_k, lane);
+            const auto read_v = run.read_v(at_k + TILE, lane);
+            fk.fill(read_k);
+            fk.run(read_k, [&](int i, const Frag<ST>& a) { mma<ST>(x, a, q[i]); });
+            fv.fill(read_v);
+            if ((t + 1) * kRows > n_all) run.hide(x, n_lane - t * kRows, lane);
+            run.follow(run.top(x, -INFINITY, 0, 16), c);
+            Frag<ST> pr[2];
+            run.exponentials(x, pr, c, run.base(c), 0, 16);
+            fv.run(read_v, [&](int i, const Frag<ST>& a) { mma<ST>(run.o[i % L::DT], a, pr[i / L::DT]); });
         }
     }
-    run.l = add_halves(run.l);
+    run.l = add_halves(run.l + run.l2);
     __syncthreads();
     float* const sums = reinterpret_cast<float*>(lds);
     float* const own = sums + (wave * kRows + (lane & 31)) * DS;
@@ -403,7 +500,7 @@ AttnArgs attn_args(const himuon_attn_t* a)
 }
 
 // Strides in bytes. `given`: whether there is an element at all; `dma`: cleared if rows are not
-// 16-byte aligned, or a tile's rows lie too far apart for 32-bit offsets.
+// 16-byte aligned, or a sequence's too far apart for 32-bit offsets.
 bool set_heads(Heads& t, const himuon_heads_t* h, const himuon_attn_t* a, int64_t tokens, int heads, bool output, bool* dma)
 {
     t = Heads{};
@@ -422,7 +519,9 @@ bool set_heads(Heads& t, const himuon_heads_t* h, const himuon_attn_t* a, int64_
     t.sh = h->stride_head * es;
     const int64_t group = a->q_heads / a->k_heads;
     if (((uintptr_t)t.ptr | (uintptr_t)t.sb | (uintptr_t)t.ss | (uintptr_t)t.sh | (uintptr_t)(a->head_dim * es)) & 15) *dma = false;
-    if (t.ss < 0 || t.sh < 0 || t.ss > INT64_C(1) << 24 || t.sh * group > INT64_C(1) << 31) *dma = false;
+    // (offsets in a sequence, and in a tile of 64 rows)
+    if (t.ss < 0 || t.sh < 0 || t.ss > INT64_C(1) << 24 || t.sh > INT64_C(1) << 30 || tokens * t.ss + group * t.sh > UINT32_MAX - (INT64_C(1) << 28))
+        *dma = false;
     return true;
 }
 

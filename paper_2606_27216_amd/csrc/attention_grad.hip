@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace himuon {
 namespace attn {
@@ -19,8 +20,30 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64, kTileRows = kRows * kWaves;
 
-// Keys of a tile that all waves read.
-template <GemmStore ST, int DP> constexpr int tile_keys() { return DP * (ST == GemmStore::BF16 ? 2 : 4) <= 256 ? 64 : 32; }
+// Tiles of 32 rows lie in a ring of LDS buffers. A tile's g v^T goes out beside its exponentials, and
+// in bf16 the next tile's scores beside its ds, as long as registers hold both; fp32 products take
+// sixteen times as long, and ds does not weigh.
+template <GemmStore ST, int DP> constexpr bool ahead() { return ST == GemmStore::BF16 && DP <= 128; }
+template <GemmStore ST, int DP> constexpr int ring() { return ahead<ST, DP>() ? 4 : 2; }
+
+// x = rows of a tile in LDS times 32 rows held as fragments; `work(i)` goes out beside the products,
+// i = 0 .. NS - 1.
+template <GemmStore ST, int DP, class Work>
+HM_DEV void row_product(f32x16& x, const uint8_t* tile, const Frag<ST> (&f)[DP / 16], int lane, Work work)
+{
+    using L = Lay<ST, DP>;
+    auto read = [=](int i) __attribute__((always_inline)) { return L::row_frag(tile, lane & 31, i, lane >> 5); };
+    Ahead<Frag<ST>, DP / 16, kDepth<ST, DP>> r;
+    x = f32x16{};
+    r.fill(read);
+    r.run(read, [&](int i, const Frag<ST>& a) {
+        mma<ST>(x, a, f[i]);
+        work(i);
+    });
+}
+
+// The part of 16 elements, in pairs, that step i of N does.
+template <int N> HM_DEV constexpr int share_of(int i) { return (16 * i / N) & ~1; }
 
 // Row of a group's heads in `stats`.
 HM_DEV int64_t stat_row(const AttnArgs& p, const Seq& s, int kh, int64_t r)
@@ -31,13 +54,13 @@ HM_DEV int64_t stat_row(const AttnArgs& p, const Seq& s, int kh, int64_t r)
 
 // Columns of a result are cut into this many parts, each a block's, where registers hold no more.
 template <GemmStore ST, int DP> constexpr int q_parts() { return ST == GemmStore::F32 && DP == 256 ? 4 : 1; }
-template <GemmStore ST, int DP> constexpr int kv_parts() { return DP < 256 ? 1 : ST == GemmStore::F32 ? 4 : 2; }
+template <GemmStore ST, int DP> constexpr int kv_parts() { return DP < 256 ? 1 : ST == GemmStore::F32 ? 8 : 2; }
 
-template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThreads) attn_grad_q(const AttnArgs p)
+template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThreads, (ahead<ST, DP>() ? 2 : 1)) attn_grad_q(const AttnArgs p)
 {
     using L = Lay<ST, DP>;
-    constexpr int BN = tile_keys<ST, DP>(), TILE = BN * L::PITCH, PARTS = q_parts<ST, DP>(), DT = L::DT / PARTS;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TILE];  // [2][keys, values]
+    constexpr int R = ring<ST, DP>(), TILE = kRows * L::PITCH, PARTS = q_parts<ST, DP>(), DT = L::DT / PARTS, VALUES = R * TILE;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * R * TILE];  // [R] keys, [R] values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
@@ -49,24 +72,24 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
     const int64_t at_item = w - kh * items;
     const int64_t tile = p.packed ? items - 1 - at_item : at_item / p.slots * p.slots + (p.slots - 1 - at_item % p.slots);
     const Seq s = find_seq<false, kTileRows>(p, tile, G);
-    const int64_t rows = (int64_t)s.q_cap * G, r0 = (int64_t)s.tile * kTileRows;
+    const int rows = s.q_cap * G, r0 = s.tile * kTileRows;  // (a sequence's rows are counted in 32 bits)
     if (r0 >= rows) return;
 
-    const int64_t r = r0 + wave * kRows + (lane & 31);
+    const int r = r0 + wave * kRows + (lane & 31);
     const int query = (int)((uint32_t)r / (uint32_t)G);
     const int head = kh * G + (int)((uint32_t)r - (uint32_t)query * (uint32_t)G);
     const bool exists = r < rows;
     const int n_lane = query < s.nq ? visible(p, s, query) : 0;
     const bool on = n_lane > 0;  // (a row that sees nothing has no gradient)
     Frag<ST> q[L::NS], g[L::NS];
-    load_row<ST, DP>(q, at(p.q, s.batch, s.q0 + query, head), on, p.dim, h);
-    load_row<ST, DP>(g, at(p.g, s.batch, s.q0 + query, head), on, p.dim, h);
+    load_row<DMA, ST, DP>(q, at(p.q, s.batch, s.q0 + query, head), on, p.dim, h);
+    load_row<DMA, ST, DP>(g, at(p.g, s.batch, s.q0 + query, head), on, p.dim, h);
     float d = 0.f;
     const uint8_t* const o_row = at(p.o, s.batch, s.q0 + query, head);
 #pragma unroll
     for (int i = 0; i < L::NS; i += 4) {
         Frag<ST> o[4];
-        load_row<ST, 64>(o, o_row + 16 * i * L::ES, on, p.dim - 16 * i, h);
+        load_row<DMA, ST, 64>(o, o_row + 16 * i * L::ES, on, p.dim - 16 * i, h);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -79,62 +102,105 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
     const float lse = on ? p.lse[((int64_t)s.batch * p.q_len + s.q0 + query) * ((int64_t)p.hk * G) + head] * kLog2e : INFINITY;
     if (exists && h == 0 && t0 == 0) p.stats[stat_row(p, s, kh, r)] = float2{lse, d};
 
-    const int last = min((int)((r0 + kTileRows - 1) / G), s.nq - 1);
-    const int n_block = s.nq > 0 && r0 < (int64_t)s.nq * G ? visible(p, s, last) : 0;
-    const int64_t w0 = r0 + wave * kRows;
-    const int n_wave = w0 < (int64_t)s.nq * G ? visible(p, s, min((int)((w0 + kRows - 1) / G), s.nq - 1)) : 0;
-    const int n_all = visible(p, s, (int)(w0 / G));
+    // tiles of keys that the block's and the wave's rows see; keys seen by all of the wave's rows
+    const int w0 = r0 + wave * kRows, in_use = s.nq * G;
+    auto seen = [&](int row) { return row < in_use ? visible(p, s, (int)((uint32_t)row / (uint32_t)G)) : 0; };
+    const int tiles = (seen(min(r0 + kTileRows, in_use) - 1) + kRows - 1) / kRows * (r0 < in_use);
+    const int mine = (seen(min(w0 + kRows, in_use) - 1) + kRows - 1) / kRows * (w0 < in_use);
+    const int n_all = seen(w0), whole = min(tiles, s.nk / kRows);
 
     f32x16 dq[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) dq[t] = f32x16{};
     const int row_bytes = p.dim * L::ES;
     const uint8_t *kp = at(p.k, s.batch, s.k0, kh), *vp = at(p.v, s.batch, s.k0, kh);
-    const Share<ST, DP, BN, kThreads> share{(int)threadIdx.x};
-    auto load = [&](int buf, int j0) __attribute__((always_inline)) {
-        uint8_t* const t = lds + buf * 2 * TILE;
-        const bool whole = j0 + BN <= s.nk;
-        auto in = [&](int i) { return j0 + share.row(i) < s.nk; };
-        share.template stage<DMA>(t, kp + j0 * p.k.ss, row_bytes, whole, [&](int i) { return share.row(i) * p.k.ss; }, in);
-        share.template stage<DMA>(t + TILE, vp + j0 * p.v.ss, row_bytes, whole, [&](int i) { return share.row(i) * p.v.ss; }, in);
-    };
-    auto keys = [&](const uint8_t* kt, const uint8_t* vt, bool masked, int left) __attribute__((always_inline)) {
-        f32x16 x{}, y{};
-        ahead<L::NS>([&](int i) { return Pair<ST>{L::row_frag(kt, lane & 31, i, h), L::row_frag(vt, lane & 31, i, h)}; },
-                     [&](int i, const Pair<ST>& f) {
-                         mma<ST>(x, f.a, q[i]);
-                         mma<ST>(y, f.b, g[i]);
-                     });
+    const Share<ST, DP, kRows, kThreads> share{(int)threadIdx.x};
+    constexpr int NI = Share<ST, DP, kRows, kThreads>::NI;
+    const bool exact = DMA && row_bytes == L::PITCH;
+    uint32_t k_off[NI], v_off[NI];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float pr = __builtin_amdgcn_exp2f(fmaf(x[i], c, -lse));
-            y[i] = pr * (y[i] - d);
-        }
-        if (masked) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = result_row(i, h) < left ? y[i] : 0.f;
-        }
-        const Frag<ST> ds[2] = {as_operand<ST>(y, 0), as_operand<ST>(y, 1)};
-        ahead<2 * DT>([&](int i) { return L::col_frag(kt, 16 * (i / DT), 32 * (t0 + i % DT), lane); },
-                      [&](int i, const Frag<ST>& a) { mma<ST>(dq[i % DT], a, ds[i / DT]); });
+    for (int i = 0; i < NI; ++i) {
+        k_off[i] = share.offset(i, p.k.ss);
+        v_off[i] = share.offset(i, p.v.ss);
+    }
+    auto load = [&](int t, int place) __attribute__((always_inline)) {
+        if (t >= tiles) return;
+        auto in = [&](int i) { return t * kRows + share.row(i) < s.nk; };
+        share.template stage<DMA>(lds + place * TILE, kp + t * (kRows * p.k.ss), row_bytes, t < whole, [&](int i) { return share.row(i) * p.k.ss; }, in);
+        share.template stage<DMA>(lds + VALUES + place * TILE, vp + t * (kRows * p.v.ss), row_bytes, t < whole,
+                                  [&](int i) { return share.row(i) * p.v.ss; }, in);
     };
-    if (n_block > 0) {
+    // hides the keys that this lane's row does not see
+    auto hide = [&](f32x16& x, int t, float with) __attribute__((always_inline)) {
+        if ((t + 1) * kRows <= n_all) return;
+        const int left = n_lane - t * kRows - 4 * h;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = result_row(i, 0) < left ? x[i] : with;
+    };
+    // (x: the tile's scores, next: those of the tile behind it)
+    auto step = [&](int t, auto place, f32x16& x, f32x16& next) __attribute__((always_inline)) {
+        const int S = place;
+        if (exact && t + R - 1 < whole) {
+            dev::dma_wait_barrier<(R > 3 ? R - 3 : 0) * 2 * NI>();
+            share.copy(lds + (S + R - 1) % R * TILE, kp + (t + R - 1) * (kRows * p.k.ss), k_off);
+            share.copy(lds + VALUES + (S + R - 1) % R * TILE, vp + (t + R - 1) * (kRows * p.v.ss), v_off);
+        } else {
+            dev::dma_wait_barrier<0>();
+            load(t + R - 1, (S + R - 1) % R);
+        }
+        if (t >= mine) return;
+        auto tile = [&](int u) { return lds + u % R * TILE; };
+        if (!ahead<ST, DP>() || t == 0) {
+            row_product<ST, DP>(x, tile(S), q, lane, [](int) {});
+            hide(x, t, -INFINITY);
+        }
+        f32x16 y;
+        row_product<ST, DP>(y, tile(S) + VALUES, g, lane, [&](int j) {
+#pragma unroll
+            for (int i = share_of<L::NS>(j); i < share_of<L::NS>(j + 1); ++i) {
+                x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -lse));
+                settle(x, i);
+            }
+        });
+        hide(y, t, d);
+        auto read = [&](int i) __attribute__((always_inline)) { return L::col_frag(tile(S), 16 * (i / DT), 32 * (t0 + i % DT), lane); };
+        Ahead<Frag<ST>, 2 * DT, kDepth<ST, DP>> cols;
+        Frag<ST> ds[2];
+        auto work = [&](int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = from; i < to; i += 2) {
+                set_pair<ST>(ds, i / 2, x[i] * (y[i] - d), x[i + 1] * (y[i + 1] - d));
+                settle_pair<ST>(ds, i / 2);
+            }
+        };
+        if constexpr (ahead<ST, DP>()) {  // (behind the wave's last tile the next scores are nothing's, and not used)
+            row_product<ST, DP>(next, tile(S + 1), q, lane, [&](int j) { work(share_of<L::NS>(j), share_of<L::NS>(j + 1)); });
+            cols.fill(read);
+            hide(next, t + 1, -INFINITY);
+        } else {
+            cols.fill(read);
+            work(0, 16);
+        }
+        cols.run(read, [&](int i, const Frag<ST>& f) { mma<ST>(dq[i % DT], f, ds[i / DT]); });
+    };
+    if (tiles > 0) {
         if (DMA && p.dim < DP) {
-            clear_lds<kThreads>(lds, 4 * TILE);
+            clear_lds<kThreads>(lds, 2 * R * TILE);
             __syncthreads();
         }
-        load(0, 0);
-        int buf = 0;
-        for (int j0 = 0; j0 < n_block; j0 += BN, buf ^= 1) {
-            dev::dma_wait_barrier<0>();
-            if (j0 + BN < n_block) load(buf ^ 1, j0 + BN);
-            const uint8_t* const t = lds + buf * 2 * TILE;
-#pragma unroll 1
-            for (int j = 0; j < BN; j += kRows) {
-                if (j0 + j >= n_wave) break;
-                const uint8_t* const kt = t + j * L::PITCH;
-                keys(kt, kt + TILE, j0 + j + kRows > n_all, n_lane - j0 - j);
+#pragma unroll
+        for (int t = 0; t < R - 1; ++t) load(t, t);
+        dev::dma_wait_barrier<0>();
+        f32x16 x, x2;
+        if constexpr (ahead<ST, DP>()) {
+            for (int t = 0; t < tiles; t += R) {
+                step(t, std::integral_constant<int, 0>{}, x, x2);
+                if (t + 1 < tiles) step(t + 1, std::integral_constant<int, 1>{}, x2, x);
+                if (t + 2 < tiles) step(t + 2, std::integral_constant<int, 2>{}, x, x2);
+                if (t + 3 < tiles) step(t + 3, std::integral_constant<int, 3>{}, x2, x);
             }
+        } else {
+            for (int t = 0; t < tiles; ++t) step(t, t % R, x, x2);
         }
     }
     if (!exists) return;
@@ -144,8 +210,8 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
 template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThreads) attn_grad_kv(const AttnArgs p)
 {
     using L = Lay<ST, DP>;
-    constexpr int BR = kRows, TILE = BR * L::PITCH, PARTS = kv_parts<ST, DP>(), DT = L::DT / PARTS, BUF = 2 * TILE + BR * 8;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * BUF];  // [2][rows of q, of g, {lse, D}]
+    constexpr int R = ring<ST, DP>(), BR = kRows, TILE = BR * L::PITCH, PARTS = kv_parts<ST, DP>(), DT = L::DT / PARTS, BUF = 2 * TILE + BR * 8;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[R * BUF];  // [R][rows of q, of g, their lse, their D]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
@@ -160,87 +226,195 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
     const int key = j0 + wave * kRows + (lane & 31);
     const bool exists = key < s.k_cap, on = key < s.nk;
     Frag<ST> k[L::NS], v[L::NS];
-    load_row<ST, DP>(k, at(p.k, s.batch, s.k0 + key, kh), on, p.dim, h);
-    load_row<ST, DP>(v, at(p.v, s.batch, s.k0 + key, kh), on, p.dim, h);
+    load_row<DMA, ST, DP>(k, at(p.k, s.batch, s.k0 + key, kh), on, p.dim, h);
+    load_row<DMA, ST, DP>(v, at(p.v, s.batch, s.k0 + key, kh), on, p.dim, h);
 
-    // rows that see keys of the block, of the wave, this lane's and all of the wave's
-    const int off = s.nk - s.nq;
-    auto first_row = [&](int j) { return p.causal ? (int64_t)max(0, j - off) * G : (int64_t)0; };
-    const int64_t end = j0 < s.nk ? (int64_t)s.nq * G : 0;
-    const int64_t begin = first_row(j0) / BR * BR, w_begin = first_row(j0 + wave * kRows);
-    const int64_t w_all = first_row(j0 + wave * kRows + kRows - 1), mine = on ? first_row(key) : INT64_MAX;
-    const bool w_on = j0 + wave * kRows < s.nk, w_whole = j0 + wave * kRows + kRows <= s.nk;
+    // rows that see keys of the block, of the wave, this lane's and all of the wave's (a
+    // sequence's rows are counted in 32 bits)
+    const int off = s.nk - s.nq, wj = j0 + wave * kRows;
+    auto first_row = [&](int j) { return p.causal ? max(0, j - off) * G : 0; };
+    const int end = j0 < s.nk ? s.nq * G : 0, begin = first_row(j0) / BR * BR;
+    const bool w_whole = wj + kRows <= s.nk;
+    const int w_begin = wj < s.nk ? first_row(wj) : INT32_MAX, w_all = w_whole ? first_row(wj + kRows - 1) : INT32_MAX;
+    const int mine = on ? first_row(key) : INT32_MAX;
 
     f32x16 dk[DT], dv[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) dk[t] = dv[t] = f32x16{};
     const float c = p.scale * kLog2e;
     const int row_bytes = p.dim * L::ES;
+    // Where this thread's rows of the next tile lie: their place in the group and offsets (with
+    // copy()'s own part), moved on by a tile's rows each time. (Without DMA each is worked out.)
     const Share<ST, DP, BR, kThreads> share{(int)threadIdx.x};
-    const float2* const stats = p.stats + stat_row(p, s, kh, 0);
-    auto load = [&](int buf, int64_t r0) __attribute__((always_inline)) {
-        uint8_t* const t = lds + buf * BUF;
-        const bool whole = r0 + BR <= end;
-        const int q0 = (int)(r0 / G), g0 = (int)(r0 - (int64_t)q0 * G);
-        const uint8_t *qp = at(p.q, s.batch, s.q0 + q0, kh * G), *gp = at(p.g, s.batch, s.q0 + q0, kh * G);
-        auto in = [&](int i) { return r0 + share.row(i) < end; };
-        auto place = [&](int i, const Heads& x) {
-            const int r = g0 + share.row(i), dq = (int)((uint32_t)r / (uint32_t)G);
-            return dq * x.ss + (r - dq * G) * x.sh;
-        };
-        share.template stage<DMA>(t, qp, row_bytes, whole, [&](int i) { return place(i, p.q); }, in);
-        share.template stage<DMA>(t + TILE, gp, row_bytes, whole, [&](int i) { return place(i, p.g); }, in);
-        if (whole) {
-            if (wave == 0) dev::dma4((uint32_t)__builtin_amdgcn_readfirstlane((int)dev::lds_offset(t + 2 * TILE)), 4 * lane, dev::uniform_address(stats + r0));
-        } else if (threadIdx.x < BR)
-            reinterpret_cast<float2*>(t + 2 * TILE)[threadIdx.x] = r0 + threadIdx.x < end ? stats[r0 + threadIdx.x] : float2{INFINITY, 0.f};
+    constexpr int NI = Share<ST, DP, BR, kThreads>::NI;
+    const uint8_t *const qp = at(p.q, s.batch, s.q0, kh * G), *const gp = at(p.g, s.batch, s.q0, kh * G);
+    const int step_q = BR / G, step_g = BR - step_q * G;
+    const uint32_t q_step = (uint32_t)(step_q * p.q.ss + step_g * p.q.sh), g_step = (uint32_t)(step_q * p.g.ss + step_g * p.g.sh);
+    const uint32_t q_wrap = (uint32_t)(p.q.ss - G * p.q.sh), g_wrap = (uint32_t)(p.g.ss - G * p.g.sh);
+    auto offset = [&](int r, const Heads& x) {
+        const uint32_t token = (uint32_t)r / (uint32_t)G;
+        return token * x.ss + (int64_t)((uint32_t)r - token * (uint32_t)G) * x.sh;
     };
-    auto rows = [&](const uint8_t* qt, const float2* st, int64_t r0, bool masked) __attribute__((always_inline)) {
-        const uint8_t* const gt = qt + TILE;
-        f32x16 x{}, y{};
-        ahead<L::NS>([&](int i) { return Pair<ST>{L::row_frag(qt, lane & 31, i, h), L::row_frag(gt, lane & 31, i, h)}; },
-                     [&](int i, const Pair<ST>& f) {
-                         mma<ST>(x, f.a, k[i]);
-                         mma<ST>(y, f.b, v[i]);
-                     });
+    int place[NI];
+    uint32_t q_off[NI], g_off[NI];
+    if constexpr (DMA) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float2 a = st[result_row(i, h)];
-            x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -a.x));
-            y[i] = x[i] * (y[i] - a.y);
+        for (int i = 0; i < NI; ++i) {
+            place[i] = (begin + share.row(i)) % G;
+            q_off[i] = (uint32_t)offset(begin + share.row(i), p.q) + share.rest(i);
+            g_off[i] = (uint32_t)offset(begin + share.row(i), p.g) + share.rest(i);
         }
-        if (masked) {
-            const int hidden = (int)min(mine - r0, (int64_t)BR);  // rows that do not see this lane's key
+    }
+    auto advance = [&]() __attribute__((always_inline)) {
+        if constexpr (DMA) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                x[i] = result_row(i, h) < hidden ? 0.f : x[i];
-                y[i] = result_row(i, h) < hidden ? 0.f : y[i];
+            for (int i = 0; i < NI; ++i) {
+                place[i] += step_g;
+                const bool wrap = place[i] >= G;
+                place[i] -= wrap ? G : 0;
+                q_off[i] += q_step + (wrap ? q_wrap : 0);
+                g_off[i] += g_step + (wrap ? g_wrap : 0);
             }
         }
-        const Frag<ST> pr[2] = {as_operand<ST>(x, 0), as_operand<ST>(x, 1)}, ds[2] = {as_operand<ST>(y, 0), as_operand<ST>(y, 1)};
-        ahead<2 * DT>(
-            [&](int i) {
-                return Pair<ST>{L::col_frag(gt, 16 * (i / DT), 32 * (t0 + i % DT), lane), L::col_frag(qt, 16 * (i / DT), 32 * (t0 + i % DT), lane)};
-            },
-            [&](int i, const Pair<ST>& f) {
-                mma<ST>(dv[i % DT], f.a, pr[i / DT]);
-                mma<ST>(dk[i % DT], f.b, ds[i / DT]);
-            });
     };
-    if (begin < end) {
+    const float2* const stats = p.stats + stat_row(p, s, kh, 0);
+    const int tiles = end > begin ? (end - begin + BR - 1) / BR : 0, whole = (end - begin) / BR;
+    const bool exact = DMA && row_bytes == L::PITCH;
+    auto load_stats = [&](uint8_t* to, int r0) __attribute__((always_inline)) {  // (by every wave, so that all count the same)
+        dev::dma4((uint32_t)__builtin_amdgcn_readfirstlane((int)dev::lds_offset(to)), 8 * (lane & 31) + 4 * h, dev::uniform_address(stats + r0));
+    };
+    auto load = [&](int t, int slot) __attribute__((always_inline)) {
+        if (t >= tiles) return;
+        uint8_t* const to = lds + slot * BUF;
+        const int r0 = begin + t * BR;
+        auto in = [&](int i) { return r0 + share.row(i) < end; };
+        share.template stage<DMA>(to, qp, row_bytes, t < whole, [&](int i) {
+            if constexpr (DMA) return q_off[i] - share.rest(i);
+            else return offset(r0 + share.row(i), p.q);
+        }, in);
+        share.template stage<DMA>(to + TILE, gp, row_bytes, t < whole, [&](int i) {
+            if constexpr (DMA) return g_off[i] - share.rest(i);
+            else return offset(r0 + share.row(i), p.g);
+        }, in);
+        if (t < whole) {
+            load_stats(to + 2 * TILE, r0);
+        } else if (threadIdx.x < BR) {
+            const float2 st = r0 + (int)threadIdx.x < end ? stats[r0 + threadIdx.x] : float2{INFINITY, 0.f};
+            reinterpret_cast<float*>(to + 2 * TILE)[threadIdx.x] = st.x;
+            reinterpret_cast<float*>(to + 2 * TILE)[BR + threadIdx.x] = st.y;
+        }
+        advance();
+    };
+    // hides the rows that do not see this lane's key
+    auto hide = [&](f32x16& x, int t, float with) __attribute__((always_inline)) {
+        const int r0 = begin + t * BR;
+        if (r0 >= w_all) return;
+        const int hidden = min(mine - r0, BR) - 4 * h;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = result_row(i, 0) < hidden ? with : x[i];
+    };
+    const int first = w_begin == INT32_MAX ? INT32_MAX : max(0, w_begin - begin) / BR;  // the wave's first tile
+    Ahead<Frag<ST>, L::NS, kDepth<ST, DP>> ry;
+    // (x: the tile's scores, next: those of the tile behind it)
+    auto step = [&](int t, auto slot, f32x16& x, f32x16& next) __attribute__((always_inline)) {
+        const int S = slot;
+        if (exact && t + R - 1 < whole) {
+            dev::dma_wait_barrier<(R > 3 ? R - 3 : 0) * (2 * NI + 1)>();
+            uint8_t* const to = lds + (S + R - 1) % R * BUF;
+            if constexpr (DMA) {
+                share.copy(to, qp, q_off);
+                share.copy(to + TILE, gp, g_off);
+            }
+            load_stats(to + 2 * TILE, begin + (t + R - 1) * BR);
+            advance();
+        } else {
+            dev::dma_wait_barrier<0>();
+            load(t + R - 1, (S + R - 1) % R);
+        }
+        if (t < first) return;
+        // Every product's first reads go out beside the product before (a lone wave has nothing else
+        // to wait with): `ry` those of g v^T, for the next step too.
+        auto tile = [&](int u) { return lds + u % R * BUF; };
+        auto read_rows = [&](const uint8_t* from) { return [=](int i) __attribute__((always_inline)) { return L::row_frag(from, lane & 31, i, h); }; };
+        auto read_cols = [&](const uint8_t* from) {
+            return [=](int i) __attribute__((always_inline)) { return L::col_frag(from, 16 * (i / DT), 32 * (t0 + i % DT), lane); };
+        };
+        const auto read_y = read_rows(tile(S) + TILE), read_next = read_rows(tile(S + 1)), read_y2 = read_rows(tile(S + 1) + TILE);
+        const auto read_g = read_cols(tile(S) + TILE), read_q = read_cols(tile(S));
+        Ahead<Frag<ST>, L::NS, kDepth<ST, DP>> rn;
+        Ahead<Frag<ST>, 2 * DT, kDepth<ST, DP>> cols_g, cols_q;
+        if (!ahead<ST, DP>() || t == first) {
+            row_product<ST, DP>(x, tile(S), k, lane, [](int) {});
+            ry.fill(read_y);
+            hide(x, t, -INFINITY);
+        }
+        const float* const st = reinterpret_cast<const float*>(tile(S) + 2 * TILE) + 4 * h;
+        f32x4 row[4];
+        auto rows_of = [&](const float* from) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) row[i] = *reinterpret_cast<const f32x4*>(from + 8 * i);
+        };
+        f32x16 y{};
+        Frag<ST> pr[2], ds[2];
+        rows_of(st);
+        if constexpr (ahead<ST, DP>()) rn.fill(read_next);
+        ry.run(read_y, [&](int j, const Frag<ST>& f) {
+            mma<ST>(y, f, v[j]);
+#pragma unroll
+            for (int i = share_of<L::NS>(j); i < share_of<L::NS>(j + 1); i += 2) {
+                x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -row[i >> 2][i & 3]));
+                x[i + 1] = __builtin_amdgcn_exp2f(fmaf(x[i + 1], c, -row[i >> 2][(i & 3) + 1]));
+                settle(x, i);
+                settle(x, i + 1);
+                set_pair<ST>(pr, i / 2, x[i], x[i + 1]);
+                settle_pair<ST>(pr, i / 2);
+            }
+        });
+        rows_of(st + BR);
+        hide(y, t, 0.f);
+        if constexpr (ahead<ST, DP>()) cols_g.fill(read_g);
+        auto work = [&](int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = from; i < to; i += 2) {
+                set_pair<ST>(ds, i / 2, x[i] * (y[i] - row[i >> 2][i & 3]), x[i + 1] * (y[i + 1] - row[i >> 2][(i & 3) + 1]));
+                settle_pair<ST>(ds, i / 2);
+            }
+        };
+        if constexpr (ahead<ST, DP>()) {  // (behind the last tile the next scores are nothing's, and not used)
+            next = f32x16{};
+            rn.run(read_next, [&](int j, const Frag<ST>& f) {
+                mma<ST>(next, f, k[j]);
+                work(share_of<L::NS>(j), share_of<L::NS>(j + 1));
+            });
+            cols_q.fill(read_q);
+            hide(next, t + 1, -INFINITY);
+        } else {
+            work(0, 16);
+            cols_g.fill(read_g);
+        }
+        cols_g.run(read_g, [&](int i, const Frag<ST>& f) { mma<ST>(dv[i % DT], f, pr[i / DT]); });
+        if constexpr (ahead<ST, DP>()) ry.fill(read_y2);
+        else cols_q.fill(read_q);
+        cols_q.run(read_q, [&](int i, const Frag<ST>& f) { mma<ST>(dk[i % DT], f, ds[i / DT]); });
+    };
+    if (tiles > 0) {
         if (DMA && p.dim < DP) {
-            clear_lds<kThreads>(lds, 2 * BUF);
+            clear_lds<kThreads>(lds, R * BUF);
             __syncthreads();
         }
-        load(0, begin);
-        int buf = 0;
-        for (int64_t r0 = begin; r0 < end; r0 += BR, buf ^= 1) {
-            dev::dma_wait_barrier<0>();
-            if (r0 + BR < end) load(buf ^ 1, r0 + BR);
-            if (!w_on || r0 + BR <= w_begin) continue;
-            const uint8_t* const t = lds + buf * BUF;
-            const float2* const st = reinterpret_cast<const float2*>(t + 2 * TILE);
-            rows(t, st, r0, r0 < w_all || !w_whole);
+#pragma unroll
+        for (int t = 0; t < R - 1; ++t) load(t, t);
+        dev::dma_wait_barrier<0>();
+        f32x16 x, x2;
+        if constexpr (ahead<ST, DP>()) {
+            for (int t = 0; t < tiles; t += R) {
+                step(t, std::integral_constant<int, 0>{}, x, x2);
+                if (t + 1 < tiles) step(t + 1, std::integral_constant<int, 1>{}, x2, x);
+                if (t + 2 < tiles) step(t + 2, std::integral_constant<int, 2>{}, x, x2);
+                if (t + 3 < tiles) step(t + 3, std::integral_constant<int, 3>{}, x2, x);
+            }
+        } else {
+            for (int t = 0; t < tiles; ++t) step(t, t % R, x, x2);
         }
     }
     if (!exists) return;

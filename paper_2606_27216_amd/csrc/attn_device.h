@@ -62,10 +62,6 @@ template <GemmStore ST> HM_DEV void mma(f32x16& acc, const Frag<ST>& a, const Fr
     }
 }
 
-template <GemmStore ST> struct Pair {
-    Frag<ST> a, b;
-};
-
 // Registers 8 t .. 8 t + 7 of a result as the second operand of the next product. (bf16:
 // rounded to nearest even, at most 2^-9 of each value; sums are taken of the unrounded ones.)
 template <GemmStore ST> HM_DEV Frag<ST> as_operand(const f32x16& c, int t)
@@ -81,13 +77,41 @@ template <GemmStore ST> HM_DEV Frag<ST> as_operand(const f32x16& c, int t)
     return f;
 }
 
+// Values 2 i and 2 i + 1 of a result's registers in that operand.
+template <GemmStore ST> HM_DEV void set_pair(Frag<ST> (&f)[2], int i, float a, float b)
+{
+    if constexpr (ST == GemmStore::BF16) {
+        f[i >> 2].w[0][i & 3] = dev::pack2<Operand::BF16>(a, b);
+    } else {
+        f[i >> 2].w[(i & 3) >> 1][2 * (i & 1)] = __float_as_uint(a);
+        f[i >> 2].w[(i & 3) >> 1][2 * (i & 1) + 1] = __float_as_uint(b);
+    }
+}
+
+// Keeps that pair's computation where it stands (the compiler would move it down to its use
+// behind the next branch, past the products that it is to run beside).
+template <GemmStore ST> HM_DEV void settle_pair(Frag<ST> (&f)[2], int i)
+{
+    if constexpr (ST == GemmStore::BF16) {
+        uint32_t w = f[i >> 2].w[0][i & 3];
+        asm volatile("" : "+v"(w));
+        f[i >> 2].w[0][i & 3] = w;
+    } else {
+        uint32_t a = f[i >> 2].w[(i & 3) >> 1][2 * (i & 1)], b = f[i >> 2].w[(i & 3) >> 1][2 * (i & 1) + 1];
+        asm volatile("" : "+v"(a), "+v"(b));
+        f[i >> 2].w[(i & 3) >> 1][2 * (i & 1)] = a;
+        f[i >> 2].w[(i & 3) >> 1][2 * (i & 1) + 1] = b;
+    }
+}
+
 template <GemmStore ST> HM_DEV float frag_value(const Frag<ST>& f, int e)
 {
     if constexpr (ST == GemmStore::BF16) return __uint_as_float((e & 1) ? (f.w[0][e >> 1] & 0xffff0000u) : (f.w[0][e >> 1] << 16));
     else return __uint_as_float(f.w[e >> 2][e & 3]);
 }
 
-// Row `r` of a result's register i in half h of the wave.
+// Row of a result's register i in half h of the wave. (Compared with a bound, it is the bound
+// less 4 h that is compared with a constant.)
 HM_DEV constexpr int result_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
 // The other half's value, combined.
@@ -157,20 +181,42 @@ template <GemmStore ST, int DP> struct Lay {
     }
 };
 
-// use(i, read(i)) for i = 0 .. N - 1, each read one step ahead of its use (and no further:
-// reads that the compiler moves up all at once cost the registers of a second wave).
-template <int N, class Read, class Use> HM_DEV void ahead(Read read, Use use)
-{
-    auto now = read(0);
+// use(i, read(i)) for i = 0 .. N - 1 with the reads DEPTH steps ahead of their uses, and no
+// further: reads that the compiler moves up all at once cost the registers of a second wave.
+// fill() sends the first ones out before work that does not need them. A step stays together, so
+// that a product's other half of work (a share of the vector ALU's) goes out beside it: left
+// alone, the compiler puts the products first and the exponentials behind them.
+template <class T, int N, int DEPTH> struct Ahead {
+    T f[DEPTH];
+    template <class Read> HM_DEV void fill(Read read)
+    {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        auto next = now;
-        if (i + 1 < N) next = read(i + 1);
-        use(i, now);
+        for (int i = 0; i < DEPTH; ++i)
+            if (i < N) f[i] = read(i);
         __builtin_amdgcn_sched_barrier(0);
-        now = next;
     }
+    template <class Read, class Use> HM_DEV void run(Read read, Use use)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            use(i, f[i % DEPTH]);
+            if (i + DEPTH < N) f[i % DEPTH] = read(i + DEPTH);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
+
+HM_DEV void settle(float& a) { asm volatile("" : "+v"(a)); }
+HM_DEV void settle(f32x16& x, int i)
+{
+    float a = x[i];
+    settle(a);
+    x[i] = a;
 }
+
+// Fragments in flight: an LDS read takes as long as three or four 16-bit products, and less
+// than one step's eight of fp32.
+template <GemmStore ST, int DP> constexpr int kDepth = ST == GemmStore::BF16 ? 4 : DP <= 128 ? 2 : 1;
 
 // 16 bytes of a row whose first `bytes` (> 0) count, from any address that is a multiple of
 // the element's size.
@@ -196,8 +242,8 @@ template <GemmStore ST> HM_DEV u32x4 load_chunk(const uint8_t* p, int bytes)
 }
 
 // An operand's fragments of one row in memory (zeros where it is not `on`), elements
-// 16 s + 8 h .. of it.
-template <GemmStore ST, int DP> HM_DEV void load_row(Frag<ST> (&f)[DP / 16], const uint8_t* row, bool on, int dim, int h)
+// 16 s + 8 h .. of it. VEC: whole 16-byte chunks, aligned.
+template <bool VEC, GemmStore ST, int DP> HM_DEV void load_row(Frag<ST> (&f)[DP / 16], const uint8_t* row, bool on, int dim, int h)
 {
     constexpr int ES = ST == GemmStore::BF16 ? 2 : 4, C = 16 / ES;
 #pragma unroll
@@ -205,7 +251,8 @@ template <GemmStore ST, int DP> HM_DEV void load_row(Frag<ST> (&f)[DP / 16], con
 #pragma unroll
         for (int x = 0; x < 8 / C; ++x) {
             const int d = 16 * s + 8 * h + C * x;
-            f[s].w[x] = on && d < dim ? load_chunk<ST>(row + d * ES, (dim - d) * ES) : u32x4{};
+            if constexpr (VEC) f[s].w[x] = on && d < dim ? *reinterpret_cast<const u32x4*>(row + d * ES) : u32x4{};
+            else f[s].w[x] = on && d < dim ? load_chunk<ST>(row + d * ES, (dim - d) * ES) : u32x4{};
         }
     }
 }
@@ -215,25 +262,48 @@ template <GemmStore ST, int DP> HM_DEV void load_row(Frag<ST> (&f)[DP / 16], con
 template <GemmStore ST, int DP, int ROWS, int NT> struct Share {
     using L = Lay<ST, DP>;
     static constexpr int NI = ROWS * L::CH / NT;
+    static constexpr int N = NI > 4 ? 4 : NI;  // copies that share m0
     static_assert(NI >= 1 && NI * NT == ROWS * L::CH, "");
     int tid;
-    HM_DEV int slot(int i) const { return NT * i + tid; }
+    HM_DEV int slot(int i) const { return (tid & ~63) * NI + 64 * i + (tid & 63); }
     HM_DEV int row(int i) const { return slot(i) / L::CH; }
     HM_DEV int byte(int i) const { return 16 * ((slot(i) % L::CH) ^ L::swz(row(i))); }
 
+    // Offsets of this thread's share of a tile of rows `stride` bytes apart, as copy() takes them.
+    HM_DEV uint32_t offset(int i, int64_t stride) const { return (uint32_t)(row(i) * stride) + rest(i); }
+    HM_DEV uint32_t rest(int i) const { return (uint32_t)(byte(i) + 4096 - 1024 * (i % N)); }
+
+    // A whole tile of whole rows (DP elements), by DMA.
+    HM_DEV void copy(uint8_t* tile, const uint8_t* base, const uint32_t (&off)[NI]) const
+    {
+        const uint64_t from = dev::uniform_address(base - 4096);
+        const uint32_t to = lds_place(tile);
+#pragma unroll
+        for (int i = 0; i < NI; i += N) {
+            uint32_t v[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = off[i + j];
+            dev::dma16_run<N>(to + 1024 * i, v, from);
+        }
+    }
+    HM_DEV uint32_t lds_place(uint8_t* tile) const
+    {
+        return (uint32_t)__builtin_amdgcn_readfirstlane((int)(dev::lds_offset(tile) + 16 * NI * (tid & ~63)));
+    }
+
     // Copies the rows to LDS: row i at base + off(i) (bytes), zeros where on(i) does not hold
-    // and behind the row's `row_bytes`. DMA: whole 16-byte chunks, aligned; off below 2^32; where
+    // and behind the row's `row_bytes`. DMA: whole 16-byte chunks, aligned; off below 2^32 - 2^28; where
     // the tile is `whole`, the places behind row_bytes stay as they are.
     template <bool DMA, class Off, class On>
     HM_DEV void stage(uint8_t* tile, const uint8_t* base, int row_bytes, bool whole, Off off, On on) const
     {
         if constexpr (DMA) {
             const uint64_t from = dev::uniform_address(base);
-            const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(dev::lds_offset(tile) + 16 * (tid & ~63)));
+            const uint32_t to = lds_place(tile);
 #pragma unroll(NI > 8 ? 4 : NI)
             for (int i = 0; i < NI; ++i) {
                 const int b = byte(i);
-                if ((whole || on(i)) && b < row_bytes) dev::dma16(to + 16 * NT * i, (uint32_t)off(i) + (uint32_t)b, from);
+                if ((whole || on(i)) && b < row_bytes) dev::dma16(to + 1024 * i, (uint32_t)off(i) + (uint32_t)b, from);
                 else if (!whole) *reinterpret_cast<u32x4*>(tile + 16 * slot(i)) = u32x4{};
             }
         } else {

@@ -29,6 +29,25 @@ HM_DEV void dma16(uint32_t dst, uint32_t voff, uint64_t base)
                  : "m0", "memory");
 }
 
+// N of them, to LDS bytes dst, dst + 1024, ..: the instruction's offset counts for both sides, so
+// voff[i] is 1024 i less than where lane i's bytes lie, and m0 is set once.
+template <int N> HM_DEV void dma16_run(uint32_t dst, const uint32_t (&voff)[N], uint64_t base)
+{
+    static_assert(N == 1 || N == 2 || N == 4, "");
+    if constexpr (N == 1) {
+        dma16(dst, voff[0], base);
+    } else if constexpr (N == 2) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(dst),
+                     "v"(voff[0]), "v"(voff[1]), "s"(base)
+                     : "m0", "memory");
+    } else {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(dst),
+                     "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(base)
+                     : "m0", "memory");
+    }
+}
+
 // The same with 4 bytes a lane: LDS bytes dst .. dst + 255.
 HM_DEV void dma4(uint32_t dst, uint32_t voff, uint64_t base)
 {
