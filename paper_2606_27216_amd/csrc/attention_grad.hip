@@ -42,6 +42,46 @@ HM_DEV void row_product(f32x16& x, const uint8_t* tile, const Frag<ST> (&f)[DP /
     });
 }
 
+// The same, of the first `steps` parts of 16 columns alone.
+template <GemmStore ST, int DP> HM_DEV void row_product_of(int steps, f32x16& x, const uint8_t* tile, const Frag<ST> (&f)[DP / 16], int lane)
+{
+    x = f32x16{};
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+        if (i < steps) mma<ST>(x, Lay<ST, DP>::row_frag(tile, lane & 31, i, lane >> 5), f[i]);
+    }
+}
+
+// acc[t] += columns 32 (t0 + t) .. of a tile times an operand, t below `cols`.
+template <GemmStore ST, int DP, int DT>
+HM_DEV void col_product(f32x16 (&acc)[DT], const uint8_t* tile, const Frag<ST> (&f)[2], int t0, int cols, int lane)
+{
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+        if (t < cols) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) mma<ST>(acc[t], Lay<ST, DP>::col_frag(tile, 16 * u, 32 * (t0 + t), lane), f[u]);
+        }
+    }
+}
+
+// A row in memory times one held as fragments.
+template <bool VEC, GemmStore ST, int DP> HM_DEV float row_dot(const Frag<ST> (&g)[DP / 16], const uint8_t* row, bool on, int dim, int h)
+{
+    float d = 0.f;
+#pragma unroll
+    for (int i = 0; i < DP / 16; i += 4) {
+        Frag<ST> o[4];
+        load_row<VEC, ST, 64>(o, row + 16 * i * Lay<ST, DP>::ES, on, dim - 16 * i, h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d = fmaf(frag_value<ST>(g[i + j], e), frag_value<ST>(o[j], e), d);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    return add_halves(d);
+}
+
 // The part of 16 elements, in pairs, that step i of N does.
 template <int N> HM_DEV constexpr int share_of(int i) { return (16 * i / N) & ~1; }
 
@@ -84,19 +124,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
     Frag<ST> q[L::NS], g[L::NS];
     load_row<DMA, ST, DP>(q, at(p.q, s.batch, s.q0 + query, head), on, p.dim, h);
     load_row<DMA, ST, DP>(g, at(p.g, s.batch, s.q0 + query, head), on, p.dim, h);
-    float d = 0.f;
-    const uint8_t* const o_row = at(p.o, s.batch, s.q0 + query, head);
-#pragma unroll
-    for (int i = 0; i < L::NS; i += 4) {
-        Frag<ST> o[4];
-        load_row<DMA, ST, 64>(o, o_row + 16 * i * L::ES, on, p.dim - 16 * i, h);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d = fmaf(frag_value<ST>(g[i + j], e), frag_value<ST>(o[j], e), d);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    d = add_halves(d);
+    const float d = row_dot<DMA, ST, DP>(g, at(p.o, s.batch, s.q0 + query, head), on, p.dim, h);
     const float c = p.scale * kLog2e;
     // (infinity: whatever the row's scores are, its p are zero)
     const float lse = on ? p.lse[((int64_t)s.batch * p.q_len + s.q0 + query) * ((int64_t)p.hk * G) + head] * kLog2e : INFINITY;
@@ -423,20 +451,239 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
     store_row<DMA, ST>(at(p.dv, s.batch, s.k0 + key, kh) + 32 * t0 * L::ES, dv, on, 1.f, dim, h);
 }
 
+// Where tiles are few, the waves of a block share 32 rows (keys) and take the other side's tiles in
+// turn, each through LDS of its own and without a barrier; their sums meet there in the end.
+constexpr int kSharedLds = 128 << 10;
+template <GemmStore ST, int DP> constexpr int shared_waves() { return std::min(4, kSharedLds / (2 * kRows * Lay<ST, DP>::PITCH)); }
+
+// The waves' sums (N of them, mul[n] times each) added in their order and stored as rows of
+// `dim` elements; row r of sum n at out(n, r), zeros if it is not on(r). `lds`: the waves' own, no longer in use.
+template <GemmStore ST, int W, int DT, int N, class Out, class On>
+HM_DEV void join_waves(uint8_t* lds, const f32x16 (&acc)[N][DT], const float (&mul)[N], int rows, int dim, Out out, On on)
+{
+    constexpr int DS = 32 * DT + 4, LR = 2 * W;  // LR: lanes to a row
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    float* const sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        __syncthreads();
+        float* const own = sums + (wave * kRows + (lane & 31)) * DS;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<f32x4*>(own + 32 * t + result_row(i, h)) = f32x4{acc[n][t][i], acc[n][t][i + 1], acc[n][t][i + 2], acc[n][t][i + 3]};
+        __syncthreads();
+        const int row = threadIdx.x / LR, x = threadIdx.x % LR;
+        if (row < rows) {
+            uint8_t* const to = out(n, row);
+            const bool live = on(row);
+            for (int d = 4 * x; d < dim && d < 32 * DT; d += 4 * LR) {
+                f32x4 v = {};
+#pragma unroll
+                for (int u = 0; u < W; ++u) v += *reinterpret_cast<const f32x4*>(sums + (u * kRows + row) * DS + d);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (d + e < dim) put1<ST>(to, d + e, live ? v[e] * mul[n] : 0.f);
+            }
+        }
+    }
+}
+
+template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 * shared_waves<ST, DP>())) attn_grad_q_shared(const AttnArgs p)
+{
+    using L = Lay<ST, DP>;
+    constexpr int W = shared_waves<ST, DP>(), TILE = kRows * L::PITCH, PARTS = q_parts<ST, DP>(), DT = L::DT / PARTS;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[W * 2 * TILE];  // of each wave: keys, values
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
+    const int G = p.group;
+
+    int64_t w = xcd_order(blockIdx.x, gridDim.x);
+    const int t0 = PARTS == 1 ? 0 : (int)(w % PARTS) * DT;
+    w /= PARTS;
+    const int64_t items = p.packed ? p.slots : (int64_t)p.slots * p.batch;
+    const int kh = (int)(w / items);
+    const Seq s = find_seq<false, kRows>(p, w - kh * items, G);
+    const int rows = s.q_cap * G, r0 = s.tile * kRows;
+    if (r0 >= rows) return;
+
+    const int r = r0 + (lane & 31);
+    const int query = (int)((uint32_t)r / (uint32_t)G);
+    const int head = kh * G + (int)((uint32_t)r - (uint32_t)query * (uint32_t)G);
+    const int n_lane = r < rows && query < s.nq ? visible(p, s, query) : 0;
+    const bool on = n_lane > 0;
+    Frag<ST> q[L::NS], g[L::NS];
+    load_row<DMA, ST, DP>(q, at(p.q, s.batch, s.q0 + query, head), on, p.dim, h);
+    load_row<DMA, ST, DP>(g, at(p.g, s.batch, s.q0 + query, head), on, p.dim, h);
+    const float d = row_dot<DMA, ST, DP>(g, at(p.o, s.batch, s.q0 + query, head), on, p.dim, h);
+    const float c = p.scale * kLog2e;
+    const float lse = on ? p.lse[((int64_t)s.batch * p.q_len + s.q0 + query) * ((int64_t)p.hk * G) + head] * kLog2e : INFINITY;
+    if (r < rows && threadIdx.x < 32 && t0 == 0) p.stats[stat_row(p, s, kh, r)] = float2{lse, d};
+
+    const int in_use = s.nq * G;
+    auto seen = [&](int row) { return row < in_use ? visible(p, s, (int)((uint32_t)row / (uint32_t)G)) : 0; };
+    const int n = r0 < in_use ? seen(min(r0 + kRows, in_use) - 1) : 0, tiles = (n + kRows - 1) / kRows, n_all = seen(r0);
+
+    f32x16 dq[1][DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) dq[0][t] = f32x16{};
+    const int row_bytes = p.dim * L::ES, steps = (p.dim + 15) / 16, cols = min(DT, (p.dim + 31) / 32 - t0);
+    const uint8_t *kp = at(p.k, s.batch, s.k0, kh), *vp = at(p.v, s.batch, s.k0, kh);
+    uint8_t *const kt = lds + wave * 2 * TILE, *const vt = kt + TILE;
+    const Share<ST, DP, kRows, 64> share{lane};
+    auto load = [&](uint8_t* to, const uint8_t* from, int64_t stride, int t) __attribute__((always_inline)) {
+        share.template stage<DMA>(to, from + t * (kRows * stride), row_bytes, false, [&](int i) { return share.row(i) * stride; },
+                                  [&](int i) { return t * kRows + share.row(i) < s.nk; });
+    };
+    if (wave < tiles) {
+        load(kt, kp, p.k.ss, wave);
+        load(vt, vp, p.v.ss, wave);
+    }
+#pragma unroll 1
+    for (int t = wave; t < tiles; t += W) {
+        wave_wait<0>();
+        const bool cut = (t + 1) * kRows > n_all;
+        const int left = n_lane - t * kRows - 4 * h;
+        f32x16 x, y;
+        Frag<ST> ds[2];
+        row_product_of<ST, DP>(steps, x, kt, q, lane);
+        row_product_of<ST, DP>(steps, y, vt, g, lane);
+        wave_wait<-1>();
+        if (t + W < tiles) load(vt, vp, p.v.ss, t + W);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(x[i], c, -lse)) * (y[i] - d);
+            y[i] = cut && result_row(i, 0) >= left ? 0.f : e;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) ds[u] = as_operand<ST>(y, u);
+        col_product<ST, DP>(dq[0], kt, ds, t0, cols, lane);
+        wave_wait<-1>();
+        if (t + W < tiles) load(kt, kp, p.k.ss, t + W);
+    }
+    const float mul[1] = {p.scale};
+    join_waves<ST, W, DT, 1>(lds, dq, mul, min(kRows, rows - r0), p.dim - 32 * t0, [&](int, int row) {
+        const int token = (int)((uint32_t)(r0 + row) / (uint32_t)G);
+        return at(p.dq, s.batch, s.q0 + token, kh * G + r0 + row - token * G) + 32 * t0 * L::ES;
+    }, [&](int row) { return seen(r0 + row) > 0; });
+}
+
+template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 * shared_waves<ST, DP>())) attn_grad_kv_shared(const AttnArgs p)
+{
+    using L = Lay<ST, DP>;
+    constexpr int W = shared_waves<ST, DP>(), TILE = kRows * L::PITCH, PARTS = kv_parts<ST, DP>(), DT = L::DT / PARTS;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[W * 2 * TILE];  // of each wave: rows of q, of g
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
+    const int G = p.group;
+
+    int64_t w = xcd_order(blockIdx.x, gridDim.x);
+    const int t0 = PARTS == 1 ? 0 : (int)(w % PARTS) * DT;
+    w /= PARTS;
+    const int64_t items = p.packed ? p.slots : (int64_t)p.slots * p.batch;
+    const int kh = (int)(w / items);
+    const Seq s = find_seq<true, kRows>(p, w - kh * items, 1);
+    const int j0 = s.tile * kRows;
+    if (j0 >= s.k_cap) return;
+    const int key = j0 + (lane & 31);
+    const bool on = key < s.nk;
+    Frag<ST> k[L::NS], v[L::NS];
+    load_row<DMA, ST, DP>(k, at(p.k, s.batch, s.k0 + key, kh), on, p.dim, h);
+    load_row<DMA, ST, DP>(v, at(p.v, s.batch, s.k0 + key, kh), on, p.dim, h);
+
+    // rows that see keys of the block, all of them, and this lane's
+    const int off = s.nk - s.nq;
+    auto first_row = [&](int j) { return p.causal ? max(0, j - off) * G : 0; };
+    const int end = j0 < s.nk ? s.nq * G : 0, begin = first_row(j0) / kRows * kRows;
+    const int all = j0 + kRows <= s.nk ? first_row(j0 + kRows - 1) : INT32_MAX, mine = on ? first_row(key) : INT32_MAX;
+    const int tiles = end > begin ? (end - begin + kRows - 1) / kRows : 0;
+
+    f32x16 acc[2][DT];  // dk, dv
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[0][t] = acc[1][t] = f32x16{};
+    const float c = p.scale * kLog2e;
+    const int row_bytes = p.dim * L::ES, steps = (p.dim + 15) / 16, cols = min(DT, (p.dim + 31) / 32 - t0);
+    const uint8_t *const qp = at(p.q, s.batch, s.q0, kh * G), *const gp = at(p.g, s.batch, s.q0, kh * G);
+    uint8_t *const qt = lds + wave * 2 * TILE, *const gt = qt + TILE;
+    const float2* const stats = p.stats + stat_row(p, s, kh, 0);
+    const Share<ST, DP, kRows, 64> share{lane};
+    auto load = [&](uint8_t* to, const uint8_t* from, const Heads& x, int t) __attribute__((always_inline)) {
+        const int r0 = begin + t * kRows;
+        share.template stage<DMA>(to, from, row_bytes, false, [&](int i) {
+            const uint32_t r = (uint32_t)(r0 + share.row(i)), token = r / (uint32_t)G;
+            return token * x.ss + (int64_t)(r - token * (uint32_t)G) * x.sh;
+        }, [&](int i) { return r0 + share.row(i) < end; });
+    };
+    if (wave < tiles) {
+        load(qt, qp, p.q, wave);
+        load(gt, gp, p.g, wave);
+    }
+#pragma unroll 1
+    for (int t = wave; t < tiles; t += W) {
+        const int r0 = begin + t * kRows;
+        // (a lane holds one row's lse and D, and hands them to the registers of that row)
+        const float2 mine_st = r0 + (lane & 31) < end ? stats[r0 + (lane & 31)] : float2{INFINITY, 0.f};
+        wave_wait<0>();
+        f32x16 x, y;
+        Frag<ST> pr[2], ds[2];
+        row_product_of<ST, DP>(steps, x, qt, k, lane);
+        row_product_of<ST, DP>(steps, y, gt, v, lane);
+        const int hidden = r0 < all ? min(mine - r0, kRows) - 4 * h : INT32_MIN;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float lse = __shfl(mine_st.x, result_row(i, h)), d = __shfl(mine_st.y, result_row(i, h));
+            x[i] = result_row(i, 0) < hidden ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[i], c, -lse));
+            y[i] = result_row(i, 0) < hidden ? 0.f : x[i] * (y[i] - d);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) pr[u] = as_operand<ST>(x, u);
+        col_product<ST, DP>(acc[1], gt, pr, t0, cols, lane);
+        wave_wait<-1>();
+        if (t + W < tiles) load(gt, gp, p.g, t + W);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) ds[u] = as_operand<ST>(y, u);
+        col_product<ST, DP>(acc[0], qt, ds, t0, cols, lane);
+        wave_wait<-1>();
+        if (t + W < tiles) load(qt, qp, p.q, t + W);
+    }
+    const float mul[2] = {p.scale, 1.f};
+    join_waves<ST, W, DT, 2>(lds, acc, mul, min(kRows, s.k_cap - j0), p.dim - 32 * t0, [&](int n, int row) {
+        return at(n == 0 ? p.dk : p.dv, s.batch, s.k0 + j0 + row, kh) + 32 * t0 * L::ES;
+    }, [&](int row) { return j0 + row < s.nk; });
+}
+
 // ---------------------------------------------------------------- host side
 
+// Blocks of four times 32 rows below which the waves of a block share 32 of them: where the first
+// kind leaves the chip idle, with one wave on the long way over the other side's tiles. Heads of 128,
+// 16 + 8 of them, causal, both kernels in the first form / the second, us: fp32 1 x 512 tokens 386 / 155
+// (32 blocks of keys), 2 x 1024 756 / 478 (128), 4 x 1024 919 / 918 (256), 8 x 1024 1724 / 1792 (512); bf16
+// 1 x 128 31 / 25 (8), 2 x 512 61 / 57 (64), 4 x 512 65 / 100 (128).
+template <GemmStore ST> constexpr int64_t shared_below() { return ST == GemmStore::F32 ? 512 : 96; }
 template <GemmStore ST, bool DMA, int DP> int launch_grad(AttnArgs p, hipStream_t stream)
 {
     int64_t q_blocks = 0, k_blocks = 0;
     AttnArgs pk = p;
+    // Blocks of four waves with 32 rows each, or with 32 rows that they share.
     if (!set_grid(p, p.q_len * p.group, kTileRows, kThreads * q_parts<ST, DP>(), &q_blocks) ||
         !set_grid(pk, pk.k_len, kTileRows, kThreads * kv_parts<ST, DP>(), &k_blocks))
         return HIMUON_ERR_UNSUPPORTED;
+    constexpr int T = 64 * shared_waves<ST, DP>();
+    const bool q_shared = q_blocks < shared_below<ST>(), k_shared = k_blocks < shared_below<ST>();
+    if ((q_shared && !set_grid(p, p.q_len * p.group, kRows, T * q_parts<ST, DP>(), &q_blocks)) ||
+        (k_shared && !set_grid(pk, pk.k_len, kRows, T * kv_parts<ST, DP>(), &k_blocks)))
+        return HIMUON_ERR_UNSUPPORTED;
+    q_blocks *= q_parts<ST, DP>();
+    k_blocks *= kv_parts<ST, DP>();
     StreamDevice on(stream);
     if (on.status != HIMUON_OK) return on.status;
-    if (p.q_len > 0) hipLaunchKernelGGL((attn_grad_q<ST, DP, DMA>), dim3((unsigned)(q_blocks * q_parts<ST, DP>())), dim3(kThreads), 0, stream, p);
-    if (p.k_len > 0)
-        hipLaunchKernelGGL((attn_grad_kv<ST, DP, DMA>), dim3((unsigned)(k_blocks * kv_parts<ST, DP>())), dim3(kThreads), 0, stream, pk);
+    if (p.q_len > 0) {
+        if (q_shared) hipLaunchKernelGGL((attn_grad_q_shared<ST, DP, DMA>), dim3((unsigned)q_blocks), dim3(T), 0, stream, p);
+        else hipLaunchKernelGGL((attn_grad_q<ST, DP, DMA>), dim3((unsigned)q_blocks), dim3(kThreads), 0, stream, p);
+    }
+    if (p.k_len > 0) {
+        if (k_shared) hipLaunchKernelGGL((attn_grad_kv_shared<ST, DP, DMA>), dim3((unsigned)k_blocks), dim3(T), 0, stream, pk);
+        else hipLaunchKernelGGL((attn_grad_kv<ST, DP, DMA>), dim3((unsigned)k_blocks), dim3(kThreads), 0, stream, pk);
+    }
     return launch_status();
 }
 
