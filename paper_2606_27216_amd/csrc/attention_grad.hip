@@ -454,6 +454,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
 // Where tiles are few, the waves of a block share 32 rows (keys) and take the other side's tiles in
 // turn, each through LDS of its own and without a barrier; their sums meet there in the end.
 constexpr int kSharedLds = 128 << 10;
+template <int W, int TILE, int DT> constexpr int shared_lds() { return W * std::max(2 * TILE, kRows * (32 * DT + 4) * (int)sizeof(float)); }
 template <GemmStore ST, int DP> constexpr int shared_waves() { return std::min(4, kSharedLds / (2 * kRows * Lay<ST, DP>::PITCH)); }
 
 // The waves' sums (N of them, mul[n] times each) added in their order and stored as rows of
@@ -461,7 +462,7 @@ template <GemmStore ST, int DP> constexpr int shared_waves() { return std::min(4
 template <GemmStore ST, int W, int DT, int N, class Out, class On>
 HM_DEV void join_waves(uint8_t* lds, const f32x16 (&acc)[N][DT], const float (&mul)[N], int rows, int dim, Out out, On on)
 {
-    constexpr int DS = 32 * DT + 4, LR = 2 * W;  // LR: lanes to a row
+    constexpr int DS = 32 * DT + 4, LR = 2 * W;  // LR: lanes to a row (shared_lds() has the room)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
     float* const sums = reinterpret_cast<float*>(lds);
 #pragma unroll
@@ -494,7 +495,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
 {
     using L = Lay<ST, DP>;
     constexpr int W = shared_waves<ST, DP>(), TILE = kRows * L::PITCH, PARTS = q_parts<ST, DP>(), DT = L::DT / PARTS;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[W * 2 * TILE];  // of each wave: keys, values
+    __shared__ __attribute__((aligned(16))) uint8_t lds[shared_lds<W, TILE, DT>()];  // of each wave: keys, values; then [waves] sums
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
@@ -572,7 +573,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
 {
     using L = Lay<ST, DP>;
     constexpr int W = shared_waves<ST, DP>(), TILE = kRows * L::PITCH, PARTS = kv_parts<ST, DP>(), DT = L::DT / PARTS;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[W * 2 * TILE];  // of each wave: rows of q, of g
+    __shared__ __attribute__((aligned(16))) uint8_t lds[shared_lds<W, TILE, DT>()];  // of each wave: rows of q, of g; then [waves] sums
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
