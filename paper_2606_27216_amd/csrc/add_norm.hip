@@ -269,7 +269,7 @@ constexpr int kLongWidth = 8 * kThreads * 8;  // the widest row in registers
 int64_t norm_blocks(int64_t rows, int64_t width, bool grad)
 {
     const int64_t per = width <= 1024 ? kThreads / 64 : 1;
-    return std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, per), grad ? 512 : 2048));
+    return std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, per), grad ? 1024 : 2048));
 }
 
 template <bool GRAD, GemmStore ST, GemmStore GT> int launch_norm(NormArgs p, hipStream_t stream)

@@ -272,7 +272,9 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
     const float c = p.scale * kLog2e;
     const int row_bytes = p.dim * L::ES;
     // Where this thread's rows of the next tile lie: their place in the group and offsets (with
-    // copy()'s own part), moved on by a tile's rows each time. (Without DMA each is worked out.)
+    // copy()'s own part), moved back by a tile's rows each time. (Without DMA each is worked out.)
+    // The rows are walked over from the last one, which all keys' blocks read, so that blocks that
+    // run together read the same rows together.
     const Share<ST, DP, BR, kThreads> share{(int)threadIdx.x};
     constexpr int NI = Share<ST, DP, BR, kThreads>::NI;
     const uint8_t *const qp = at(p.q, s.batch, s.q0, kh * G), *const gp = at(p.g, s.batch, s.q0, kh * G);
@@ -283,48 +285,52 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
         const uint32_t token = (uint32_t)r / (uint32_t)G;
         return token * x.ss + (int64_t)((uint32_t)r - token * (uint32_t)G) * x.sh;
     };
+    const int tiles = end > begin ? (end - begin + BR - 1) / BR : 0;
     int place[NI];
     uint32_t q_off[NI], g_off[NI];
     if constexpr (DMA) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            place[i] = (begin + share.row(i)) % G;
-            q_off[i] = (uint32_t)offset(begin + share.row(i), p.q) + share.rest(i);
-            g_off[i] = (uint32_t)offset(begin + share.row(i), p.g) + share.rest(i);
+            const int r = begin + max(0, tiles - 1) * BR + share.row(i);
+            place[i] = r % G;
+            q_off[i] = (uint32_t)offset(r, p.q) + share.rest(i);
+            g_off[i] = (uint32_t)offset(r, p.g) + share.rest(i);
         }
     }
     auto advance = [&]() __attribute__((always_inline)) {
         if constexpr (DMA) {
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-                place[i] += step_g;
-                const bool wrap = place[i] >= G;
-                place[i] -= wrap ? G : 0;
-                q_off[i] += q_step + (wrap ? q_wrap : 0);
-                g_off[i] += g_step + (wrap ? g_wrap : 0);
+                place[i] -= step_g;
+                const bool wrap = place[i] < 0;
+                place[i] += wrap ? G : 0;
+                q_off[i] -= q_step + (wrap ? q_wrap : 0);
+                g_off[i] -= g_step + (wrap ? g_wrap : 0);
             }
         }
     };
     const float2* const stats = p.stats + stat_row(p, s, kh, 0);
-    const int tiles = end > begin ? (end - begin + BR - 1) / BR : 0, whole = (end - begin) / BR;
     const bool exact = DMA && row_bytes == L::PITCH;
     auto load_stats = [&](uint8_t* to, int r0) __attribute__((always_inline)) {  // (by every wave, so that all count the same)
         dev::dma4((uint32_t)__builtin_amdgcn_readfirstlane((int)dev::lds_offset(to)), 8 * (lane & 31) + 4 * h, dev::uniform_address(stats + r0));
     };
-    auto load = [&](int t, int slot) __attribute__((always_inline)) {
-        if (t >= tiles) return;
+    // First row of the tile that is the u-th; all but the first one are whole.
+    auto row_of = [&](int u) { return begin + (tiles - 1 - u) * BR; };
+    auto load = [&](int u, int slot) __attribute__((always_inline)) {
+        if (u >= tiles) return;
         uint8_t* const to = lds + slot * BUF;
-        const int r0 = begin + t * BR;
+        const int r0 = row_of(u);
+        const bool whole = r0 + BR <= end;
         auto in = [&](int i) { return r0 + share.row(i) < end; };
-        share.template stage<DMA>(to, qp, row_bytes, t < whole, [&](int i) {
+        share.template stage<DMA>(to, qp, row_bytes, whole, [&](int i) {
             if constexpr (DMA) return q_off[i] - share.rest(i);
             else return offset(r0 + share.row(i), p.q);
         }, in);
-        share.template stage<DMA>(to + TILE, gp, row_bytes, t < whole, [&](int i) {
+        share.template stage<DMA>(to + TILE, gp, row_bytes, whole, [&](int i) {
             if constexpr (DMA) return g_off[i] - share.rest(i);
             else return offset(r0 + share.row(i), p.g);
         }, in);
-        if (t < whole) {
+        if (whole) {
             load_stats(to + 2 * TILE, r0);
         } else if (threadIdx.x < BR) {
             const float2 st = r0 + (int)threadIdx.x < end ? stats[r0 + threadIdx.x] : float2{INFINITY, 0.f};
@@ -334,35 +340,35 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
         advance();
     };
     // hides the rows that do not see this lane's key
-    auto hide = [&](f32x16& x, int t, float with) __attribute__((always_inline)) {
-        const int r0 = begin + t * BR;
+    auto hide = [&](f32x16& x, int u, float with) __attribute__((always_inline)) {
+        const int r0 = row_of(u);
         if (r0 >= w_all) return;
         const int hidden = min(mine - r0, BR) - 4 * h;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = result_row(i, 0) < hidden ? with : x[i];
     };
-    const int first = w_begin == INT32_MAX ? INT32_MAX : max(0, w_begin - begin) / BR;  // the wave's first tile
+    const int own = w_begin == INT32_MAX ? 0 : tiles - max(0, w_begin - begin) / BR;  // the wave's tiles
     Ahead<Frag<ST>, L::NS, kDepth<ST, DP>> ry;
     // (x: the tile's scores, next: those of the tile behind it)
-    auto step = [&](int t, auto slot, f32x16& x, f32x16& next) __attribute__((always_inline)) {
+    auto step = [&](int u, auto slot, f32x16& x, f32x16& next) __attribute__((always_inline)) {
         const int S = slot;
-        if (exact && t + R - 1 < whole) {
+        if (exact && u + R - 1 < tiles) {
             dev::dma_wait_barrier<(R > 3 ? R - 3 : 0) * (2 * NI + 1)>();
             uint8_t* const to = lds + (S + R - 1) % R * BUF;
             if constexpr (DMA) {
                 share.copy(to, qp, q_off);
                 share.copy(to + TILE, gp, g_off);
             }
-            load_stats(to + 2 * TILE, begin + (t + R - 1) * BR);
+            load_stats(to + 2 * TILE, row_of(u + R - 1));
             advance();
         } else {
             dev::dma_wait_barrier<0>();
-            load(t + R - 1, (S + R - 1) % R);
+            load(u + R - 1, (S + R - 1) % R);
         }
-        if (t < first) return;
+        if (u >= own) return;
         // Every product's first reads go out beside the product before (a lone wave has nothing else
         // to wait with): `ry` those of g v^T, for the next step too.
-        auto tile = [&](int u) { return lds + u % R * BUF; };
+        auto tile = [&](int i) { return lds + i % R * BUF; };
         auto read_rows = [&](const uint8_t* from) { return [=](int i) __attribute__((always_inline)) { return L::row_frag(from, lane & 31, i, h); }; };
         auto read_cols = [&](const uint8_t* from) {
             return [=](int i) __attribute__((always_inline)) { return L::col_frag(from, 16 * (i / DT), 32 * (t0 + i % DT), lane); };
@@ -371,10 +377,10 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
         const auto read_g = read_cols(tile(S) + TILE), read_q = read_cols(tile(S));
         Ahead<Frag<ST>, L::NS, kDepth<ST, DP>> rn;
         Ahead<Frag<ST>, 2 * DT, kDepth<ST, DP>> cols_g, cols_q;
-        if (!ahead<ST, DP>() || t == first) {
+        if (!ahead<ST, DP>() || u == 0) {
             row_product<ST, DP>(x, tile(S), k, lane, [](int) {});
             ry.fill(read_y);
-            hide(x, t, -INFINITY);
+            hide(x, u, -INFINITY);
         }
         const float* const st = reinterpret_cast<const float*>(tile(S) + 2 * TILE) + 4 * h;
         f32x4 row[4];
@@ -399,7 +405,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
             }
         });
         rows_of(st + BR);
-        hide(y, t, 0.f);
+        hide(y, u, 0.f);
         if constexpr (ahead<ST, DP>()) cols_g.fill(read_g);
         auto work = [&](int from, int to) __attribute__((always_inline)) {
 #pragma unroll
@@ -415,7 +421,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
                 work(share_of<L::NS>(j), share_of<L::NS>(j + 1));
             });
             cols_q.fill(read_q);
-            hide(next, t + 1, -INFINITY);
+            hide(next, u + 1, -INFINITY);
         } else {
             work(0, 16);
             cols_g.fill(read_g);

@@ -7,7 +7,7 @@
 // so one pass over the logits with a running maximum gives them all; memory bounds it. The
 // most likely tokens come from a second look at few of them: every lane keeps the largest
 // logit that it saw, the k-th largest of those is a bound that the row's k largest logits reach,
-// and only lanes whose own reaches it read theirs again.
+// and only the shares of lanes whose own reaches it are read again, by all lanes together.
 #include "elementwise8.h"
 #include "train_ops.h"
 
@@ -44,9 +44,10 @@ struct Sums {
             m = now;
         }
     }
-    __device__ __forceinline__ void add(float z)
+    // Logit x, c = scale log2 e.
+    __device__ __forceinline__ void add(float x, float c)
     {
-        const float d = m == -INFINITY ? z : z - m, e = __builtin_amdgcn_exp2f(d);
+        const float d = fmaf(x, c, m == -INFINITY ? 0.f : -m), e = __builtin_amdgcn_exp2f(d);
         s += e;
         u = fmaf(e, fmaxf(d, -1e30f), u);  // (e is 0 for minus infinity)
     }
@@ -86,8 +87,9 @@ template <int NT> struct Shared {
     float m[NT / 64 + 1], s[NT / 64 + 1], u[NT / 64 + 1];
     uint64_t best[NT / 64 + 1];
     uint32_t lane_top[256];
+    uint16_t hot[NT];
     uint64_t cand[kCand];
-    uint32_t bound, count;
+    uint32_t bound, hot_count, count;
 };
 
 // The largest key of the group's lanes.
@@ -128,20 +130,37 @@ template <GemmStore ST, int NT, bool TOP> __global__ void __launch_bounds__(NT =
     const float c = p.scale * kLog2e;
     const int vocab = p.vocab;
 
+    // Four chunks at a time, all on their way before the first is used.
+    constexpr int U = 4;
     Sums sum;
     float best = -INFINITY;
-    for (int at = 8 * lane; at < vocab; at += 8 * NT) {
-        const int n = vocab - at >= 8 ? 8 : vocab - at;
-        const Raw8<ST> raw = get_raw8<ST>(p.logits, base + at, n);
-        float z[8];
+    auto take = [&](const Raw8<ST>* raw, int count, int last) __attribute__((always_inline)) {  // (the last chunk's first `last` count)
+        float top = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = e < n ? raw_value<ST>(raw, e) : -INFINITY;
-        const float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (i < count && (i < count - 1 || e < last)) top = fmaxf(top, raw_value<ST>(raw[i], e));
         best = fmaxf(best, top);
         sum.rescale(top * c);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) sum.add(z[e] * c);
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (i < count && (i < count - 1 || e < last)) sum.add(raw_value<ST>(raw[i], e), c);
+    };
+    int at = 8 * lane;
+    for (; at + 8 * NT * (U - 1) + 8 <= vocab; at += 8 * NT * U) {
+        Raw8<ST> raw[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) raw[i] = get_raw8<ST>(p.logits, base + at + 8 * NT * i, 8);
+        take(raw, U, 8);
+    }
+    for (; at < vocab; at += 8 * NT) {
+        const int n = vocab - at >= 8 ? 8 : vocab - at;
+        Raw8<ST> raw[U];
+        raw[0] = get_raw8<ST>(p.logits, base + at, n);
+        take(raw, 1, n);
     }
     const float mine = best;
 #pragma unroll
@@ -190,12 +209,10 @@ template <GemmStore ST, int NT, bool TOP> __global__ void __launch_bounds__(NT =
     // Bound: the k-th largest of 64 or 256 disjoint sets of lanes' largest logits.
     constexpr int SETS = NT == 64 ? 64 : 256;
     float set_top = mine;
-    if constexpr (NT > 256) {
-        set_top = fmaxf(set_top, __shfl_xor(set_top, 1));
-        set_top = fmaxf(set_top, __shfl_xor(set_top, 2));
-    }
+#pragma unroll
+    for (int o = 1; o < NT / SETS; o *= 2) set_top = fmaxf(set_top, __shfl_xor(set_top, o));
     if (lane % (NT / SETS) == 0) sh.lane_top[lane / (NT / SETS)] = order_of(set_top);
-    if (lane == 0) sh.count = 0;
+    if (lane == 0) sh.count = sh.hot_count = 0;
     group_sync<NT>();
     if (lane < 64) {
         uint32_t v[SETS / 64];
@@ -215,15 +232,20 @@ template <GemmStore ST, int NT, bool TOP> __global__ void __launch_bounds__(NT =
     const uint32_t bound = sh.bound;
     // (a row with NaN, or with fewer than k sets above minus infinity, is left to the search below)
     const bool plain = sum.s == sum.s && bound > order_of(-INFINITY);
-    if (plain && order_of(mine) >= bound) {
-        for (int at = 8 * lane; at < vocab; at += 8 * NT) {
+    if (plain && order_of(mine) >= bound) sh.hot[atomicAdd(&sh.hot_count, 1u)] = (uint16_t)lane;  // (in any order: what they hold is ranked)
+    group_sync<NT>();
+    const int hot = (int)sh.hot_count, chunks = (vocab + 8 * NT - 1) / (8 * NT);
+    if (hot <= (NT == 64 ? 64 : NT / 4)) {  // (more: equal logits everywhere, for the search below)
+        for (int i = lane; i < hot * chunks; i += NT) {
+            const int h = i / chunks, at = 8 * (sh.hot[h] + NT * (i - h * chunks));
+            if (at >= vocab) continue;
             const int n = vocab - at >= 8 ? 8 : vocab - at;
             const Raw8<ST> raw = get_raw8<ST>(p.logits, base + at, n);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float x = raw_value<ST>(raw, e);
                 if (e < n && order_of(x) >= bound) {
-                    const uint32_t place = atomicAdd(&sh.count, 1u);  // (their order does not matter: they are ranked below)
+                    const uint32_t place = atomicAdd(&sh.count, 1u);
                     if (place < kCand) sh.cand[place] = key_of(x, at + e);
                 }
             }
@@ -291,8 +313,8 @@ template <GemmStore ST> __global__ void __launch_bounds__(kGradThreads) logprob_
     }
 }
 
-// Lanes of a row: a wave's, or a block's of 256 or 1024.
-int row_lanes(int64_t vocab) { return vocab <= 2048 ? 64 : vocab <= 16384 ? 256 : 1024; }
+// Lanes of a row: a wave's, or a block's of 256 or 512.
+int row_lanes(int64_t vocab) { return vocab <= 2048 ? 64 : vocab <= 16384 ? 256 : 512; }
 int64_t row_blocks(int64_t rows, int64_t vocab) { return row_lanes(vocab) == 64 ? ceil_div(rows, 4) : rows; }
 
 template <GemmStore ST, bool TOP> int launch_logprob(const LogprobArgs& p, hipStream_t stream)
@@ -301,7 +323,7 @@ template <GemmStore ST, bool TOP> int launch_logprob(const LogprobArgs& p, hipSt
     const dim3 grid((unsigned)row_blocks(p.rows, p.vocab)), block(std::max(lanes, 256));
     if (lanes == 64) hipLaunchKernelGGL((logprob_rows<ST, 64, TOP>), grid, block, 0, stream, p);
     else if (lanes == 256) hipLaunchKernelGGL((logprob_rows<ST, 256, TOP>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((logprob_rows<ST, 1024, TOP>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((logprob_rows<ST, 512, TOP>), grid, block, 0, stream, p);
     return launch_status();
 }
 
