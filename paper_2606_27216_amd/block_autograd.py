@@ -71,7 +71,8 @@ class Attention(torch.autograd.Function):
 class TokenLogprob(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tokens, top, scale):
-        results = ops.token_logprob(logits, tokens, top, scale)
+        # (tensors of their own: views of one could not be written in place)
+        results = ops._token_logprob(logits, tokens, top, scale, [logits.new_empty(tokens.shape, dtype=torch.float32) for _ in range(3)])
         ctx.save_for_backward(logits, tokens, results[2], results[1])
         ctx.scale = scale
         ctx.set_materialize_grads(False)

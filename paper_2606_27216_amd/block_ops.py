@@ -53,10 +53,6 @@ def _functions():
     return block_autograd
 
 
-def _records(*tensors):
-    return any(t is not None and t.requires_grad for t in tensors) and _torch().is_grad_enabled()
-
-
 # ----------------------------------------------------------------- residual and norm
 
 def _rows(t, what):
@@ -100,7 +96,8 @@ def add_norm(x, residual, gain, eps=1e-6, pack=False, out=None, stream=None):
     _same_device(dev, gain)
     if _away(dev, stream):
         return _on(dev, stream, add_norm, x, residual, gain, eps, pack, out)
-    if out is None and _records(x, residual, gain):
+    if out is None and (x.requires_grad or gain.requires_grad or (residual is not None and residual.requires_grad)) and \
+            torch.is_grad_enabled():
         return _functions().AddNorm.apply(x, residual, gain, eps, pack) if residual is not None else \
             (x, *_functions().Norm.apply(x, gain, eps, pack))
     if out is None:
@@ -236,7 +233,7 @@ def attention(q, k, v, q_starts=None, k_starts=None, q_lengths=None, k_lengths=N
     dev = q.device
     if _away(dev, stream):
         return _on(dev, stream, attention, q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale, out, workspace)
-    if out is None and _records(q, k, v):
+    if out is None and (q.requires_grad or k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
         return _functions().Attention.apply(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale)
     L = lib()
     held, ws, ws_bytes = _workspace(L.himuon_attention_workspace_size(args), workspace, q)
@@ -244,7 +241,7 @@ def attention(q, k, v, q_starts=None, k_starts=None, q_lengths=None, k_lengths=N
         out, ho = _fresh(q, sq)
     else:
         ho = _heads_like(out, "out", sq, q)
-    lse = torch.empty(sq[:-1], dtype=torch.float32, device=dev)
+    lse = out.new_empty(sq[:-1], dtype=torch.float32)
     _done(L.himuon_attention(args, hq, hk, hv, ho, lse.data_ptr(), ws, ws_bytes, _stream_of(dev.index)), "himuon_attention")
     return out, lse
 
@@ -298,22 +295,30 @@ def token_logprob(logits, tokens, top=0, scale=1.0, stream=None):
 
     The gradient of ``logits`` from those of logprob and entropy is ``token_logprob_grad``'s."""
     torch = _torch()
-    rows, vocab, ld = _logits(logits, tokens)
-    dev, code, index = logits.device, _type_code(logits), _index_code(tokens)
+    vocab = _logits(logits, tokens)[1]
+    dev = logits.device
+    _type_code(logits), _index_code(tokens)
     if not 0 <= top <= min(vocab, MAX_TOP):
         raise ValueError(f"top must be between 0 and the smaller of {MAX_TOP} and the vocabulary")
     if _away(dev, stream):
         return _on(dev, stream, token_logprob, logits, tokens, top, scale)
-    if _records(logits):
+    if logits.requires_grad and torch.is_grad_enabled():
         return _functions().TokenLogprob.apply(logits, tokens, top, scale)
-    logprob, entropy, lse = (torch.empty(tokens.shape, dtype=torch.float32, device=dev) for _ in range(3))
+    return _token_logprob(logits, tokens, top, scale, torch.empty((3, *tokens.shape), dtype=torch.float32, device=dev).unbind(0))
+
+
+def _token_logprob(logits, tokens, top, scale, results):
+    """``token_logprob`` into (logprob, entropy, lse); the arguments have been checked."""
+    rows, vocab, ld = _rows(logits, "logits")
+    logprob, entropy, lse = results
     best = best_index = None
     if top:
-        best = torch.empty((*tokens.shape, top), dtype=torch.float32, device=dev)
-        best_index = torch.empty((*tokens.shape, top), dtype=torch.int64, device=dev)
-    _done(lib().himuon_token_logprob(rows, vocab, logits.data_ptr(), ld, code, tokens.data_ptr(), index, scale, top, logprob.data_ptr(),
-                                     entropy.data_ptr(), lse.data_ptr(), best.data_ptr() if top else None,
-                                     best_index.data_ptr() if top else None, _stream_of(dev.index)), "himuon_token_logprob")
+        best = lse.new_empty((*tokens.shape, top))
+        best_index = lse.new_empty((*tokens.shape, top), dtype=_torch().int64)
+    _done(lib().himuon_token_logprob(rows, vocab, logits.data_ptr(), ld, _type_code(logits), tokens.data_ptr(), _index_code(tokens),
+                                     scale, top, logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
+                                     best.data_ptr() if top else None, best_index.data_ptr() if top else None,
+                                     _stream_of(logits.device.index)), "himuon_token_logprob")
     return (logprob, entropy, lse, best, best_index) if top else (logprob, entropy, lse)
 
 
