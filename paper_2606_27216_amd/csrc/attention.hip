@@ -109,12 +109,12 @@ __global__ void __launch_bounds__(kThreads, (Lay<ST, DP>::PITCH <= 256 ? 2 : 1))
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
-    const int64_t w = xcd_order(blockIdx.x, gridDim.x);
-    const int64_t items = p.packed ? p.slots : (int64_t)p.slots * p.batch;  // of a key head
+    const uint32_t w = xcd_order(blockIdx.x, gridDim.x);
+    const uint32_t items = p.packed ? p.slots : (uint32_t)p.slots * (uint32_t)p.batch;  // of a key head
     const int kh = (int)(w / items);
-    const int64_t at_item = w - kh * items;
+    const uint32_t at_item = w - kh * items;
     // (a sequence's last tiles, which see the most keys, first)
-    const int64_t tile = p.packed ? items - 1 - at_item : at_item / p.slots * p.slots + (p.slots - 1 - at_item % p.slots);
+    const uint32_t slots = p.slots, tile = p.packed ? items - 1 - at_item : at_item / slots * slots + (slots - 1 - at_item % slots);
     const Seq s = find_seq<false, kTileRows>(p, tile, G);
     const int rows = s.q_cap * G, r0 = s.tile * kTileRows;  // (a sequence's rows are counted in 32 bits)
     if (r0 >= rows) return;
@@ -259,7 +259,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     __shared__ __attribute__((aligned(16))) uint8_t lds[few_lds<ST, DP>()];  // of each wave: [2][keys, values]; then [waves][32][DS] floats
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group, split = (int)(blockIdx.x % (uint32_t)p.splits);
-    const int64_t w = blockIdx.x / (uint32_t)p.splits;
+    const uint32_t w = blockIdx.x / (uint32_t)p.splits;
     const int kh = (int)(w % (uint32_t)p.hk);
     const Seq s = find_seq<false, kRows>(p, w / (uint32_t)p.hk, G);  // (one tile to a sequence)
     const int rows = s.q_cap * G;
@@ -348,7 +348,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     }
     const int token = row / G, hd = kh * G + row - token * G;
     const bool used = token < s.nq;
-    float* const part = p.splits > 1 ? p.part + (((w * p.splits) + split) * kRows + row) * DS : nullptr;
+    float* const part = p.splits > 1 ? p.part + (((int64_t)w * p.splits + split) * kRows + row) * DS : nullptr;
     uint8_t* const out = at(p.o, s.batch, s.q0 + token, hd);
     const float mul = 1.f / l;
     const bool some = used && l != 0.f;
@@ -384,12 +384,11 @@ template <GemmStore ST, int DP> __global__ void __launch_bounds__(kThreads) attn
 {
     constexpr int DS = DP + kStat, E = DP / 64;
     const int lane = threadIdx.x & 63, G = p.group, rows = (int)p.q_len * G;
-    const int64_t id = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    const int64_t w = id / rows;
-    const int row = (int)(id - w * rows), kh = (int)(w % (uint32_t)p.hk);
-    if (w >= (int64_t)p.batch * p.hk) return;
+    const uint32_t id = blockIdx.x * kWaves + (threadIdx.x >> 6), w = id / (uint32_t)rows;
+    const int row = (int)(id - w * (uint32_t)rows), kh = (int)(w % (uint32_t)p.hk);
+    if (w >= (uint32_t)p.batch * (uint32_t)p.hk) return;
     const Seq s = find_seq<false, kRows>(p, w / (uint32_t)p.hk, G);
-    const float* const part = p.part + (w * p.splits * kRows + row) * DS;
+    const float* const part = p.part + ((int64_t)w * p.splits * kRows + row) * DS;
     const float c = p.scale * kLog2e;
     float m = -INFINITY;
     for (int i = 0; i < p.splits; ++i) m = fmaxf(m, part[(int64_t)i * kRows * DS + DP]);

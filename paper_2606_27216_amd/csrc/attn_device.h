@@ -372,10 +372,11 @@ template <bool VEC, GemmStore ST, int DT> HM_DEV void store_row(uint8_t* row, co
 // --------------------------------------------------------- where a block's rows lie
 
 // Blocks that read the same keys run on one XCD (blocks are dealt out to the eight in turn).
-HM_DEV int64_t xcd_order(int64_t id, int64_t n)
+// (A launch has fewer than 2^24 blocks.)
+HM_DEV uint32_t xcd_order(uint32_t id, uint32_t n)
 {
-    const int64_t x = id & 7, per = n >> 3, rest = n & 7;
-    return x * per + (x < rest ? x : rest) + (id >> 3);
+    const uint32_t x = id & 7, per = n >> 3, rest = n & 7;
+    return x * per + min(x, rest) + (id >> 3);
 }
 
 struct Seq {
@@ -391,20 +392,21 @@ HM_DEV int64_t clamped(const void* p, int64_t i, bool wide, int64_t hi)
 }
 
 // Work item `w` of a sequence's queries (KEYS: keys): the sequence and the tile of it, ROWS rows
-// to a tile and `group` rows to a token.
+// to a tile and `group` rows to a token. (All lanes of a wave call it.)
 //
 // Packed: tile t of sequence s has place floor(first row / ROWS) + s + t, counted with the tokens
 // ahead of the first sequence as sequence 0 and those behind the last one as the last, so that
 // the places need no sums over sequences and a grid of rows / ROWS + batch + 2 holds them
-// all; a place behind a sequence's last tile has nothing to do.
-template <bool KEYS, int ROWS> HM_DEV Seq find_seq(const AttnArgs& p, int64_t w, int group)
+// all; a place behind a sequence's last tile has nothing to do. The sequence is the last whose first place
+// is not behind w: 64 of them are looked at together. (Starts that decrease leave results
+// unspecified, and no access outside of the arrays.)
+template <bool KEYS, int ROWS> HM_DEV Seq find_seq(const AttnArgs& p, uint32_t w, int group)
 {
     Seq s{};
     const bool wide = p.wide;
     if (!p.packed) {
-        const int64_t tiles = p.slots;
-        s.batch = (int32_t)(w / tiles);
-        s.tile = (int32_t)(w - s.batch * tiles);
+        s.batch = (int32_t)(w / (uint32_t)p.slots);
+        s.tile = (int32_t)(w - (uint32_t)s.batch * (uint32_t)p.slots);
         s.q_cap = (int32_t)p.q_len;
         s.k_cap = (int32_t)p.k_len;
         s.nq = p.ql ? (int32_t)clamped(p.ql, s.batch, wide, p.q_len) : s.q_cap;
@@ -413,15 +415,16 @@ template <bool KEYS, int ROWS> HM_DEV Seq find_seq(const AttnArgs& p, int64_t w,
     }
     const void* const starts = KEYS ? p.ks : p.qs;
     const int64_t len = KEYS ? p.k_len : p.q_len;
-    int lo = 0, hi = p.batch + 1;  // the last sequence whose first place is not behind w
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        const int64_t at = clamped(starts, mid - 1, wide, len) * group / ROWS + mid;
-        if (at <= w) lo = mid;
-        else hi = mid - 1;
+    auto place = [&](int i) { return i == 0 ? (int64_t)0 : clamped(starts, i - 1, wide, len) * group / ROWS + i; };
+    int lo = -1;
+    for (int base = 0; base < p.batch + 2; base += 64) {
+        const int i = base + (int)(threadIdx.x & 63);
+        lo += __popcll(__ballot(i < p.batch + 2 && place(min(i, p.batch + 1)) <= (int64_t)w));
     }
     const int64_t first = lo == 0 ? 0 : clamped(starts, lo - 1, wide, len);
-    s.tile = (int32_t)(w - (first * group / ROWS + lo));
+    const int64_t tile = (int64_t)w - (first * group / ROWS + lo);
+    if (tile < 0) return s;
+    s.tile = (int32_t)tile;
     const bool real = lo > 0 && lo <= p.batch;
     if (!real) {  // tokens that belong to no sequence
         const int64_t end = lo == 0 ? clamped(starts, 0, wide, len) : len;
