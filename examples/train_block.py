@@ -2,12 +2,13 @@
 
     python examples/train_block.py [--steps 60]
 
-Tokens are looked up in a scaled table (``embed``); queries and keys are normalised per
-head and rotated (``qk_norm_rope``); every projection keeps its input in 8 bits for the
-backward pass (``act_pack``) and forms its weight gradient from it (``weight_grad``) in the
-buffer that ``HiMuon`` steps on; the table's gradient comes from the sorted tokens
-(``embed_grad``). Lookup and norms join autograd by themselves, the projections through the
-function below; attention itself, the loss and the residual's norms are torch's.
+Tokens are looked up in a scaled table (``embed``); the residual is added and normalised in
+one pass (``add_norm``); queries and keys are normalised per head and rotated
+(``qk_norm_rope``) and go through ``attention`` with grouped heads; the loss comes from
+``token_logprob``. Every projection keeps its input in 8 bits for the backward pass
+(``act_pack``) and forms its weight gradient from it (``weight_grad``) in the buffer that
+``HiMuon`` steps on; the table's gradient comes from the sorted tokens (``embed_grad``). All of
+them join autograd by themselves, the projections through the function below.
 
 The task: every token has one successor, and a sequence walks from a random one on.
 """
@@ -58,10 +59,10 @@ class Block:
         self.grads = {n: torch.zeros_like(w) for n, w in self.weights.items()}
         self.table = (0.02 * torch.randn(VOCAB, WIDTH, generator=gen, device=device)).bfloat16().requires_grad_()
         self.gains = [torch.ones(HEAD, device=device, requires_grad=True) for _ in range(2)]
+        self.norm_gains = [torch.ones(WIDTH, device=device, requires_grad=True) for _ in range(3)]
         rate = 10000.0 ** (-torch.arange(HEAD // 2, device=device, dtype=torch.float64) / (HEAD // 2))
         angle = torch.arange(SEQ, device=device, dtype=torch.float64)[:, None] * rate
         self.cos, self.sin = angle.cos().float(), angle.sin().float()
-        self.mask = torch.ones(SEQ, SEQ, dtype=torch.bool, device=device).tril()
 
     def linear(self, name, x):
         return Linear8.apply(x, self.weights[name], self.grads[name])
@@ -72,22 +73,25 @@ class Block:
     def norm_rope(self, q, k):
         return hm.qk_norm_rope(q, k, *self.gains, self.cos, self.sin, eps=EPS)
 
-    def loss(self, tokens):
-        def norm(x):
-            return F.normalize(x.float(), dim=-1).mul(math.sqrt(WIDTH)).bfloat16()
+    def add_norm(self, x, residual, i):
+        return hm.add_norm(x, residual, self.norm_gains[i], eps=EPS)
 
+    def attention(self, q, k, v):
+        return hm.attention(q, k, v)[0]
+
+    def logprob(self, logits, tokens):
+        return hm.token_logprob(logits, tokens)[0]
+
+    def loss(self, tokens):
         B, S = tokens.shape
-        x = self.embed(tokens)
-        qkv = self.linear("qkv", norm(x)).view(B, S, HEADS + 2 * KV_HEADS, HEAD)
+        x, y = self.add_norm(self.embed(tokens), None, 0)
+        qkv = self.linear("qkv", y).view(B, S, HEADS + 2 * KV_HEADS, HEAD)
         q, k = self.norm_rope(qkv[:, :, :HEADS], qkv[:, :, HEADS:HEADS + KV_HEADS])
-        q, k, v = (t.float().transpose(1, 2) for t in (q, k, qkv[:, :, HEADS + KV_HEADS:]))
-        k, v = (t.repeat_interleave(HEADS // KV_HEADS, 1) for t in (k, v))
-        score = (q @ k.transpose(-1, -2) / math.sqrt(HEAD)).masked_fill(~self.mask, float("-inf"))
-        y = (score.softmax(-1) @ v).transpose(1, 2).reshape(B, S, HEADS * HEAD).bfloat16()
-        x = x + self.linear("o", y)
-        x = x + self.linear("down", F.silu(self.linear("up", norm(x))))
-        logits = self.linear("head", norm(x))
-        return F.cross_entropy(logits[:, :-1].float().flatten(0, 1), tokens[:, 1:].flatten())
+        y = self.attention(q, k, qkv[:, :, HEADS + KV_HEADS:]).reshape(B, S, HEADS * HEAD)
+        x, y = self.add_norm(self.linear("o", y), x, 1)
+        x, y = self.add_norm(self.linear("down", F.silu(self.linear("up", y))), x, 2)
+        # (the last token of a sequence has no successor: -1 is no token, and counts for nothing)
+        return -self.logprob(self.linear("head", y), F.pad(tokens[:, 1:], (0, 1), value=-1)).sum() / (B * (S - 1))
 
 
 class Walks:
@@ -105,7 +109,7 @@ class Walks:
 def train(steps, seed=0, lr=0.02, say=print):
     block = Block(seed)
     optimizer = hm.HiMuon(block.weights.values(), T=128, lr=lr, momentum=0.9)
-    rest = torch.optim.Adam([block.table, *block.gains], lr=lr / 10, eps=1e-6)
+    rest = torch.optim.Adam([block.table, *block.gains, *block.norm_gains], lr=lr / 10, eps=1e-6)
     data = Walks(seed + 1)
     losses = []
     for step in range(steps):

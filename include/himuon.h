@@ -654,7 +654,7 @@ int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, const void* 
  * h = x + residual (NULL: h is x, and nothing is written to h), and
  *     y = h * gain / sqrt(mean(h^2) + eps)
  * over each of n_tokens rows of `width` elements. The norm is that of the sum in
- * fp32, before h is rounded on store. With codes and exponents (both or neither) y is
+ * fp32, before h is rounded on store (the sum of its squares has to lie in fp32's range). With codes and exponents (both or neither) y is
  * kept in 8 bits too, as himuon_act_pack of the stored y gives them.
  *
  * x, residual, h, y  storage `dtype`, ld >= width. h may be x or residual, y any of
@@ -755,7 +755,8 @@ int himuon_attention_grad(const himuon_attn_t* args, const himuon_heads_t* g, co
  *                 tokens, the largest first, equal logits by index (NaN counts as largest)
  * A token outside [0, vocab) (such as -1) marks a row that is not in use: it is not
  * read, its results are zeros and its top_index -1. A row whose logits are all
- * minus infinity has the log probabilities and lse minus infinity and entropy zero.
+ * minus infinity has the log probabilities and lse minus infinity and entropy zero; one with
+ * NaN or plus infinity has NaN for its numbers.
  * Sums are fp32, relative to the row's maximum.
  *
  * logits     n_tokens x vocab, storage `dtype`, ld >= vocab; vocab below 2^31.

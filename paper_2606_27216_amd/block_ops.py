@@ -11,7 +11,9 @@ They keep the rules of ``train_ops``: argument checks and marshalling only, work
 HimuonError for an error of the library; float32 or bfloat16 storage.
 
 ``add_norm``, ``attention`` and ``token_logprob`` join autograd where it records (results
-written to ``out`` carry no graph). lse and the most likely tokens carry none.
+written to ``out`` carry no graph). lse and the most likely tokens carry none. A backward
+pass is captured into a HIP graph as any of torch's is: after a warm-up on the capturing
+stream, and while no eager graph of the same leaves is alive.
 """
 from __future__ import annotations
 

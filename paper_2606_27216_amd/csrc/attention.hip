@@ -560,6 +560,7 @@ extern "C" int himuon_attention(const himuon_attn_t* args, const himuon_heads_t*
     if (!set_heads(p.q, q, args, args->q_len, args->q_heads, false, &dma) || !set_heads(p.k, k, args, args->k_len, args->k_heads, false, &dma) ||
         !set_heads(p.v, v, args, args->k_len, args->k_heads, false, &dma) || !set_heads(p.o, out, args, args->q_len, args->q_heads, true, &dma) || !lse)
         return HIMUON_ERR_INVALID_ARG;
+    if (p.o.ptr == p.q.ptr || p.o.ptr == p.k.ptr || p.o.ptr == p.v.ptr) return HIMUON_ERR_INVALID_ARG;
     p.lse = lse;
     const bool few = few_rows(args);
     if (few) p.splits = (int32_t)few_splits(args);

@@ -732,6 +732,9 @@ extern "C" int himuon_attention_grad(const himuon_attn_t* args, const himuon_hea
         !set_heads(p.dk, dk, args, nk, args->k_heads, true, &dma) || !set_heads(p.dv, dv, args, nk, args->k_heads, true, &dma) ||
         (nq > 0 && !lse))
         return HIMUON_ERR_INVALID_ARG;
+    for (const Heads* o : {&p.dq, &p.dk, &p.dv})
+        for (const Heads* i : {&p.g, &p.q, &p.k, &p.v, &p.o})
+            if (o->ptr && o->ptr == i->ptr) return HIMUON_ERR_INVALID_ARG;
     p.lse = const_cast<float*>(lse);
     const size_t need = himuon_attention_grad_workspace_size(args);
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return HIMUON_ERR_WORKSPACE;

@@ -398,8 +398,8 @@ HM_DEV int64_t clamped(const void* p, int64_t i, bool wide, int64_t hi)
 // ahead of the first sequence as sequence 0 and those behind the last one as the last, so that
 // the places need no sums over sequences and a grid of rows / ROWS + batch + 2 holds them
 // all; a place behind a sequence's last tile has nothing to do. The sequence is the last whose first place
-// is not behind w: 64 of them are looked at together. (Starts that decrease leave results
-// unspecified, and no access outside of the arrays.)
+// is not behind w: 64 of them, evenly spread, are looked at together until it is one of 64 neighbours.
+// (Starts that decrease leave results unspecified, and no access outside of the arrays.)
 template <bool KEYS, int ROWS> HM_DEV Seq find_seq(const AttnArgs& p, uint32_t w, int group)
 {
     Seq s{};
@@ -416,10 +416,13 @@ template <bool KEYS, int ROWS> HM_DEV Seq find_seq(const AttnArgs& p, uint32_t w
     const void* const starts = KEYS ? p.ks : p.qs;
     const int64_t len = KEYS ? p.k_len : p.q_len;
     auto place = [&](int i) { return i == 0 ? (int64_t)0 : clamped(starts, i - 1, wide, len) * group / ROWS + i; };
-    int lo = -1;
-    for (int base = 0; base < p.batch + 2; base += 64) {
-        const int i = base + (int)(threadIdx.x & 63);
-        lo += __popcll(__ballot(i < p.batch + 2 && place(min(i, p.batch + 1)) <= (int64_t)w));
+    int lo = 0;
+    for (int n = p.batch + 2; n > 1;) {  // it is among lo .. lo + n - 1
+        const int step = (n + 63) >> 6, i = (int)(threadIdx.x & 63) * step;
+        const bool at_or_before = i < n && place(lo + min(i, n - 1)) <= (int64_t)w;
+        const int k = max(0, __popcll(__ballot(at_or_before)) - 1) * step;
+        lo += k;
+        n = min(step, n - k);
     }
     const int64_t first = lo == 0 ? 0 : clamped(starts, lo - 1, wide, len);
     const int64_t tile = (int64_t)w - (first * group / ROWS + lo);

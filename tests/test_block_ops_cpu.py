@@ -81,14 +81,15 @@ def _attn(**bad):
 
 
 HEADS = train_ops._HEADS.pack(P, 64 * 4 * 12, 64 * 4, 64)
+OUT = train_ops._HEADS.pack(2 * P, 64 * 4 * 12, 64 * 4, 64)
 NONE = train_ops._HEADS.pack(0, 64 * 4 * 12, 64 * 4, 64)
 
 
-def _forward(args, heads=(HEADS,) * 4, lse=P, ws=None, ws_bytes=0):
+def _forward(args, heads=(HEADS,) * 3 + (OUT,), lse=P, ws=None, ws_bytes=0):
     return hm.lib().himuon_attention(args, *heads, lse, ws, ws_bytes, None)
 
 
-def _backward(args, heads=(HEADS,) * 8, lse=P, ws=P, ws_bytes=BIG):
+def _backward(args, heads=(HEADS,) * 5 + (OUT,) * 3, lse=P, ws=P, ws_bytes=BIG):
     return hm.lib().himuon_attention_grad(args, *heads[:5], lse, *heads[5:], ws, ws_bytes, None)
 
 
@@ -110,18 +111,18 @@ def test_attention_sizes_beyond_the_kernels(bad):
 
 
 def test_attention_pointers_strides_and_workspaces():
-    for n, call in ((4, _forward), (8, _backward)):
+    for good, call in (([HEADS] * 3 + [OUT], _forward), ([HEADS] * 5 + [OUT] * 3, _backward)):
         assert call(None) == hm.ERR_INVALID_ARG
-        for i in range(n):
-            assert call(_attn(), [NONE if i == j else HEADS for j in range(n)]) == hm.ERR_INVALID_ARG
-            assert call(_attn(), [None if i == j else HEADS for j in range(n)]) == hm.ERR_INVALID_ARG
-            far = train_ops._HEADS.pack(P, 1 << 50, 64 * 4, 64)
-            assert call(_attn(), [far if i == j else HEADS for j in range(n)]) == hm.ERR_INVALID_ARG
+        for i in range(len(good)):
+            for bad in (NONE, None, train_ops._HEADS.pack(5 * P, 1 << 50, 64 * 4, 64)):
+                assert call(_attn(), [bad if i == j else h for j, h in enumerate(good)]) == hm.ERR_INVALID_ARG
+            if good[i] is OUT:  # a result in an input's place
+                assert call(_attn(), [HEADS if i == j else h for j, h in enumerate(good)]) == hm.ERR_INVALID_ARG
         assert call(_attn(), lse=None) == hm.ERR_INVALID_ARG
-    for flat in (train_ops._HEADS.pack(P, 0, 256, 64), train_ops._HEADS.pack(P, 4096, 0, 64), train_ops._HEADS.pack(P, 4096, 256, 0)):
+    for flat in (train_ops._HEADS.pack(5 * P, 0, 256, 64), train_ops._HEADS.pack(5 * P, 4096, 0, 64), train_ops._HEADS.pack(5 * P, 4096, 256, 0)):
         assert _forward(_attn(), [HEADS] * 3 + [flat]) == hm.ERR_INVALID_ARG  # rows of a result must not fall on each other
         for i in range(5, 8):
-            assert _backward(_attn(), [flat if i == j else HEADS for j in range(8)]) == hm.ERR_INVALID_ARG
+            assert _backward(_attn(), [flat if i == j else HEADS if j < 5 else OUT for j in range(8)]) == hm.ERR_INVALID_ARG
     L = hm.lib()
     assert L.himuon_attention_grad_workspace_size(_attn()) >= 2 * 10 * 4 * 8
     for bad in (dict(ws=None), dict(ws=P + 8), dict(ws_bytes=2 * 10 * 4 * 8 - 1)):

@@ -160,6 +160,9 @@ def test_packed(causal, dtype, index):
         assert torch.equal(again[0], out) and torch.equal(again[1], lse)
         for t in (out, *grads):
             assert not t[off.cuda()].any()
+    # many sequences, short ones, some of them empty
+    cuts = torch.randint(0, 1200, (700,), generator=torch.Generator().manual_seed(5)).sort().values.to(index).cuda()
+    check(*make((), 1210, 1210, 4, 2, 64, dtype, "tokens", 6), causal=causal, q_starts=cuts)
     # keys of their own, and tokens in use of each sequence
     qs = torch.tensor([0, 40, 41, 100, 170], dtype=index, device="cuda")
     ks = torch.tensor([2, 30, 200, 260, 390], dtype=index, device="cuda")
