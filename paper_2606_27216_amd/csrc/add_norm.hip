@@ -53,7 +53,9 @@ template <GemmStore ST> __device__ __forceinline__ void put8n(void* base, int64_
 }
 
 // The sum over a row's NT lanes, in every one of them. `slot` alternates from row to row.
-template <int NT> __device__ __forceinline__ float row_sum(float v, float (*sums)[kThreads / 64], int slot)
+// (F: the forward pass sums squares in 64 bits, which memory hides: r is then off by half a step of 32 bits,
+// and y's roundings to 16 and 8 bits fall where the definition's do.)
+template <int NT, class F> __device__ __forceinline__ F row_sum(F v, F (*sums)[kThreads / 64], int slot)
 {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
@@ -65,9 +67,12 @@ template <int NT> __device__ __forceinline__ float row_sum(float v, float (*sums
     return v;
 }
 
+// (mean + eps)^(-1/2) of a row's sum of squares.
+__device__ __forceinline__ float scale_of(double sum, const NormArgs& p) { return (float)(1.0 / sqrt(sum / (double)p.width + (double)p.eps)); }
+
 template <GemmStore ST, GemmStore GT, int NT, int C> __global__ void __launch_bounds__(kThreads) add_norm(const NormArgs p)
 {
-    __shared__ float sums[2][kThreads / 64];
+    __shared__ double sums[2][kThreads / 64];
     constexpr int R = kThreads / NT;
     const int lane = threadIdx.x % NT;
     const int unit = blockIdx.x * R + threadIdx.x / NT;
@@ -88,12 +93,12 @@ template <GemmStore ST, GemmStore GT, int NT, int C> __global__ void __launch_bo
             for (int c = 0; c < C; ++c)
                 if (n[c] > 0) v[c] += get8n<ST>(p.res, row * p.ldr + chunk_at<NT>(lane, c), n[c]);
         }
-        float s = 0.f;
+        double s = 0.0;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s = fmaf(v[c][e], v[c][e], s);
-        const float r = 1.f / sqrtf(fmaf(row_sum<NT>(s, sums, slot), p.inv_width, p.eps));
+            for (int e = 0; e < 8; ++e) s = fma((double)v[c][e], (double)v[c][e], s);
+        const float r = scale_of(row_sum<NT>(s, sums, slot), p);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             if (n[c] > 0) {
@@ -171,7 +176,7 @@ template <GemmStore ST, GemmStore GT, int NT, int C> __global__ void __launch_bo
 // Rows that registers do not hold: a block reads each of them twice.
 template <GemmStore ST, GemmStore GT> __global__ void __launch_bounds__(kThreads) add_norm_long(const NormArgs p)
 {
-    __shared__ float sums[2][kThreads / 64];
+    __shared__ double sums[2][kThreads / 64];
     int slot = 0;
     for (int64_t row = blockIdx.x; row < p.rows; row += p.units, slot ^= 1) {
         auto sum = [&](int at, int n) {
@@ -179,13 +184,13 @@ template <GemmStore ST, GemmStore GT> __global__ void __launch_bounds__(kThreads
             if (p.res) v += get8n<ST>(p.res, row * p.ldr + at, n);
             return v;
         };
-        float s = 0.f;
+        double s = 0.0;
         for (int at = 8 * threadIdx.x; at < p.width; at += 8 * kThreads) {
             const f32x8 v = sum(at, chunk_size(p.width, at));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
+            for (int e = 0; e < 8; ++e) s = fma((double)v[e], (double)v[e], s);
         }
-        const float r = 1.f / sqrtf(fmaf(row_sum<kThreads>(s, sums, slot), p.inv_width, p.eps));
+        const float r = scale_of(row_sum<kThreads>(s, sums, slot), p);
         for (int at = 8 * threadIdx.x; at < p.width; at += 8 * kThreads) {
             const int n = chunk_size(p.width, at);
             const f32x8 v = sum(at, n), w = get8n<GT>(p.gain, at, n);

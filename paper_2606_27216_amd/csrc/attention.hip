@@ -239,11 +239,11 @@ __global__ void __launch_bounds__(kThreads, (Lay<ST, DP>::PITCH <= 256 ? 2 : 1))
             !on || l == 0.f ? -INFINITY : fmaf(run.m, p.scale, __logf(l));
 }
 
-// Few rows in all (a token or some of each sequence against many keys): a tile's 32 rows are
-// all that a group of heads has, and the keys are shared out over the waves of a block and over
-// `splits` blocks. Each wave keeps two tiles of 32 keys of its own on the way, without a
-// barrier; the waves' results meet in LDS, the blocks' in `part`: [splits] rows of DP sums and
-// of {m, l}.
+// Few tiles: the waves of a block share 32 rows and take the keys in pieces, each with two tiles of 32
+// keys of its own on the way and without a barrier; their results meet in LDS. Where the 32 rows are all
+// that a group of heads has (a token or some of each sequence against many keys), the keys are
+// shared out over `splits` blocks too, whose results meet in `part`: [splits] rows of DP sums and of
+// {m, l}.
 constexpr int kFewLds = 128 << 10;
 template <GemmStore ST, int DP> constexpr int few_waves() { return std::min(4, kFewLds / (4 * kRows * Lay<ST, DP>::PITCH)); }
 template <GemmStore ST, int DP> constexpr int few_lds()
@@ -261,14 +261,16 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     const int G = p.group, split = (int)(blockIdx.x % (uint32_t)p.splits);
     const uint32_t w = blockIdx.x / (uint32_t)p.splits;
     const int kh = (int)(w % (uint32_t)p.hk);
-    const Seq s = find_seq<false, kRows>(p, w / (uint32_t)p.hk, G);  // (one tile to a sequence)
-    const int rows = s.q_cap * G;
-    const int query = (lane & 31) / G, head = kh * G + (lane & 31) - query * G;
+    const Seq s = find_seq<false, kRows>(p, w / (uint32_t)p.hk, G);
+    const int r0 = s.tile * kRows, rows = min(kRows, s.q_cap * G - r0), in_use = s.nq * G;
+    if (rows <= 0) return;
+    const int query = (r0 + (lane & 31)) / G, head = kh * G + r0 + (lane & 31) - query * G;
     const bool exists = (lane & 31) < rows, on = query < s.nq;
     Frag<ST> q[L::NS];
     load_row<DMA, ST, DP>(q, at(p.q, s.batch, s.q0 + query, head), on && exists, p.dim, h);
 
-    const int n = s.nq > 0 ? visible(p, s, s.nq - 1) : 0, n_all = visible(p, s, 0), n_lane = on && exists ? visible(p, s, query) : 0;
+    const int n = r0 < in_use ? visible(p, s, (min(r0 + kRows, in_use) - 1) / G) : 0;  // seen by any row, by all, by this lane's
+    const int n_all = visible(p, s, r0 / G), n_lane = on && exists ? visible(p, s, query) : 0;
     const int tiles = (n + kRows - 1) / kRows, turns = (tiles + p.splits * W - 1) / (p.splits * W);
     const int first = (split * W + wave) * turns, end = min(tiles, first + turns);
     Running<ST, DP> run;
@@ -346,7 +348,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
         f[v] = from[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((from[0] - m) * c);
         l += from[0] == -INFINITY ? from[1] : f[v] * from[1];
     }
-    const int token = row / G, hd = kh * G + row - token * G;
+    const int token = (r0 + row) / G, hd = kh * G + r0 + row - token * G;
     const bool used = token < s.nq;
     float* const part = p.splits > 1 ? p.part + (((int64_t)w * p.splits + split) * kRows + row) * DS : nullptr;
     uint8_t* const out = at(p.o, s.batch, s.q0 + token, hd);
@@ -432,6 +434,11 @@ int64_t few_splits(const himuon_attn_t* a)
     return std::max<int64_t>(1, std::min<int64_t>(most, ceil_div(256, a->batch * a->k_heads)));
 }
 
+// Blocks of four times 32 rows below which the waves of a block share 32 of them. Heads of 128, 16 + 8 of
+// them, causal, first form / second, us: 1 x 128 tokens (16 blocks) bf16 11.4 / 11.2, fp32 28 / 20; 1 x 512
+// (64) 17 / 14 and 81 / 62; 2 x 512 (128) 18 / 25 and 83 / 109.
+constexpr int64_t kSharedBelow = 96;
+
 template <GemmStore ST, bool DMA> int launch_forward(AttnArgs p, bool few, hipStream_t stream)
 {
     return by_dim(p, [&](auto dim) {
@@ -452,6 +459,14 @@ template <GemmStore ST, bool DMA> int launch_forward(AttnArgs p, bool few, hipSt
         }
         int64_t blocks;
         if (!set_grid(p, p.q_len * p.group, kTileRows, kThreads, &blocks)) return (int)HIMUON_ERR_UNSUPPORTED;
+        if (blocks < kSharedBelow) {
+            constexpr int T = 64 * few_waves<ST, DP>();
+            if (!set_grid(p, p.q_len * p.group, kRows, T, &blocks)) return (int)HIMUON_ERR_UNSUPPORTED;
+            StreamDevice on(stream);
+            if (on.status != HIMUON_OK) return on.status;
+            hipLaunchKernelGGL((attn_few<ST, DP, DMA>), dim3((unsigned)blocks), dim3(T), 0, stream, p);
+            return launch_status();
+        }
         StreamDevice on(stream);
         if (on.status != HIMUON_OK) return on.status;
         hipLaunchKernelGGL((attn_forward<ST, DP, DMA>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
