@@ -109,13 +109,9 @@ __global__ void __launch_bounds__(kThreads, (Lay<ST, DP>::PITCH <= 256 ? 2 : 1))
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
-    const uint32_t w = xcd_order(blockIdx.x, gridDim.x);
-    const uint32_t items = p.packed ? p.slots : (uint32_t)p.slots * (uint32_t)p.batch;  // of a key head
-    const int kh = (int)(w / items);
-    const uint32_t at_item = w - kh * items;
-    // (a sequence's last tiles, which see the most keys, first)
-    const uint32_t slots = p.slots, tile = p.packed ? items - 1 - at_item : at_item / slots * slots + (slots - 1 - at_item % slots);
-    const Seq s = find_seq<false, kTileRows>(p, tile, G);
+    const Item item = find_item<1, true>(p, blockIdx.x, gridDim.x);
+    const int kh = item.kh;
+    const Seq s = find_seq<false, kTileRows>(p, item.item, G);
     const int rows = s.q_cap * G, r0 = s.tile * kTileRows;  // (a sequence's rows are counted in 32 bits)
     if (r0 >= rows) return;
 

@@ -104,14 +104,9 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
-    uint32_t w = xcd_order(blockIdx.x, gridDim.x);
-    const int t0 = PARTS == 1 ? 0 : (int)(w % PARTS) * DT;  // the first of this block's tiles of 32 columns
-    w /= PARTS;
-    const uint32_t items = p.packed ? p.slots : (uint32_t)p.slots * (uint32_t)p.batch;
-    const int kh = (int)(w / items);
-    const uint32_t at_item = w - kh * items;
-    const uint32_t slots = p.slots, tile = p.packed ? items - 1 - at_item : at_item / slots * slots + (slots - 1 - at_item % slots);
-    const Seq s = find_seq<false, kTileRows>(p, tile, G);
+    const Item item = find_item<PARTS, true>(p, blockIdx.x, gridDim.x);
+    const int kh = item.kh, t0 = item.part * DT;  // the first of this block's tiles of 32 columns
+    const Seq s = find_seq<false, kTileRows>(p, item.item, G);
     const int rows = s.q_cap * G, r0 = s.tile * kTileRows;  // (a sequence's rows are counted in 32 bits)
     if (r0 >= rows) return;
 
@@ -243,12 +238,9 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
-    uint32_t w = xcd_order(blockIdx.x, gridDim.x);
-    const int t0 = PARTS == 1 ? 0 : (int)(w % PARTS) * DT;
-    w /= PARTS;
-    const uint32_t items = p.packed ? p.slots : (uint32_t)p.slots * (uint32_t)p.batch;
-    const int kh = (int)(w / items);
-    const Seq s = find_seq<true, kTileRows>(p, w - kh * items, 1);
+    const Item item = find_item<PARTS, false>(p, blockIdx.x, gridDim.x);
+    const int kh = item.kh, t0 = item.part * DT;
+    const Seq s = find_seq<true, kTileRows>(p, item.item, 1);
     const int j0 = s.tile * kTileRows;  // (a sequence's first keys, which most queries see, first)
     if (j0 >= s.k_cap) return;
     const int key = j0 + wave * kRows + (lane & 31);
@@ -505,12 +497,9 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
-    uint32_t w = xcd_order(blockIdx.x, gridDim.x);
-    const int t0 = PARTS == 1 ? 0 : (int)(w % PARTS) * DT;
-    w /= PARTS;
-    const uint32_t items = p.packed ? p.slots : (uint32_t)p.slots * (uint32_t)p.batch;
-    const int kh = (int)(w / items);
-    const Seq s = find_seq<false, kRows>(p, w - kh * items, G);
+    const Item item = find_item<PARTS, true>(p, blockIdx.x, gridDim.x);
+    const int kh = item.kh, t0 = item.part * DT;
+    const Seq s = find_seq<false, kRows>(p, item.item, G);
     const int rows = s.q_cap * G, r0 = s.tile * kRows;
     if (r0 >= rows) return;
 
@@ -583,12 +572,9 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
-    uint32_t w = xcd_order(blockIdx.x, gridDim.x);
-    const int t0 = PARTS == 1 ? 0 : (int)(w % PARTS) * DT;
-    w /= PARTS;
-    const uint32_t items = p.packed ? p.slots : (uint32_t)p.slots * (uint32_t)p.batch;
-    const int kh = (int)(w / items);
-    const Seq s = find_seq<true, kRows>(p, w - kh * items, 1);
+    const Item item = find_item<PARTS, false>(p, blockIdx.x, gridDim.x);
+    const int kh = item.kh, t0 = item.part * DT;
+    const Seq s = find_seq<true, kRows>(p, item.item, 1);
     const int j0 = s.tile * kRows;
     if (j0 >= s.k_cap) return;
     const int key = j0 + (lane & 31);
