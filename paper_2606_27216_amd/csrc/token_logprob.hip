@@ -71,7 +71,7 @@ struct Sums {
 // Larger logits have larger keys, NaN the largest; of equal ones the first index.
 __device__ __forceinline__ uint32_t order_of(float x)
 {
-    if (!(x == x)) return 0xffffffffu;
+    if (!(x == x)) return 0xfffffffeu;  // (so that no key is ~0)
     const uint32_t b = __float_as_uint(x + 0.f);  // (minus zero equals zero)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }

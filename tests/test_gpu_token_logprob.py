@@ -115,6 +115,21 @@ def test_ties_masks_and_special_values(vocab, dtype):
         assert torch.equal(a[others], b[others])
 
 
+@pytest.mark.parametrize("vocab", [1, 5, 64, 3000, 20000])
+def test_nan_at_the_first_token(vocab):
+    print("[gpu-case] token_logprob first NaN", vocab, flush=True)
+    z, t = make(6, vocab, "f32", 12)
+    z[2, 0] = math.nan
+    z[4] = math.nan
+    k = min(vocab, 64)
+    got = hm.token_logprob(z, t, top=k)
+    want = ordered(torch.where(z.isnan(), math.inf, z), k)
+    assert torch.equal(got[4], want)
+    for r in (2, 4):
+        assert all(bool(x[r].isnan().all()) for x in got[:4])
+    assert all(bool(x[[0, 1, 3, 5]].isfinite().all()) for x in got[:4])
+
+
 def test_rows_not_in_use_and_empty_rows():
     z, t = make(40, 700, "f32", 4)
     t[::3] = -1
