@@ -253,7 +253,8 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
     // sequence's rows are counted in 32 bits)
     const int off = s.nk - s.nq, wj = j0 + wave * kRows;
     auto first_row = [&](int j) { return p.causal ? max(0, j - off) * G : 0; };
-    const int end = j0 < s.nk ? s.nq * G : 0, begin = first_row(j0) / BR * BR;
+    // (keys behind those in use have none, and their rows no place in 32 bits)
+    const int end = j0 < s.nk ? s.nq * G : 0, begin = j0 < s.nk ? first_row(j0) / BR * BR : 0;
     const bool w_whole = wj + kRows <= s.nk;
     const int w_begin = wj < s.nk ? first_row(wj) : INT32_MAX, w_all = w_whole ? first_row(wj + kRows - 1) : INT32_MAX;
     const int mine = on ? first_row(key) : INT32_MAX;
@@ -586,7 +587,8 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     // rows that see keys of the block, all of them, and this lane's
     const int off = s.nk - s.nq;
     auto first_row = [&](int j) { return p.causal ? max(0, j - off) * G : 0; };
-    const int end = j0 < s.nk ? s.nq * G : 0, begin = first_row(j0) / kRows * kRows;
+    // (keys behind those in use have none, and their rows no place in 32 bits)
+    const int end = j0 < s.nk ? s.nq * G : 0, begin = j0 < s.nk ? first_row(j0) / kRows * kRows : 0;
     const int all = j0 + kRows <= s.nk ? first_row(j0 + kRows - 1) : INT32_MAX, mine = on ? first_row(key) : INT32_MAX;
     const int tiles = end > begin ? (end - begin + kRows - 1) / kRows : 0;
 

@@ -230,6 +230,20 @@ def test_large_scores_and_equal_calls():
         assert torch.equal(x, y)
 
 
+def test_long_cache_with_few_keys_in_use():
+    # token times heads of the group passes 2^31 behind the keys in use
+    tokens, n = (1 << 26) + 4096, torch.tensor([40], device="cuda")
+    q, k, v, g = make((1,), 3, 128 * 100, 32, 1, 8, "bf16", "tokens", 13)  # (100 blocks of keys: the same kernels)
+    out, lse = hm.attention(q, k, v, k_lengths=n)
+    want = hm.attention_grad(g, q, k, v, out, lse, k_lengths=n)
+    K, V = (torch.zeros(1, tokens, 1, 8, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    K[:, :128 * 100], V[:, :128 * 100] = k, v
+    got = hm.attention_grad(g, q, K, V, out, lse, k_lengths=n)
+    assert torch.equal(got[0], want[0])
+    for a, b in zip(got[1:], want[1:]):
+        assert torch.equal(a[:, :128 * 100], b) and not a[:, 128 * 100:].any()
+
+
 def test_outputs_strides_and_broadcast_keys():
     q, k, v, g = make((2,), 90, 90, 4, 2, 64, "bf16", "tokens", 10)
     out, lse = hm.attention(q, k, v)
