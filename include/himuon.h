@@ -654,11 +654,11 @@ int himuon_weight_grad(int64_t n_tokens, int64_t out, int64_t cols, const void* 
  * h = x + residual (NULL: h is x, and nothing is written to h), and
  *     y = h * gain / sqrt(mean(h^2) + eps)
  * over each of n_tokens rows of `width` elements. The norm is that of the sum in
- * fp32, before h is rounded on store (the sum of its squares has to lie in fp32's range). With codes and exponents (both or neither) y is
+ * fp32, before h is rounded on store. With codes and exponents (both or neither) y is
  * kept in 8 bits too, as himuon_act_pack of the stored y gives them.
  *
- * x, residual, h, y  storage `dtype`, ld >= width. h may be x or residual, y any of
- *                    the three inputs' buffers (same ld) unless h is it too.
+ * x, residual, h, y  storage `dtype`, ld >= width. h may be x or residual, and y
+ *                    either of them unless h is it (same ld).
  * gain               width elements, storage `gain_dtype`.
  * codes              16-byte aligned.
  * width              at most 2^26; n_tokens below 2^31 (2^29 with codes).
@@ -671,7 +671,8 @@ int himuon_add_norm(int64_t n_tokens, int64_t width, const void* x, int64_t ld_x
  * Its backward pass, from the gradients g_y of y and g_h of h (NULL: none) and from
  * h: dh, the gradient of x and of the residual alike, and dgain (width elements of
  * gain_dtype, overwritten, summed over rows in an order that depends on the sizes
- * alone). dh may be g_y or g_h (same ld).
+ * alone). dh may be g_y or g_h (same ld). The sum of a row's squares has to lie in
+ * fp32's range.
  * workspace  himuon_add_norm_grad_workspace_size(n_tokens, width) bytes, 16-byte
  *            aligned.
  */
@@ -770,7 +771,8 @@ int himuon_token_logprob(int64_t n_tokens, int64_t vocab, const void* logits, in
 /*
  * The logits' gradient from those of logprob and entropy (each may be NULL: none):
  *     d[i, j] = scale * (g_logprob[i] (delta(j, tokens[i]) - p) - g_entropy[i] p (log p + entropy[i]))
- * with p from the logits and lse. Rows that are not in use, and rows whose lse is minus
+ * with p from the logits and lse, or from the logits alone where lse, 1024 or more, is
+ * rounded too far. Rows that are not in use, and rows whose lse is minus
  * infinity, get zeros; so do logits of minus infinity but for the token's own. d: storage
  * `dtype`, ld_d >= vocab; may be the logits (same ld).
  */

@@ -130,6 +130,48 @@ def test_nan_at_the_first_token(vocab):
     assert all(bool(x[[0, 1, 3, 5]].isfinite().all()) for x in got[:4])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [33, 3000, 20000, 70000])
+def test_logits_far_from_zero(vocab, dtype):
+    # lse rounds by 2^-24 of itself, which leaves the probabilities to the logits' distances: products
+    # with c = log2 e of distances to the maximum (6 U of up to D), sums of vocab terms
+    print("[gpu-case] token_logprob far", vocab, dtype, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    near = torch.randint(0, 9, (10, vocab), generator=gen, device="cuda").float()
+    t = torch.randint(0, vocab, (10,), generator=gen, device="cuda")
+    low = torch.finfo(T[dtype]).min
+    z = torch.stack([near[0] - 2.0 ** (10 if dtype == "bf16" else 20), near[1] + 2.0 ** (10 if dtype == "bf16" else 20), near[2] * 512 - 1e6,
+                     torch.full_like(near[3], -1e9), torch.full_like(near[4], low), near[5], near[6] * 512 + 1e5, near[7] - 5000, near[8] + 5000,
+                     near[9]]).to(T[dtype])
+    z[4, ::2] = -math.inf if vocab > 33 else low
+    z[9, ::3] = low
+    t[4], t[9] = 1, 1
+    s = z.double()
+    lp = torch.log_softmax(s, 1)
+    p = lp.exp()
+    H = -torch.where(p == 0, 0.0, p * lp).sum(1)
+    got = hm.token_logprob(z, t, top=min(vocab, 20))
+    D = (s.amax(1, keepdim=True) - s).clamp(0, 200) + math.log(vocab) + 1  # (beyond: a probability of less than e^-150)
+    tol = (6 * D + vocab + 16) * U
+    at = t[:, None]
+    assert bool(((got[0].double() - lp.gather(1, at)[:, 0]).abs() <= tol.gather(1, at)[:, 0] + 4 * U * lp.gather(1, at)[:, 0].abs()).all())
+    assert bool(((got[1].double() - H).abs() <= (p * (tol * (lp.abs().clamp(0, 300) + 2))).sum(1) + tol.amin(1) * (H + 2)).all())
+    lse = torch.logsumexp(s, 1)
+    assert bool(((got[2].double() - lse).abs() <= tol.amin(1) + 2 * U * lse.abs()).all())
+    assert torch.equal(got[4], ordered(z, min(vocab, 20)))
+    gl, gh = (torch.randn(10, generator=gen, device="cuda") for _ in range(2))
+    for a, b, out in ((gl, gh, None), (gl, None, z.clone()), (None, gh, None)):
+        d = hm.token_logprob_grad(a, b, z if out is None else out, t, got[2], got[1], out=out)
+        delta = torch.zeros_like(p).scatter_(1, at, 1.0)
+        A, B = (0.0 if x is None else x.double()[:, None] for x in (a, b))
+        E = got[1].double()[:, None]
+        L = lp.clamp_min(-1e30)
+        want = A * (delta - p) - B * p * (L + E)
+        e = tol + 2.0 ** -13  # (an lse below 1024 is off by 2^-14 or less, and so is a sum of two)
+        size = abs(A) * (p * e + (delta + p) * 4 * U) + abs(B) * p * ((L.abs() + E) * (e + 6 * U) + e)
+        assert bool(((d.double() - want).abs() <= size * 1.1 + want.abs() * torch.finfo(T[dtype]).eps / 2 + 1e-37).all())
+
+
 def test_rows_not_in_use_and_empty_rows():
     z, t = make(40, 700, "f32", 4)
     t[::3] = -1
