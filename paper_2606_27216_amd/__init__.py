@@ -12,7 +12,8 @@ Low-level names mirror the C ABI (``himuon_ns_tiled``, ``himuon_plan_chunks``,
 ``ns_tiled`` is the tensor-level convenience wrapper. The operators of a training
 step around the optimizer (``embed``, ``embed_grad``, ``qk_norm_rope``,
 ``qk_norm_rope_grad``, ``act_pack``, ``act_unpack``, ``weight_grad``) are in
-``train_ops``.
+``train_ops``, those of a decoder block between its projections (``add_norm``,
+``attention``, ``token_logprob`` and their gradients) in ``block_ops``.
 """
 from __future__ import annotations
 

@@ -21,8 +21,8 @@ import ctypes
 import struct
 
 from . import lib
-from .train_ops import (ACT_GROUP, I32, _away, _done, _heads, _heads_like, _HEADS, _index_code, _matrix, _new, _on,  # noqa: F401
-                        _packed, _same_device, _stream_of, _torch, _type_code, _workspace)
+from .train_ops import (ACT_GROUP, I32, _away, _done, _heads, _heads_like, _HEADS, _index_code, _matrix, _on, _same_device,
+                        _stream_of, _torch, _type_code, _workspace)
 
 MAX_ATTN_DIM = 256           # HIMUON_MAX_ATTN_DIM
 MAX_TOP = 64                 # HIMUON_MAX_TOP

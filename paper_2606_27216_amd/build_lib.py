@@ -31,7 +31,8 @@ COMMON = [
 # them after each product (fp32, T = 64: 1493 us without the flag, 1383 with it;
 # bf16 operands, T = 32 / 64 / 128 on 12 x 2048^2: 149 / 194 / 299 and 118 / 128 / 264).
 # So do the attention kernels, whose scores turn from a result into an operand: with it two waves
-# share a SIMD at a head of 128 (242 registers, 258 without it in the queries' gradient).
+# share a SIMD in the keys' gradient at a bf16 head of 64 (241 registers, 275 without it), and at an
+# fp32 head of 128 it fits without scratch memory.
 SOURCES = [
     ("ns_tiled_kernels.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
     ("ns_tiled_f16.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),

@@ -4,7 +4,8 @@
 // For a row of D elements, h = x + residual, r = (mean h^2 + eps)^(-1/2), gain w:
 //     y = h r w
 //     dh = g_h + r (g_y w - h r^2 mean(g_y w h)),   dw = sum over rows of g_y h r
-// Memory bounds both: every array is read or written once. A row is held in registers by a
+// Memory bounds both: every array is read or written once (16384 x 4096 bf16: 105 us forward, 5.1 TB/s, and 107
+// backward with the gain's 7; a copy of 2 GiB runs at 4.9); few rows the host (32 x 4096: 4.4 us of 10.6). A row is held in registers by a
 // wave or by a block of four (rows of more than 1024 elements), which walks over rows with the
 // gain, and in the backward pass the sums of its gradient, in registers too. A row's sums
 // are its waves' in their order.

@@ -41,9 +41,9 @@ template <int N> HM_DEV void dma16_run(uint32_t dst, const uint32_t (&voff)[N], 
                      "v"(voff[0]), "v"(voff[1]), "s"(base)
                      : "m0", "memory");
     } else {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(dst),
-                     "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(base)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:%6\n\t"
+                     "global_load_lds_dwordx4 %3, %5 offset:%7\n\tglobal_load_lds_dwordx4 %4, %5 offset:%8" ::"s"(dst),
+                     "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(base), "n"(1024), "n"(2 * 1024), "n"(3 * 1024)
                      : "m0", "memory");
     }
 }
