@@ -4,10 +4,16 @@
 //     dv = p^T g,  dk = c ds^T q,  dq = c ds k
 // from the forward pass's inputs, o and lse. Two kernels: one whose waves hold 32 rows of queries
 // and walk over the keys (dq; it also leaves every row's lse and D behind for the other one), and
-// one whose waves hold 32 keys and walk over the rows of the head's whole group (dk, dv). Scores
+// one whose waves hold 32 keys and walk over the rows of the head's whole group (dk, dv). (Few
+// tiles: both in one launch, behind one that computes lse and D.) Scores
 // are computed in both: seven products instead of five, but no sum is shared between blocks, so
 // that results have one order of summation and there are no atomics. As in the forward pass p and
 // ds are a product's second operand as they stand.
+//
+// What bounds it: the issue of instructions, and in the keys' kernel one wave to a SIMD, as its
+// registers hold two operands and two sums of 32 keys (causal bf16, 16 x 1024 tokens, 16 + 8 heads of 128:
+// queries' side 145 us, keys' 200; 2 x 4096 with 32 + 8 heads 890 both, 0.77 PFLOP/s of the five products that
+// the mathematics asks for); in fp32 the products (8 x 1024 tokens 1100 us).
 #include "attn_device.h"
 
 #include <algorithm>
@@ -45,24 +51,25 @@ HM_DEV void row_product(f32x16& x, const uint8_t* tile, const Frag<ST> (&f)[DP /
 // The same, of the first `steps` parts of 16 columns alone.
 template <GemmStore ST, int DP> HM_DEV void row_product_of(int steps, f32x16& x, const uint8_t* tile, const Frag<ST> (&f)[DP / 16], int lane)
 {
+    auto read = [=](int i) __attribute__((always_inline)) { return Lay<ST, DP>::row_frag(tile, lane & 31, i, lane >> 5); };
+    Ahead<Frag<ST>, DP / 16, kDepth<ST, DP>> r;
     x = f32x16{};
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) {
-        if (i < steps) mma<ST>(x, Lay<ST, DP>::row_frag(tile, lane & 31, i, lane >> 5), f[i]);
-    }
+    r.fill(read);
+    r.run(read, [&](int i, const Frag<ST>& a) {
+        if (i < steps) mma<ST>(x, a, f[i]);
+    });
 }
 
 // acc[t] += columns 32 (t0 + t) .. of a tile times an operand, t below `cols`.
 template <GemmStore ST, int DP, int DT>
 HM_DEV void col_product(f32x16 (&acc)[DT], const uint8_t* tile, const Frag<ST> (&f)[2], int t0, int cols, int lane)
 {
-#pragma unroll
-    for (int t = 0; t < DT; ++t) {
-        if (t < cols) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) mma<ST>(acc[t], Lay<ST, DP>::col_frag(tile, 16 * u, 32 * (t0 + t), lane), f[u]);
-        }
-    }
+    auto read = [=](int i) __attribute__((always_inline)) { return Lay<ST, DP>::col_frag(tile, 16 * (i & 1), 32 * (t0 + (i >> 1)), lane); };
+    Ahead<Frag<ST>, 2 * DT, kDepth<ST, DP>> r;
+    r.fill(read);
+    r.run(read, [&](int i, const Frag<ST>& a) {
+        if (i >> 1 < cols) mma<ST>(acc[i >> 1], a, f[i & 1]);
+    });
 }
 
 // A row in memory times one held as fragments.
@@ -451,7 +458,10 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
 }
 
 // Where tiles are few, the waves of a block share 32 rows (keys) and take the other side's tiles in
-// turn, each through LDS of its own and without a barrier; their sums meet there in the end.
+// turn, each through LDS of its own and without a barrier; their sums meet there in the end. (fp32, 901
+// packed tokens in documents, 12 + 4 heads of 80: 78 us both sides, 112 in a launch of each; 1 x 512 tokens, 16 + 8
+// heads of 128 109, of which the products' cycles on the longest block's way are 55. Copying a tile's rows in
+// an order that hid them behind products changed nothing.)
 constexpr int kSharedLds = 128 << 10;
 template <int W, int TILE, int DT> constexpr int shared_lds() { return W * std::max(2 * TILE, kRows * (32 * DT + 4) * (int)sizeof(float)); }
 template <GemmStore ST, int DP> constexpr int shared_waves() { return std::min(4, kSharedLds / (2 * kRows * Lay<ST, DP>::PITCH)); }
@@ -490,15 +500,15 @@ HM_DEV void join_waves(uint8_t* lds, const f32x16 (&acc)[N][DT], const float (&m
     }
 }
 
-template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 * shared_waves<ST, DP>())) attn_grad_q_shared(const AttnArgs p)
+// Block `id` of `n` of queries. lds: of each wave keys and values, then [waves] sums.
+template <GemmStore ST, int DP, bool DMA> HM_DEV void grad_q_shared(const AttnArgs& p, uint8_t* lds, uint32_t id, uint32_t n_blocks)
 {
     using L = Lay<ST, DP>;
     constexpr int W = shared_waves<ST, DP>(), TILE = kRows * L::PITCH, PARTS = q_parts<ST, DP>(), DT = L::DT / PARTS;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[shared_lds<W, TILE, DT>()];  // of each wave: keys, values; then [waves] sums
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
-    const Item item = find_item<PARTS, true>(p, blockIdx.x, gridDim.x);
+    const Item item = find_item<PARTS, true>(p, id, n_blocks);
     const int kh = item.kh, t0 = item.part * DT;
     const Seq s = find_seq<false, kRows>(p, item.item, G);
     const int rows = s.q_cap * G, r0 = s.tile * kRows;
@@ -512,10 +522,8 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     Frag<ST> q[L::NS], g[L::NS];
     load_row<DMA, ST, DP>(q, at(p.q, s.batch, s.q0 + query, head), on, p.dim, h);
     load_row<DMA, ST, DP>(g, at(p.g, s.batch, s.q0 + query, head), on, p.dim, h);
-    const float d = row_dot<DMA, ST, DP>(g, at(p.o, s.batch, s.q0 + query, head), on, p.dim, h);
-    const float c = p.scale * kLog2e;
-    const float lse = on ? p.lse[((int64_t)s.batch * p.q_len + s.q0 + query) * ((int64_t)p.hk * G) + head] * kLog2e : INFINITY;
-    if (r < rows && threadIdx.x < 32 && t0 == 0) p.stats[stat_row(p, s, kh, r)] = float2{lse, d};
+    const float2 st = r < rows ? p.stats[stat_row(p, s, kh, r)] : float2{INFINITY, 0.f};
+    const float c = p.scale * kLog2e, lse = st.x, d = st.y;
 
     const int in_use = s.nq * G;
     auto seen = [&](int row) { return row < in_use ? visible(p, s, (int)((uint32_t)row / (uint32_t)G)) : 0; };
@@ -565,15 +573,15 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     }, [&](int row) { return seen(r0 + row) > 0; });
 }
 
-template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 * shared_waves<ST, DP>())) attn_grad_kv_shared(const AttnArgs p)
+// Block `id` of `n` of keys. lds: of each wave rows of q and of g, then [waves] sums.
+template <GemmStore ST, int DP, bool DMA> HM_DEV void grad_kv_shared(const AttnArgs& p, uint8_t* lds, float* stats_lds, uint32_t id, uint32_t n_blocks)
 {
     using L = Lay<ST, DP>;
     constexpr int W = shared_waves<ST, DP>(), TILE = kRows * L::PITCH, PARTS = kv_parts<ST, DP>(), DT = L::DT / PARTS;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[shared_lds<W, TILE, DT>()];  // of each wave: rows of q, of g; then [waves] sums
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5;
     const int G = p.group;
 
-    const Item item = find_item<PARTS, false>(p, blockIdx.x, gridDim.x);
+    const Item item = find_item<PARTS, false>(p, id, n_blocks);
     const int kh = item.kh, t0 = item.part * DT;
     const Seq s = find_seq<true, kRows>(p, item.item, 1);
     const int j0 = s.tile * kRows;
@@ -599,13 +607,18 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     const int row_bytes = p.dim * L::ES, steps = (p.dim + 15) / 16, cols = min(DT, (p.dim + 31) / 32 - t0);
     const uint8_t *const qp = at(p.q, s.batch, s.q0, kh * G), *const gp = at(p.g, s.batch, s.q0, kh * G);
     uint8_t *const qt = lds + wave * 2 * TILE, *const gt = qt + TILE;
+    float* const st = stats_lds + wave * 2 * kRows;  // a tile's lse, then its D
     const float2* const stats = p.stats + stat_row(p, s, kh, 0);
     const Share<ST, DP, kRows, 64> share{lane};
+    const uint32_t over_g = (65535u + (uint32_t)G) / (uint32_t)G;
     auto load = [&](uint8_t* to, const uint8_t* from, const Heads& x, int t) __attribute__((always_inline)) {
-        const int r0 = begin + t * kRows;
-        share.template stage<DMA>(to, from, row_bytes, false, [&](int i) {
-            const uint32_t r = (uint32_t)(r0 + share.row(i)), token = r / (uint32_t)G;
-            return token * x.ss + (int64_t)(r - token * (uint32_t)G) * x.sh;
+        // A row lies less than G + 32 behind its tile's first token: the tokens in between without a
+        // division (below 32 times 2^16 / G, rounded up, is exact to 2^16).
+        const int r0 = begin + t * kRows, token0 = (int)((uint32_t)r0 / (uint32_t)G), place0 = r0 - token0 * G;
+        share.template stage<DMA>(to, from + token0 * x.ss, row_bytes, false, [&](int i) {
+            const int place = place0 + share.row(i);
+            const int tokens = G < kRows ? (int)((uint32_t)place * over_g >> 16) : place >= G;
+            return tokens * x.ss + (int64_t)(place - tokens * G) * x.sh;
         }, [&](int i) { return r0 + share.row(i) < end; });
     };
     if (wave < tiles) {
@@ -615,17 +628,18 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
 #pragma unroll 1
     for (int t = wave; t < tiles; t += W) {
         const int r0 = begin + t * kRows;
-        // (a lane holds one row's lse and D, and hands them to the registers of that row)
         const float2 mine_st = r0 + (lane & 31) < end ? stats[r0 + (lane & 31)] : float2{INFINITY, 0.f};
         wave_wait<0>();
+        st[lane] = h ? mine_st.y : mine_st.x;
         f32x16 x, y;
         Frag<ST> pr[2], ds[2];
         row_product_of<ST, DP>(steps, x, qt, k, lane);
         row_product_of<ST, DP>(steps, y, gt, v, lane);
+        wave_wait<-1>();
         const int hidden = r0 < all ? min(mine - r0, kRows) - 4 * h : INT32_MIN;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const float lse = __shfl(mine_st.x, result_row(i, h)), d = __shfl(mine_st.y, result_row(i, h));
+            const float lse = st[result_row(i, h)], d = st[kRows + result_row(i, h)];
             x[i] = result_row(i, 0) < hidden ? 0.f : __builtin_amdgcn_exp2f(fmaf(x[i], c, -lse));
             y[i] = result_row(i, 0) < hidden ? 0.f : x[i] * (y[i] - d);
         }
@@ -646,14 +660,51 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 
     }, [&](int row) { return j0 + row < s.nk; });
 }
 
+// Both in one launch, keys first: a block of either has a CU to itself, and where blocks are few the
+// queries' run on the CUs that the keys' leave. Every row's lse and D have to be there before.
+template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__((64 * shared_waves<ST, DP>())) attn_grad_shared(const AttnArgs p)
+{
+    constexpr int W = shared_waves<ST, DP>(), TILE = kRows * Lay<ST, DP>::PITCH, DT = Lay<ST, DP>::DT;
+    constexpr int Q = shared_lds<W, TILE, DT / q_parts<ST, DP>()>(), KV = shared_lds<W, TILE, DT / kv_parts<ST, DP>()>();
+    __shared__ __attribute__((aligned(16))) uint8_t lds[std::max(Q, KV)];
+    __shared__ __attribute__((aligned(16))) float stats[W * 2 * kRows];
+    const uint32_t of_keys = (uint32_t)p.k_blocks;
+    if (blockIdx.x < of_keys) {
+        AttnArgs k = p;
+        k.slots = p.k_slots;
+        grad_kv_shared<ST, DP, DMA>(k, lds, stats, blockIdx.x, of_keys);
+    } else {
+        grad_q_shared<ST, DP, DMA>(p, lds, blockIdx.x - of_keys, gridDim.x - of_keys);
+    }
+}
+
+// lse and D of every row.
+template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThreads) attn_grad_rows(const AttnArgs p)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x) >> 6, h = lane >> 5, G = p.group;
+    const Item item = find_item<1, true>(p, blockIdx.x, gridDim.x);
+    const Seq s = find_seq<false, kTileRows>(p, item.item, G);
+    const int r = s.tile * kTileRows + wave * kRows + (lane & 31);
+    const int query = (int)((uint32_t)r / (uint32_t)G), head = item.kh * G + (int)((uint32_t)r - (uint32_t)query * (uint32_t)G);
+    const bool exists = r < s.q_cap * G, on = exists && query < s.nq && visible(p, s, query) > 0;
+    Frag<ST> g[DP / 16];
+    load_row<DMA, ST, DP>(g, at(p.g, s.batch, s.q0 + query, head), on, p.dim, h);
+    const float d = row_dot<DMA, ST, DP>(g, at(p.o, s.batch, s.q0 + query, head), on, p.dim, h);
+    if (!exists || h != 0) return;
+    const float lse = on ? p.lse[((int64_t)s.batch * p.q_len + s.q0 + query) * ((int64_t)p.hk * G) + head] * kLog2e : INFINITY;
+    p.stats[stat_row(p, s, item.kh, r)] = float2{lse, d};
+}
+
 // ---------------------------------------------------------------- host side
 
-// Blocks of four times 32 rows below which the waves of a block share 32 of them: where the first
-// kind leaves the chip idle, with one wave on the long way over the other side's tiles. Heads of 128,
-// 16 + 8 of them, causal, both kernels in the first form / the second, us: fp32 1 x 512 tokens 386 / 155
-// (32 blocks of keys), 2 x 1024 756 / 478 (128), 4 x 1024 919 / 918 (256), 8 x 1024 1724 / 1792 (512); bf16
-// 1 x 128 31 / 25 (8), 2 x 512 61 / 57 (64), 4 x 512 65 / 100 (128).
+// Blocks of four times 32 keys (rows) below which the waves of a block share 32 of them: where the
+// first kind leaves the chip idle, with one wave on the long way over the other side's tiles. Heads of 128,
+// 16 + 8 of them, causal, first form / second, us: fp32 1 x 128 tokens 111 / 38 (8 blocks of keys, 16 of
+// rows), 1 x 512 382 / 109 (32, 64), 2 x 1024 747 / 386 (128, 256), 4 x 1024 774 / 771 (256, 512; keys in the second
+// and rows in the first 660), 8 x 1024 1093 / 1551; bf16 1 x 128 29 / 20, 1 x 512 57 / 35, 2 x 512 59 / 46 (64, 128;
+// keys in the second and rows in the first 50), 4 x 512 61 / 79 (128, 256).
 template <GemmStore ST> constexpr int64_t shared_below() { return ST == GemmStore::F32 ? 512 : 96; }
+template <GemmStore ST> int64_t rows_shared_below(bool keys) { return ST == GemmStore::F32 ? 512 : keys ? 192 : 96; }
 template <GemmStore ST, bool DMA, int DP> int launch_grad(AttnArgs p, hipStream_t stream)
 {
     int64_t q_blocks = 0, k_blocks = 0;
@@ -663,22 +714,25 @@ template <GemmStore ST, bool DMA, int DP> int launch_grad(AttnArgs p, hipStream_
         !set_grid(pk, pk.k_len, kTileRows, kThreads * kv_parts<ST, DP>(), &k_blocks))
         return HIMUON_ERR_UNSUPPORTED;
     constexpr int T = 64 * shared_waves<ST, DP>();
-    const bool q_shared = q_blocks < shared_below<ST>(), k_shared = k_blocks < shared_below<ST>();
-    if ((q_shared && !set_grid(p, p.q_len * p.group, kRows, T * q_parts<ST, DP>(), &q_blocks)) ||
-        (k_shared && !set_grid(pk, pk.k_len, kRows, T * kv_parts<ST, DP>(), &k_blocks)))
+    const bool k_shared = p.k_len > 0 && k_blocks < shared_below<ST>();
+    const bool q_shared = p.q_len > 0 && q_blocks < rows_shared_below<ST>(k_shared);
+    AttnArgs ps = p;
+    int64_t qs_blocks = 0, ks_blocks = 0;
+    if ((q_shared && !set_grid(ps, p.q_len * p.group, kRows, T * q_parts<ST, DP>(), &qs_blocks)) ||
+        (k_shared && !set_grid(pk, pk.k_len, kRows, T * kv_parts<ST, DP>(), &ks_blocks)))
         return HIMUON_ERR_UNSUPPORTED;
-    q_blocks *= q_parts<ST, DP>();
-    k_blocks *= kv_parts<ST, DP>();
+    ps.k_slots = pk.slots;
+    ps.k_blocks = (int32_t)(ks_blocks * kv_parts<ST, DP>());
+    const int64_t blocks = qs_blocks * q_parts<ST, DP>() + ps.k_blocks;
+    if (blocks > 0 && !launchable(blocks, T)) return HIMUON_ERR_UNSUPPORTED;
     StreamDevice on(stream);
     if (on.status != HIMUON_OK) return on.status;
-    if (p.q_len > 0) {
-        if (q_shared) hipLaunchKernelGGL((attn_grad_q_shared<ST, DP, DMA>), dim3((unsigned)q_blocks), dim3(T), 0, stream, p);
-        else hipLaunchKernelGGL((attn_grad_q<ST, DP, DMA>), dim3((unsigned)q_blocks), dim3(kThreads), 0, stream, p);
-    }
-    if (p.k_len > 0) {
-        if (k_shared) hipLaunchKernelGGL((attn_grad_kv_shared<ST, DP, DMA>), dim3((unsigned)k_blocks), dim3(T), 0, stream, pk);
-        else hipLaunchKernelGGL((attn_grad_kv<ST, DP, DMA>), dim3((unsigned)k_blocks), dim3(kThreads), 0, stream, pk);
-    }
+    if (q_shared) hipLaunchKernelGGL((attn_grad_rows<ST, DP, DMA>), dim3((unsigned)q_blocks), dim3(kThreads), 0, stream, p);
+    else if (p.q_len > 0)
+        hipLaunchKernelGGL((attn_grad_q<ST, DP, DMA>), dim3((unsigned)(q_blocks * q_parts<ST, DP>())), dim3(kThreads), 0, stream, p);
+    if (blocks > 0) hipLaunchKernelGGL((attn_grad_shared<ST, DP, DMA>), dim3((unsigned)blocks), dim3(T), 0, stream, ps);
+    if (p.k_len > 0 && !k_shared)
+        hipLaunchKernelGGL((attn_grad_kv<ST, DP, DMA>), dim3((unsigned)(k_blocks * kv_parts<ST, DP>())), dim3(kThreads), 0, stream, pk);
     return launch_status();
 }
 

@@ -21,7 +21,6 @@ using dev::u32x2;
 using dev::u32x4;
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr float kLn2 = 0.693147180559945309f;
 constexpr int kRows = 32;  // of a wave: rows or columns of a product's tile
 
 // ------------------------------------------------------------------ arguments
@@ -38,7 +37,8 @@ struct AttnArgs {
     float* part;        // few rows: partial results
     const void *qs, *ks, *ql, *kl;  // starts and lengths
     int64_t q_len, k_len;
-    int32_t batch, hk, group, dim, causal, wide, packed, slots, splits, span;
+    int32_t batch, hk, group, dim, causal, wide, packed, slots, splits;
+    int32_t k_blocks, k_slots;  // backward, few tiles: the blocks of keys ahead of those of queries, and their slots
     float scale;
 };
 

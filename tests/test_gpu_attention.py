@@ -205,6 +205,15 @@ def test_padded_batches_and_caches(dtype):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("batch,nq,nk,hq,hk,dtype", [(4, 512, 512, 16, 2, "bf16"), (4, 512, 480, 32, 2, "f32"), (2, 40, 2300, 4, 4, "bf16"),
+                                                      (2, 500, 520, 16, 8, "bf16"), (2, 200, 200, 12, 4, "f32")])
+def test_few_tiles_of_either_side(batch, nq, nk, hq, hk, dtype, causal):
+    q, k, v, g = make((batch,), nq, nk, hq, hk, 80, dtype, "tokens", 14)
+    n, m = (torch.tensor([c] + [c // 3] * (batch - 1), device="cuda") for c in (nq, nk))
+    check(q, k, v, g, causal=causal, q_lengths=n, k_lengths=m)
+
+
 def test_lengths_outside_are_cut():
     """Starts and lengths beyond the tokens there are do not reach outside of them."""
     q, k, v, g = make((2,), 50, 50, 2, 1, 64, "f32", "tokens", 8)
