@@ -171,6 +171,8 @@ def _attn_args(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale)
     dim, dev = sq[-1], q.device
     if len(sk) != len(sq) or sk[-1] != dim or k.dtype != q.dtype or k.device != dev:
         raise ValueError("q and k must share dimensions, head size, type and device")
+    if dim < 1:
+        raise ValueError("heads must have at least one element")
     hv = _heads_like(v, "v", sk, k)
     if sk[-2] < 1 or sq[-2] % sk[-2]:
         raise ValueError("the number of query heads must be a multiple of the number of key heads")

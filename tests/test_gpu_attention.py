@@ -268,6 +268,12 @@ def test_outputs_strides_and_broadcast_keys():
         assert torch.equal(x, y)
 
 
+def test_heads_without_elements_are_refused():
+    q = torch.zeros(1, 3, 2, 0, device="cuda")
+    with pytest.raises(ValueError):
+        hm.attention(q, q, q)
+
+
 def test_empty_calls():
     q, k, v, g = make((2,), 5, 0, 2, 1, 64, "f32", "tokens", 11)
     out, lse = hm.attention(q, k, v)
