@@ -671,8 +671,8 @@ int himuon_add_norm(int64_t n_tokens, int64_t width, const void* x, int64_t ld_x
  * Its backward pass, from the gradients g_y of y and g_h of h (NULL: none) and from
  * h: dh, the gradient of x and of the residual alike, and dgain (width elements of
  * gain_dtype, overwritten, summed over rows in an order that depends on the sizes
- * alone). dh may be g_y or g_h (same ld). The sum of a row's squares has to lie in
- * fp32's range.
+ * alone). dh may be g_y or g_h (same ld). A row's sums are taken in fp64: its squares may
+ * leave fp32's range, as in the forward pass.
  * workspace  himuon_add_norm_grad_workspace_size(n_tokens, width) bytes, 16-byte
  *            aligned.
  */

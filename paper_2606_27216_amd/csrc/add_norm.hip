@@ -3,7 +3,7 @@
 //
 // For a row of D elements, h = x + residual, r = (mean h^2 + eps)^(-1/2), gain w:
 //     y = h r w
-//     dh = g_h + r (g_y w - h r^2 mean(g_y w h)),   dw = sum over rows of g_y h r
+//     dh = g_h + r (g_y w - h r mean(g_y w h r)),   dw = sum over rows of g_y h r
 // Memory bounds both: every array is read or written once (16384 x 4096 bf16: 105 us forward, 5.1 TB/s, and 107
 // backward with the gain's 7; a copy of 2 GiB runs at 4.9); few rows the host (32 x 4096: 4.4 us of 10.6). A row is held in registers by a
 // wave or by a block of four (rows of more than 1024 elements), which walks over rows with the
@@ -26,7 +26,8 @@ struct NormArgs {
     float* part;
     int64_t ldx, ldr, ldh, ldy, ldgy, ldgh, rows;
     int32_t width, units;
-    float eps, inv_width;
+    float eps;
+    double inv_width;
 };
 
 // A lane's chunks of eight elements of a row: NT lanes hold it, C chunks each.
@@ -54,9 +55,10 @@ template <GemmStore ST> __device__ __forceinline__ void put8n(void* base, int64_
 }
 
 // The sum over a row's NT lanes, in every one of them. `slot` alternates from row to row.
-// (F: the forward pass sums squares in 64 bits, which memory hides: r is then off by half a step of 32 bits,
-// and y's roundings to 16 and 8 bits fall where the definition's do.)
-template <int NT, class F> __device__ __forceinline__ F row_sum(F v, F (*sums)[kThreads / 64], int slot)
+// (Sums over rows are in 64 bits, which memory hides: r is then off by half a step of 32 bits, y's roundings
+// to 16 and 8 bits fall where the definition's do, and rows whose squares leave fp32's range keep r and
+// their gradient.)
+template <int NT> __device__ __forceinline__ double row_sum(double v, double (*sums)[kThreads / 64], int slot)
 {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
@@ -70,6 +72,20 @@ template <int NT, class F> __device__ __forceinline__ F row_sum(F v, F (*sums)[k
 
 // (mean + eps)^(-1/2) of a row's sum of squares.
 __device__ __forceinline__ float scale_of(double sum, const NormArgs& p) { return (float)(1.0 / sqrt(sum / (double)p.width + (double)p.eps)); }
+
+// r of a row and mean(g_y w h r), from its sums of h^2 and of g_y w h. (h r and that mean are of the gradients'
+// size whatever h's is. An estimate of 2^-23 and a step of Newton's, which takes it to 2^-44: a division and
+// a root of 64 bits would cost the registers of a wave.)
+struct RowTerms {
+    float r, mean;
+    __device__ __forceinline__ RowTerms(double s, double t, const NormArgs& p)
+    {
+        const double x = fma(s, p.inv_width, (double)p.eps), y = __builtin_amdgcn_rsq(x);
+        const double root = y * fma(-0.5 * x * y, y, 1.5);
+        r = (float)root;
+        mean = (float)(t * root * p.inv_width);
+    }
+};
 
 template <GemmStore ST, GemmStore GT, int NT, int C> __global__ void __launch_bounds__(kThreads) add_norm(const NormArgs p)
 {
@@ -110,13 +126,15 @@ template <GemmStore ST, GemmStore GT, int NT, int C> __global__ void __launch_bo
     }
 }
 
-template <GemmStore ST, GemmStore GT, int NT, int C> __global__ void __launch_bounds__(kThreads) add_norm_grad(const NormArgs p)
+// (All of a launch's 1024 blocks are on the chip at once while a row has at most 4096 elements: four to a CU. With three of
+// them 16384 x 4096 bf16 takes 171 us, not 113.)
+template <GemmStore ST, GemmStore GT, int NT, int C> __global__ void __launch_bounds__(kThreads, (C <= 2 ? 4 : C == 4 ? 2 : 1)) add_norm_grad(const NormArgs p)
 {
-    __shared__ float sums[4][kThreads / 64];
+    __shared__ double sums[4][kThreads / 64];
     __shared__ float join[NT == 64 ? kThreads * C * 8 : 1];
     constexpr int R = kThreads / NT;
     const int lane = threadIdx.x % NT;
-    const int unit = blockIdx.x * R + threadIdx.x / NT;
+    const int unit = blockIdx.x * R + (R == 1 ? 0 : threadIdx.x / NT);
     f32x8 w[C], dw[C];
     int n[C];
 #pragma unroll
@@ -134,23 +152,25 @@ template <GemmStore ST, GemmStore GT, int NT, int C> __global__ void __launch_bo
             g[c] = n[c] > 0 ? get8n<ST>(p.gy, row * p.ldgy + chunk_at<NT>(lane, c), n[c]) : f32x8{};
             a[c] = p.gh && n[c] > 0 ? get8n<ST>(p.gh, row * p.ldgh + chunk_at<NT>(lane, c), n[c]) : f32x8{};
         }
-        float s = 0.f, t = 0.f;
+        double s = 0.0, t = 0.0;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                s = fmaf(h[c][e], h[c][e], s);
-                t = fmaf(g[c][e] * w[c][e], h[c][e], t);
+                s = fma((double)h[c][e], (double)h[c][e], s);
+                t = fma((double)(g[c][e] * w[c][e]), (double)h[c][e], t);
+                asm volatile("" : "+v"(s), "+v"(t));  // (one after the other: conversions ahead of them cost a wave's registers)
             }
         s = row_sum<NT>(s, sums, slot);
         t = row_sum<NT>(t, sums, slot + 1);
-        const float r = 1.f / sqrtf(fmaf(s, p.inv_width, p.eps)), f = r * r * t * p.inv_width;
+        const RowTerms f(s, t, p);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                dw[c][e] = fmaf(g[c][e], h[c][e] * r, dw[c][e]);
-                a[c][e] = fmaf(r, g[c][e] * w[c][e] - h[c][e] * f, a[c][e]);
+                const float n = h[c][e] * f.r;
+                dw[c][e] = fmaf(g[c][e], n, dw[c][e]);
+                a[c][e] = fmaf(f.r, fmaf(-n, f.mean, g[c][e] * w[c][e]), a[c][e]);
             }
             if (n[c] > 0) put8n<ST>(p.y, row * p.ldy + chunk_at<NT>(lane, c), n[c], a[c]);
         }
@@ -204,32 +224,33 @@ template <GemmStore ST, GemmStore GT> __global__ void __launch_bounds__(kThreads
 // The gain's gradient goes to `part` as its own blocks' sums: they are read and written there.
 template <GemmStore ST, GemmStore GT> __global__ void __launch_bounds__(kThreads) add_norm_grad_long(const NormArgs p)
 {
-    __shared__ float sums[4][kThreads / 64];
+    __shared__ double sums[4][kThreads / 64];
     float* const out = p.part + (int64_t)blockIdx.x * p.width;
     for (int at = 8 * threadIdx.x; at < p.width; at += 8 * kThreads) put8n<GemmStore::F32>(out, at, chunk_size(p.width, at), f32x8{});
     int slot = 0;
     for (int64_t row = blockIdx.x; row < p.rows; row += p.units, slot ^= 2) {
-        float s = 0.f, t = 0.f;
+        double s = 0.0, t = 0.0;
         for (int at = 8 * threadIdx.x; at < p.width; at += 8 * kThreads) {
             const int n = chunk_size(p.width, at);
             const f32x8 h = get8n<ST>(p.h, row * p.ldh + at, n), g = get8n<ST>(p.gy, row * p.ldgy + at, n), w = get8n<GT>(p.gain, at, n);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                s = fmaf(h[e], h[e], s);
-                t = fmaf(g[e] * w[e], h[e], t);
+                s = fma((double)h[e], (double)h[e], s);
+                t = fma((double)(g[e] * w[e]), (double)h[e], t);
             }
         }
         s = row_sum<kThreads>(s, sums, slot);
         t = row_sum<kThreads>(t, sums, slot + 1);
-        const float r = 1.f / sqrtf(fmaf(s, p.inv_width, p.eps)), f = r * r * t * p.inv_width;
+        const RowTerms f(s, t, p);
         for (int at = 8 * threadIdx.x; at < p.width; at += 8 * kThreads) {
             const int n = chunk_size(p.width, at);
             const f32x8 h = get8n<ST>(p.h, row * p.ldh + at, n), g = get8n<ST>(p.gy, row * p.ldgy + at, n), w = get8n<GT>(p.gain, at, n);
             f32x8 a = p.gh ? get8n<ST>(p.gh, row * p.ldgh + at, n) : f32x8{}, d = get8n<GemmStore::F32>(out, at, n);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                d[e] = fmaf(g[e], h[e] * r, d[e]);
-                a[e] = fmaf(r, g[e] * w[e] - h[e] * f, a[e]);
+                const float n = h[e] * f.r;
+                d[e] = fmaf(g[e], n, d[e]);
+                a[e] = fmaf(f.r, fmaf(-n, f.mean, g[e] * w[e]), a[e]);
             }
             put8n<GemmStore::F32>(out, at, n, d);
             put8n<ST>(p.y, row * p.ldy + at, n, a);
@@ -352,7 +373,7 @@ extern "C" int himuon_add_norm(int64_t n_tokens, int64_t width, const void* x, i
     p.rows = n_tokens;
     p.width = (int32_t)width;
     p.eps = eps;
-    p.inv_width = 1.f / (float)width;
+    p.inv_width = 1.0 / (double)width;
     const int status = launch_types<false>(p, dtype, gain_dtype, static_cast<hipStream_t>(stream));
     if (status != HIMUON_OK || !codes) return status;
     return himuon_act_pack(n_tokens, width, y, ld_y, dtype, codes, exponents, stream);
@@ -396,7 +417,7 @@ extern "C" int himuon_add_norm_grad(int64_t n_tokens, int64_t width, const void*
     p.rows = n_tokens;
     p.width = (int32_t)width;
     p.eps = eps;
-    p.inv_width = 1.f / (float)width;
+    p.inv_width = 1.0 / (double)width;
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     const int status = launch_types<true>(p, dtype, gain_dtype, hs);
     if (status != HIMUON_OK) return status;

@@ -1,0 +1,52 @@
+"""add_norm and add_norm_grad on rows whose squares leave fp32's range, against the definition in
+64 bits.
+
+Tolerances (U = 2^-24): sums over a row are taken in 64 bits of products that round once or
+not at all, so a sum is off by U of its terms' magnitudes. y: the addition (by itself and in
+r) 2 U, r, two products: 6 U at the most. dh: r, h r, their mean's terms and its rounding, two products, the difference
+and the last multiply-add: 12 U of the parts' magnitudes. dgain: h r is off by 2 U and a sum
+of n rows by n U. Stores: half a step.
+"""
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2606_27216_amd as hm
+
+pytestmark = pytest.mark.gpu
+T = {"f32": torch.float32, "bf16": torch.bfloat16}
+U = 2.0 ** -24
+
+
+def close(got, want, tol):
+    off = (got.double() - want).abs()
+    assert bool(got.isfinite().all())
+    assert bool((off <= tol).all()), f"worst {float((off / tol.clamp_min(1e-300)).max()):.3g} times the tolerance"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [100, 1000, 2048, 4096, 8192, 16384, 16400])
+@pytest.mark.parametrize("scale,eps", [(1e19, 1e-6), (1e25, 1e-6), (1e30, 1e-6), (1e-25, 0.0), (1e-12, 1e-6)])
+def test_large_and_small_rows(scale, eps, width, dtype):
+    print("[gpu-case] add_norm range", scale, width, dtype, flush=True)
+    rows, e = 9, torch.finfo(T[dtype]).eps / 2
+    gen = torch.Generator(device="cuda").manual_seed(width)
+
+    def one(size):
+        return (torch.randn(rows, width, generator=gen, device="cuda") * size).to(T[dtype])
+    x, res, gy, gh = one(scale), one(scale), one(0.1), one(0.1 / scale)
+    x[4], res[4] = one(1.0)[0], one(1.0)[0]  # (a row like others beside them)
+    w = 1 + 0.3 * torch.randn(width, generator=gen, device="cuda")
+    h, y = hm.add_norm(x, res, w, eps=eps)
+    s, W = x.double() + res.double(), w.double()
+    r = (s.square().mean(1, keepdim=True) + eps).rsqrt()
+    want = s * r * W
+    close(y, want, want.abs() * (e + 6 * U))
+    H, G = h.double(), gy.double()
+    r = (H.square().mean(1, keepdim=True) + eps).rsqrt()
+    for up in (gh, None):
+        dh, dw = hm.add_norm_grad(gy, h, w, g_h=up, eps=eps)
+        part = r * (G * W - H * r * r * (G * W * H).mean(1, keepdim=True))
+        size = r * ((G * W).abs() + H.abs() * r * r * (G * W * H).abs().mean(1, keepdim=True))
+        want = part + (0.0 if up is None else up.double())
+        close(dh, want, want.abs() * (e + 2 * U) + size * 12 * U)
+        close(dw, (G * H * r).sum(0), (G * H * r).abs().sum(0) * (rows + 4) * U)
