@@ -35,7 +35,9 @@ struct LogprobArgs {
 
 // Running maximum of the logits, and sums of powers of two: c = scale log2 e, z log2 e = c x. (Logits are
 // subtracted before they are multiplied: so those of the type's lowest value are equal ones, not
-// infinite, and what is rounded is their distance.)
+// infinite, and what is rounded is their distance.) A distance below kNothing has the power 0, which takes it
+// out of u: it is cut there, so that it stays finite with the number of a row's logits times it.
+constexpr float kNothing = -1024.f;
 struct Sums {
     float m = -INFINITY, s = 0.f, u = 0.f;
 
@@ -43,7 +45,7 @@ struct Sums {
     {
         if (now > m) {
             const float d = (m - now) * c, f = __builtin_amdgcn_exp2f(d);  // (d may be minus infinity: nothing so far)
-            u = f * fmaf(fmaxf(d, -1e30f), s, u);
+            u = f * fmaf(fmaxf(d, kNothing), s, u);
             s *= f;
             m = now;
         }
@@ -52,7 +54,7 @@ struct Sums {
     {
         const float d = (x - (m == -INFINITY ? 0.f : m)) * c, e = __builtin_amdgcn_exp2f(d);
         s += e;
-        u = fmaf(e, fmaxf(d, -1e30f), u);  // (e is 0 for minus infinity)
+        u = fmaf(e, fmaxf(d, kNothing), u);
     }
     __device__ __forceinline__ void join(float m2, float s2, float u2, float c)
     {
@@ -63,7 +65,7 @@ struct Sums {
             return;
         }
         const float d = (m - now) * c, d2 = (m2 - now) * c, f = __builtin_amdgcn_exp2f(d), f2 = __builtin_amdgcn_exp2f(d2);
-        const float a = f * fmaf(fmaxf(d, -1e30f), s, u), b = f2 * fmaf(fmaxf(d2, -1e30f), s2, u2);
+        const float a = f * fmaf(fmaxf(d, kNothing), s, u), b = f2 * fmaf(fmaxf(d2, kNothing), s2, u2);
         u = a + b;
         s = f * s + f2 * s2;
         m = now;
