@@ -771,8 +771,8 @@ int himuon_token_logprob(int64_t n_tokens, int64_t vocab, const void* logits, in
 /*
  * The logits' gradient from those of logprob and entropy (each may be NULL: none):
  *     d[i, j] = scale * (g_logprob[i] (delta(j, tokens[i]) - p) - g_entropy[i] p (log p + entropy[i]))
- * with p from the logits and lse, or from the logits alone where lse, 1024 or more, is
- * rounded too far. Rows that are not in use, and rows whose lse is minus
+ * with p from the logits and lse, or from the logits alone where lse is rounded too far (1024 or more
+ * from zero, 32 or more for fp32 logits). Rows that are not in use, and rows whose lse is minus
  * infinity, get zeros; so do logits of minus infinity but for the token's own. d: storage
  * `dtype`, ld_d >= vocab; may be the logits (same ld).
  */
