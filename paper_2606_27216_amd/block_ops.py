@@ -11,7 +11,9 @@ They keep the rules of ``train_ops``: argument checks and marshalling only, work
 HimuonError for an error of the library; float32 or bfloat16 storage.
 
 ``add_norm``, ``attention`` and ``token_logprob`` join autograd where it records (results
-written to ``out`` carry no graph). lse and the most likely tokens carry none. A backward
+written to ``out`` carry no graph). lse and the most likely tokens carry none. Tensors with
+tangents are refused (there are no forward-mode derivatives), and so are scales and eps that are
+tensors which ask for a gradient. A backward
 pass is captured into a HIP graph as any of torch's is: after a warm-up on the capturing
 stream, and while no eager graph of the same leaves is alive.
 """
@@ -21,7 +23,7 @@ import ctypes
 import struct
 
 from . import lib
-from .train_ops import (ACT_GROUP, I32, _away, _done, _heads, _heads_like, _HEADS, _index_code, _matrix, _on, _same_device,
+from .train_ops import (ACT_GROUP, I32, _away, _done, _heads, _heads_like, _HEADS, _index_code, _keeps, _matrix, _on, _same_device,
                         _stream_of, _torch, _type_code, _workspace)
 
 MAX_ATTN_DIM = 256           # HIMUON_MAX_ATTN_DIM
@@ -92,6 +94,7 @@ def add_norm(x, residual, gain, eps=1e-6, pack=False, out=None, stream=None):
 
     The gradients of ``x``, ``residual`` and ``gain`` are ``add_norm_grad``'s."""
     torch = _torch()
+    _keeps("add_norm", eps, x, residual, gain)
     rows, width, ld = _rows(x, "x")
     dev, code, gain_code = x.device, _type_code(x), _gain(gain, width)
     ld_res = 0 if residual is None else _rows_like(residual, "residual", x)
@@ -129,6 +132,7 @@ def add_norm_grad(g_y, h, gain, g_h=None, eps=1e-6, out=None, workspace=None, st
     (None: h was not used further) and from h, (dh, dgain). dh is the gradient of x and of
     the residual alike. ``out``: the tensor for dh (``g_y`` or ``g_h`` is allowed)."""
     torch = _torch()
+    _keeps("add_norm_grad", eps, g_y, h, gain, g_h)
     rows, width, ld = _rows(h, "h")
     dev, code, gain_code = h.device, _type_code(h), _gain(gain, width)
     ld_gy = _rows_like(g_y, "g_y", h)
@@ -165,7 +169,6 @@ def _where(t, what, count, dev, index):
 
 def _attn_args(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale):
     """(shapes of q and k, himuon_attn_t, q, k and v as himuon_heads_t), checked."""
-    _torch()
     sq, hq = _heads(q, "q")
     sk, hk = _heads(k, "k")
     dim, dev = sq[-1], q.device
@@ -233,6 +236,7 @@ def attention(q, k, v, q_starts=None, k_starts=None, q_lengths=None, k_lengths=N
 
     The gradients of q, k and v are ``attention_grad``'s."""
     torch = _torch()
+    _keeps("attention", scale, q, k, v)
     sq, sk, args, hq, hk, hv = _attn_args(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale)
     dev = q.device
     if _away(dev, stream):
@@ -255,6 +259,7 @@ def attention_grad(g, q, k, v, out, lse, q_starts=None, k_starts=None, q_lengths
     """The backward pass of ``attention``: from the gradient ``g`` of its result, and its
     inputs and results, (dq, dk, dv). ``grads``: the tensors to write."""
     torch = _torch()
+    _keeps("attention_grad", scale, g, q, k, v, out, lse)
     sq, sk, args, hq, hk, hv = _attn_args(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale)
     dev = q.device
     hg, ho = _heads_like(g, "g", sq, q), _heads_like(out, "out", sq, q)
@@ -299,6 +304,7 @@ def token_logprob(logits, tokens, top=0, scale=1.0, stream=None):
 
     The gradient of ``logits`` from those of logprob and entropy is ``token_logprob_grad``'s."""
     torch = _torch()
+    _keeps("token_logprob", scale, logits)
     vocab = _logits(logits, tokens)[1]
     dev = logits.device
     _type_code(logits), _index_code(tokens)
@@ -338,6 +344,7 @@ def token_logprob_grad(g_logprob, g_entropy, logits, tokens, lse, entropy, scale
     """The backward pass of ``token_logprob``: from the gradients of logprob and entropy
     (either may be None), its inputs and its results lse and entropy, the gradient of the
     logits. ``out``: the tensor for it (the logits themselves are allowed)."""
+    _keeps("token_logprob_grad", scale, g_logprob, g_entropy, logits, lse, entropy)
     rows, vocab, ld = _logits(logits, tokens)
     dev, code, index = logits.device, _type_code(logits), _index_code(tokens)
     if lse is None or (g_entropy is not None and entropy is None):

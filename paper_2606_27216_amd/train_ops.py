@@ -13,7 +13,9 @@ of the library raises HimuonError. Tensors are float32 or bfloat16.
 
 ``embed`` and ``qk_norm_rope`` join autograd where it records: gradients reach the table,
 queries, keys and gains (not the cosines and sines). Results written to ``out``, and the
-other operators' results, carry no graph.
+other operators' results, carry no graph. Neither has a forward-mode derivative: tensors with
+tangents are refused, by their gradients too, and so are scales and eps that are tensors
+which ask for a gradient.
 
 Inputs of a call for another stream are the caller's to keep until it has read them
 (``record_stream``), as with torch's own operations.
@@ -61,14 +63,15 @@ def declare(L):
 # once, and the error messages are made only when something is wrong.)
 
 _INDEX, _TYPES = {}, {}
-_device = _raw_stream = None
+_device = _raw_stream = _forward = None
 
 
 def _torch():
-    global _device, _raw_stream
+    global _device, _raw_stream, _forward
     import torch
     if not _INDEX:  # (filled last: another thread that finds it filled finds all of this)
         _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        from torch.autograd import forward_ad as _forward
         _TYPES.update({torch.float32: F32, torch.bfloat16: BF16})
         _INDEX.update({torch.int32: I32, torch.int64: I64})
     return torch
@@ -84,6 +87,20 @@ def _index_code(t):
 def _type_code(t):
     code = _TYPES.get(t.dtype)
     return _dtype_code(t) if code is None else code
+
+
+def _keeps(op, number, *tensors):
+    """Refuses what would lose a derivative without a word: a tensor with a tangent (the operators
+    have no forward-mode rules), and a number that is a tensor which asks for a gradient."""
+    if _forward is not None and _forward._current_level < 0 and (type(number) is float or number is None):
+        return
+    torch = _torch()
+    if getattr(number, "requires_grad", False) and torch.is_grad_enabled():
+        raise NotImplementedError(f"{op} gives no gradient of its scale or eps: pass a number, or the tensor detached")
+    if _forward._current_level >= 0:
+        for t in (number, *tensors):
+            if isinstance(t, torch.Tensor) and _forward.unpack_dual(t).tangent is not None:
+                raise NotImplementedError(f"{op} has no forward-mode derivative: its arguments must not carry tangents")
 
 
 def _matrix(t, what):
@@ -172,6 +189,7 @@ def embed(tokens, table, scale=1.0, out=None, stream=None):
     of a 2-D ``out`` (one row per token) may be strided. The table's gradient is
     ``embed_grad``'s."""
     torch = _torch()
+    _keeps("embed", scale, table)
     rows, width, ld = _matrix(table, "table")
     if not tokens.is_cuda or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous CUDA tensor")
@@ -204,7 +222,7 @@ def embed_grad(tokens, grad, num_rows, scale=1.0, out=None, dtype=None, accumula
     (``tokens.shape + (width,)`` or 2-D with strided rows); the result is
     ``num_rows`` x width in ``dtype`` (default: ``grad``'s), or is added to ``out``
     with ``accumulate``."""
-    _torch()
+    _keeps("embed_grad", scale, grad, out)
     if not tokens.is_cuda or not tokens.is_contiguous():
         raise ValueError("tokens must be a contiguous CUDA tensor")
     n = tokens.numel()
@@ -312,6 +330,7 @@ def qk_norm_rope(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, inter
     ``out``         the two tensors to write (q and k themselves are allowed).
 
     The gradients of ``q``, ``k`` and the gains are ``qk_norm_rope_grad``'s."""
+    _keeps("qk_norm_rope", eps, q, k, q_gain, k_gain, cos, sin)
     sq, sk, args, hq, hk = _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
     dev = q.device
     if _away(dev, stream):
@@ -330,6 +349,7 @@ def qk_norm_rope_grad(g_q, g_k, q, k, q_gain, k_gain, cos, sin, positions=None, 
     outputs and its inputs, (dq, dk, dq_gain, dk_gain). ``out``: the tensors for dq
     and dk (``g_q`` and ``g_k`` themselves are allowed)."""
     torch = _torch()
+    _keeps("qk_norm_rope_grad", eps, g_q, g_k, q, k, q_gain, k_gain, cos, sin)
     sq, sk, args, hq, hk = _qk_args(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
     dev = q.device
     if _away(dev, stream):
