@@ -54,8 +54,8 @@ class Norm(torch.autograd.Function):
 
 class Attention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale):
-        out, lse = ops.attention(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale)
+    def forward(ctx, q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale, workspace):
+        out, lse = ops.attention(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale, workspace=workspace)
         ctx.save_for_backward(q, k, v, out, lse, q_starts, k_starts, q_lengths, k_lengths)
         ctx.causal, ctx.scale = causal, scale
         ctx.mark_non_differentiable(lse)
@@ -65,7 +65,7 @@ class Attention(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, g, _):
         grads = ops.attention_grad(_adjacent(g), *ctx.saved_tensors, ctx.causal, ctx.scale)
-        return (*grads, None, None, None, None, None, None)
+        return (*grads, None, None, None, None, None, None, None)
 
 
 class TokenLogprob(torch.autograd.Function):

@@ -242,7 +242,7 @@ def attention(q, k, v, q_starts=None, k_starts=None, q_lengths=None, k_lengths=N
     if _away(dev, stream):
         return _on(dev, stream, attention, q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale, out, workspace)
     if out is None and (q.requires_grad or k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
-        return _functions().Attention.apply(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale)
+        return _functions().Attention.apply(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale, workspace)
     L = lib()
     held, ws, ws_bytes = _workspace(L.himuon_attention_workspace_size(args), workspace, q)
     if out is None:
