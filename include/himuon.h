@@ -734,7 +734,7 @@ int himuon_attention(const himuon_attn_t* args, const himuon_heads_t* q, const h
 /*
  * Its backward pass: from the gradient g of out, and the inputs and results of the
  * forward call, the gradients dq, dk, dv (summed over the heads that share a key head).
- * They must not overlap the inputs.
+ * They must not overlap the inputs, nor each other.
  * workspace  himuon_attention_grad_workspace_size(args) bytes, 16-byte aligned.
  */
 size_t himuon_attention_grad_workspace_size(const himuon_attn_t* args);

@@ -257,7 +257,7 @@ def attention(q, k, v, q_starts=None, k_starts=None, q_lengths=None, k_lengths=N
 def attention_grad(g, q, k, v, out, lse, q_starts=None, k_starts=None, q_lengths=None, k_lengths=None, causal=True, scale=None,
                    grads=None, workspace=None, stream=None):
     """The backward pass of ``attention``: from the gradient ``g`` of its result, and its
-    inputs and results, (dq, dk, dv). ``grads``: the tensors to write."""
+    inputs and results, (dq, dk, dv). ``grads``: the three tensors to write, which must not overlap."""
     torch = _torch()
     _keeps("attention_grad", scale, g, q, k, v, out, lse)
     sq, sk, args, hq, hk, hv = _attn_args(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale)

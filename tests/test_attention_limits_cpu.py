@@ -1,0 +1,21 @@
+"""attention's sizes and results at their limits, on a machine without a GPU: refused before anything
+is enqueued."""
+import pytest
+from test_block_ops_cpu import HEADS, P, _attn, _backward
+
+import paper_2606_27216_amd as hm
+from paper_2606_27216_amd import train_ops
+
+
+def _place(n):
+    return train_ops._HEADS.pack(n * P, 64 * 4 * 12, 64 * 4, 64)
+
+
+@pytest.mark.parametrize("places", [(2, 2, 3), (2, 3, 2), (2, 3, 3)])
+def test_gradients_in_each_others_place(places):
+    """Two results in one array would be written by two blocks at a time."""
+    assert _backward(_attn(), [HEADS] * 5 + [_place(n) for n in places]) == hm.ERR_INVALID_ARG
+    # (a side without tokens has no place)
+    none = train_ops._HEADS.pack(0, 64 * 4 * 12, 64 * 4, 64)
+    assert _backward(_attn(q_len=0, k_len=0), [none] * 8, lse=None, ws=None, ws_bytes=0) == hm.OK
+
