@@ -725,6 +725,7 @@ template <GemmStore ST, bool DMA, int DP> int launch_grad(AttnArgs p, hipStream_
     ps.k_blocks = (int32_t)(ks_blocks * kv_parts<ST, DP>());
     const int64_t blocks = qs_blocks * q_parts<ST, DP>() + ps.k_blocks;
     if (blocks > 0 && !launchable(blocks, T)) return HIMUON_ERR_UNSUPPORTED;
+    if ((p.dq.ptr && (p.dq.ptr == p.dk.ptr || p.dq.ptr == p.dv.ptr)) || (p.dk.ptr && p.dk.ptr == p.dv.ptr)) return HIMUON_ERR_INVALID_ARG;
     StreamDevice on(stream);
     if (on.status != HIMUON_OK) return on.status;
     if (q_shared) hipLaunchKernelGGL((attn_grad_rows<ST, DP, DMA>), dim3((unsigned)q_blocks), dim3(kThreads), 0, stream, p);
@@ -780,7 +781,6 @@ extern "C" int himuon_attention_grad(const himuon_attn_t* args, const himuon_hea
     p.lse = const_cast<float*>(lse);
     const size_t need = himuon_attention_grad_workspace_size(args);
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return HIMUON_ERR_WORKSPACE;
-    if ((p.dq.ptr && (p.dq.ptr == p.dk.ptr || p.dq.ptr == p.dv.ptr)) || (p.dk.ptr && p.dk.ptr == p.dv.ptr)) return HIMUON_ERR_INVALID_ARG;
     p.stats = static_cast<float2*>(workspace);
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     if (args->dtype == HIMUON_BF16) return dma ? launch_dim<GemmStore::BF16, true>(p, hs) : launch_dim<GemmStore::BF16, false>(p, hs);
