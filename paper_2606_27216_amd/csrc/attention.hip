@@ -489,7 +489,7 @@ int check_attn(const himuon_attn_t* a)
     const int64_t group = a->q_heads / a->k_heads;
     if (a->batch > most || a->q_len > most / group || a->k_len > most) return HIMUON_ERR_UNSUPPORTED;
     // (rows of statistics; a batch's index)
-    if (!small_product(a->batch * (a->q_starts ? 1 : a->q_len), a->q_heads * 8) || !small_product(a->batch, a->k_len))
+    if (!small_product(a->batch * (a->q_starts ? 1 : a->q_len), (int64_t)a->q_heads * 8) || !small_product(a->batch, a->k_len))
         return HIMUON_ERR_UNSUPPORTED;
     return HIMUON_OK;
 }
