@@ -23,7 +23,8 @@ namespace himuon {
 namespace attn {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64, kTileRows = kRows * kWaves;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+static_assert(kTileRows == kRows * kWaves, "");
 
 // A row's softmax as far as it has come: o unnormalised, the maximum m that its exponentials are
 // relative to, their sum l (of this half's keys).
@@ -246,7 +247,6 @@ __global__ void __launch_bounds__(kThreads, (Lay<ST, DP>::PITCH <= 256 ? 2 : 1))
 // that a group of heads has (a token or some of each sequence against many keys), the keys are
 // shared out over `splits` blocks too, whose results meet in `part`: [splits] rows of DP sums and of
 // {m, l}.
-constexpr int kFewLds = 128 << 10;
 template <GemmStore ST, int DP> constexpr int few_waves() { return std::min(4, kFewLds / (4 * kRows * Lay<ST, DP>::PITCH)); }
 template <GemmStore ST, int DP> constexpr int few_lds()
 {
@@ -424,28 +424,11 @@ template <class F> int by_dim(const AttnArgs& p, F f)
     return f(std::integral_constant<int, 256>{});
 }
 
-int padded_dim(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
-
-bool few_rows(const himuon_attn_t* a) { return !a->q_starts && a->q_len * (a->q_heads / a->k_heads) <= kRows && a->k_len > 64; }
-
-// Blocks that share the keys of a group of heads: as many as fill the chip, one to a CU.
-int64_t few_splits(const himuon_attn_t* a)
-{
-    const int64_t waves = std::min<int64_t>(4, kFewLds / (4 * kRows * padded_dim(a->head_dim) * dtype_size(a->dtype)));
-    const int64_t most = ceil_div(a->k_len, kRows * waves * 2);  // two tiles to a wave
-    return std::max<int64_t>(1, std::min<int64_t>(most, ceil_div(256, a->batch * a->k_heads)));
-}
-
-// Blocks of four times 32 rows below which the waves of a block share 32 of them. Heads of 128, 16 + 8 of
-// them, causal, first form / second, us: 1 x 128 tokens (16 blocks) bf16 11.4 / 11.2, fp32 28 / 20; 1 x 512
-// (64) 17 / 14 and 81 / 62; 2 x 512 (128) 18 / 25 and 83 / 109.
-constexpr int64_t kSharedBelow = 96;
-
-template <GemmStore ST, bool DMA> int launch_forward(AttnArgs p, bool few, hipStream_t stream)
+template <GemmStore ST, bool DMA> int launch_forward(AttnArgs p, Forward form, hipStream_t stream)
 {
     return by_dim(p, [&](auto dim) {
         constexpr int DP = decltype(dim)::value;
-        if (few) {
+        if (form == Forward::FEW_ROWS) {
             const int64_t blocks = (int64_t)p.batch * p.hk * p.splits;
             constexpr int T = 64 * few_waves<ST, DP>();
             if (!launchable(blocks, T)) return (int)HIMUON_ERR_UNSUPPORTED;
@@ -460,15 +443,15 @@ template <GemmStore ST, bool DMA> int launch_forward(AttnArgs p, bool few, hipSt
             return launch_status();
         }
         int64_t blocks;
-        if (!set_grid(p, p.q_len * p.group, kTileRows, kThreads, &blocks)) return (int)HIMUON_ERR_UNSUPPORTED;
-        if (blocks < kSharedBelow) {
+        if (form == Forward::FEW_TILES) {
             constexpr int T = 64 * few_waves<ST, DP>();
-            if (!set_grid(p, p.q_len * p.group, kRows, T, &blocks)) return (int)HIMUON_ERR_UNSUPPORTED;
+            if (!set_grid<false>(p, kRows, T, &blocks)) return (int)HIMUON_ERR_UNSUPPORTED;
             StreamDevice on(stream);
             if (on.status != HIMUON_OK) return on.status;
             hipLaunchKernelGGL((attn_few<ST, DP, DMA>), dim3((unsigned)blocks), dim3(T), 0, stream, p);
             return launch_status();
         }
+        if (!set_grid<false>(p, kTileRows, kThreads, &blocks)) return (int)HIMUON_ERR_UNSUPPORTED;
         StreamDevice on(stream);
         if (on.status != HIMUON_OK) return on.status;
         hipLaunchKernelGGL((attn_forward<ST, DP, DMA>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
@@ -541,16 +524,6 @@ bool set_heads(Heads& t, const himuon_heads_t* h, const himuon_attn_t* a, int64_
     return true;
 }
 
-bool set_grid(AttnArgs& p, int64_t rows, int tile, int threads, int64_t* blocks)
-{
-    const int64_t slots = p.packed ? rows / tile + p.batch + 2 : ceil_div(rows, tile);
-    const int64_t items = p.packed ? slots : slots * p.batch;
-    if (slots > INT32_MAX || !small_product(items, p.hk) || !launchable(items * p.hk, threads)) return false;
-    p.slots = (int32_t)slots;
-    *blocks = items * p.hk;
-    return true;
-}
-
 }  // namespace attn
 }  // namespace himuon
 
@@ -558,8 +531,8 @@ extern "C" size_t himuon_attention_workspace_size(const himuon_attn_t* args)
 {
     using namespace himuon;
     using namespace himuon::attn;
-    if (check_attn(args) != HIMUON_OK || empty_batch(args) || args->q_len == 0 || !few_rows(args)) return 0;
-    const int64_t splits = few_splits(args);
+    if (check_attn(args) != HIMUON_OK || empty_batch(args) || args->q_len == 0 || !few_rows(*args)) return 0;
+    const int64_t splits = few_splits(*args);
     if (splits == 1) return 0;
     return (size_t)(args->batch * args->k_heads * splits) * kRows * (size_t)(padded_dim(args->head_dim) + kStat) * sizeof(float);
 }
@@ -579,13 +552,13 @@ extern "C" int himuon_attention(const himuon_attn_t* args, const himuon_heads_t*
         return HIMUON_ERR_INVALID_ARG;
     if (p.o.ptr == p.q.ptr || p.o.ptr == p.k.ptr || p.o.ptr == p.v.ptr) return HIMUON_ERR_INVALID_ARG;
     p.lse = lse;
-    const bool few = few_rows(args);
-    if (few) p.splits = (int32_t)few_splits(args);
+    const Forward form = plan_forward(*args);
+    if (form == Forward::FEW_ROWS) p.splits = (int32_t)few_splits(*args);
     const size_t need = himuon_attention_workspace_size(args);
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return HIMUON_ERR_WORKSPACE;
     p.part = static_cast<float*>(workspace);
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     if (args->dtype == HIMUON_BF16)
-        return dma ? launch_forward<GemmStore::BF16, true>(p, few, hs) : launch_forward<GemmStore::BF16, false>(p, few, hs);
-    return dma ? launch_forward<GemmStore::F32, true>(p, few, hs) : launch_forward<GemmStore::F32, false>(p, few, hs);
+        return dma ? launch_forward<GemmStore::BF16, true>(p, form, hs) : launch_forward<GemmStore::BF16, false>(p, form, hs);
+    return dma ? launch_forward<GemmStore::F32, true>(p, form, hs) : launch_forward<GemmStore::F32, false>(p, form, hs);
 }

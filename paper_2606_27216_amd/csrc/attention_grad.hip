@@ -24,7 +24,8 @@ namespace himuon {
 namespace attn {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64, kTileRows = kRows * kWaves;
+constexpr int kThreads = 256;
+static_assert(kTileRows == kRows * kThreads / 64, "");
 
 // Tiles of 32 rows lie in a ring of LDS buffers. A tile's g v^T goes out beside its exponentials, and
 // in bf16 the next tile's scores beside its ds, as long as registers hold both; fp32 products take
@@ -697,29 +698,21 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
 
 // ---------------------------------------------------------------- host side
 
-// Blocks of four times 32 keys (rows) below which the waves of a block share 32 of them: where the
-// first kind leaves the chip idle, with one wave on the long way over the other side's tiles. Heads of 128,
-// 16 + 8 of them, causal, first form / second, us: fp32 1 x 128 tokens 111 / 38 (8 blocks of keys, 16 of
-// rows), 1 x 512 382 / 109 (32, 64), 2 x 1024 747 / 386 (128, 256), 4 x 1024 774 / 771 (256, 512; keys in the second
-// and rows in the first 660), 8 x 1024 1093 / 1551; bf16 1 x 128 29 / 20, 1 x 512 57 / 35, 2 x 512 59 / 46 (64, 128;
-// keys in the second and rows in the first 50), 4 x 512 61 / 79 (128, 256).
-template <GemmStore ST> constexpr int64_t shared_below() { return ST == GemmStore::F32 ? 512 : 96; }
-template <GemmStore ST> int64_t rows_shared_below(bool keys) { return ST == GemmStore::F32 ? 512 : keys ? 192 : 96; }
 template <GemmStore ST, bool DMA, int DP> int launch_grad(AttnArgs p, hipStream_t stream)
 {
     int64_t q_blocks = 0, k_blocks = 0;
     AttnArgs pk = p;
     // Blocks of four waves with 32 rows each, or with 32 rows that they share.
-    if (!set_grid(p, p.q_len * p.group, kTileRows, kThreads * q_parts<ST, DP>(), &q_blocks) ||
-        !set_grid(pk, pk.k_len, kTileRows, kThreads * kv_parts<ST, DP>(), &k_blocks))
+    if (!set_grid<false>(p, kTileRows, kThreads * q_parts<ST, DP>(), &q_blocks) ||
+        !set_grid<true>(pk, kTileRows, kThreads * kv_parts<ST, DP>(), &k_blocks))
         return HIMUON_ERR_UNSUPPORTED;
     constexpr int T = 64 * shared_waves<ST, DP>();
-    const bool k_shared = p.k_len > 0 && k_blocks < shared_below<ST>();
-    const bool q_shared = p.q_len > 0 && q_blocks < rows_shared_below<ST>(k_shared);
+    const GradPlan plan = plan_grad(ST == GemmStore::F32, p.q_len > 0 ? q_blocks : 0, p.k_len > 0 ? k_blocks : 0);
+    const bool k_shared = plan.k_shared, q_shared = plan.q_shared;
     AttnArgs ps = p;
     int64_t qs_blocks = 0, ks_blocks = 0;
-    if ((q_shared && !set_grid(ps, p.q_len * p.group, kRows, T * q_parts<ST, DP>(), &qs_blocks)) ||
-        (k_shared && !set_grid(pk, pk.k_len, kRows, T * kv_parts<ST, DP>(), &ks_blocks)))
+    if ((q_shared && !set_grid<false>(ps, kRows, T * q_parts<ST, DP>(), &qs_blocks)) ||
+        (k_shared && !set_grid<true>(pk, kRows, T * kv_parts<ST, DP>(), &ks_blocks)))
         return HIMUON_ERR_UNSUPPORTED;
     ps.k_slots = pk.slots;
     ps.k_blocks = (int32_t)(ks_blocks * kv_parts<ST, DP>());

@@ -8,6 +8,7 @@
 // reads follow that order. So scores never pass through LDS.
 #pragma once
 
+#include "attn_plan.h"
 #include "lds_dma.h"
 #include "train_ops.h"
 
@@ -21,7 +22,6 @@ using dev::u32x2;
 using dev::u32x4;
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kRows = 32;  // of a wave: rows or columns of a product's tile
 
 // ------------------------------------------------------------------ arguments
 
@@ -498,8 +498,15 @@ inline bool empty_batch(const himuon_attn_t* a) { return a->batch == 0 && !a->q_
 AttnArgs attn_args(const himuon_attn_t* a);
 bool set_heads(Heads& t, const himuon_heads_t* h, const himuon_attn_t* a, int64_t tokens, int heads, bool output, bool* dma);
 
-// A grid of one block to each tile of `rows` rows and key head (false: more than a launch holds).
-bool set_grid(AttnArgs& p, int64_t rows, int tile, int threads, int64_t* blocks);
+// A grid of one block to each tile of `tile` rows (KEYS: keys) and key head (false: more than a launch holds).
+template <bool KEYS> bool set_grid(AttnArgs& p, int tile, int threads, int64_t* blocks)
+{
+    const AttnTiles t = attn_tiles<KEYS>(p.packed, p.batch, KEYS ? p.k_len : p.q_len, p.group, p.hk, tile);
+    if (t.slots > INT32_MAX || t.blocks < 0 || !launchable(t.blocks, threads)) return false;
+    p.slots = (int32_t)t.slots;
+    *blocks = t.blocks;
+    return true;
+}
 
 }  // namespace attn
 }  // namespace himuon
