@@ -234,7 +234,8 @@ def attention(q, k, v, q_starts=None, k_starts=None, q_lengths=None, k_lengths=N
                     A query that sees no key gives zeros, and minus infinity for lse.
     ``scale``         dim ** -0.5 by default; positive.
 
-    The gradients of q, k and v are ``attention_grad``'s."""
+    bfloat16 inputs' probabilities are rounded to bfloat16 for their product with v; float32 inputs keep
+    them in float32. The gradients of q, k and v are ``attention_grad``'s."""
     torch = _torch()
     _keeps("attention", scale, q, k, v)
     sq, sk, args, hq, hk, hv = _attn_args(q, k, v, q_starts, k_starts, q_lengths, k_lengths, causal, scale)

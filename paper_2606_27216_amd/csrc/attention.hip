@@ -8,11 +8,15 @@
 // a row's statistics are one lane's, and p^T is the second operand of o^T = v^T p^T as it
 // stands.
 //
-// What bounds it: with many rows the issue of instructions, products (47% of the matrix cores'
-// cycles) and softmax side by side (causal bf16, heads of 128: 4 x 4096 tokens with 32 + 8 heads 542 us,
-// 1.01 PFLOP/s; 16 x 1024 with 16 + 8 106; without exponentials in a trial the first took 9% less, without either
-// product 18%); in fp32 the products (71% of the cycles; 8 x 1024 tokens 350 us, 98 TFLOP/s); with some queries
-// against a cache the memory (4 against 32768 keys of 8 heads in 8 sequences 99 us).
+// What bounds it: with many rows the issue of instructions, products (52% of the matrix cores' cycles; LDS is
+// read in 26% of a CU's) and softmax side by side (causal bf16, heads of 128: 4 x 4096 tokens with 32 + 8 heads 542 us,
+// 1.01 PFLOP/s; 16 x 1024 with 16 + 8 106, 37% and 18%; without exponentials in a trial the first took 9% less, without
+// either product 18%); in fp32 the products (71% of the cycles; 8 x 1024 tokens 350 us, 98 TFLOP/s); with a query or some
+// against a cache the memory (one query of each of 4 sequences against their 16384 to 32768 keys, 32 + 8 heads of 128: 99 us).
+//
+// bf16 probabilities are rounded to bf16 for their product with v, as the matrix cores take both operands in one type:
+// results are off by 0.0021 to 0.0023 of their size (root mean square, against 64 bits), 0.0017 if only they are
+// rounded. fp32 arrays keep them in fp32.
 #include "attn_device.h"
 
 #include <algorithm>

@@ -12,8 +12,13 @@
 //
 // What bounds it: the issue of instructions, and in the keys' kernel one wave to a SIMD, as its
 // registers hold two operands and two sums of 32 keys (causal bf16, 16 x 1024 tokens, 16 + 8 heads of 128:
-// queries' side 145 us, keys' 200; 2 x 4096 with 32 + 8 heads 890 both, 0.77 PFLOP/s of the five products that
-// the mathematics asks for); in fp32 the products (8 x 1024 tokens 1100 us).
+// queries' side 145 us, keys' 200, the matrix cores busy in 38% and 36% of their cycles and LDS read in 19% and 22% of a
+// CU's; 2 x 4096 with 32 + 8 heads 890 both, 0.77 PFLOP/s of the five products that the mathematics asks for); in
+// fp32 the products (8 x 1024 tokens 1090 us). Heads of more than 128 columns in fp32: each of a result's parts forms the
+// scores and g v^T for itself, 27 products for 5 (8 x 1024 tokens, 16 + 8 heads of 256: 8.2 ms).
+//
+// bf16 p and ds are rounded to bf16 for their products, as in the forward pass: gradients are off by 0.0025 of their
+// size, 0.0018 if only they are rounded. fp32 arrays keep them in fp32.
 #include "attn_device.h"
 
 #include <algorithm>
@@ -460,7 +465,7 @@ template <GemmStore ST, int DP, bool DMA> __global__ void __launch_bounds__(kThr
 
 // Where tiles are few, the waves of a block share 32 rows (keys) and take the other side's tiles in
 // turn, each through LDS of its own and without a barrier; their sums meet there in the end. (fp32, 901
-// packed tokens in documents, 12 + 4 heads of 80: 78 us both sides, 112 in a launch of each; 1 x 512 tokens, 16 + 8
+// packed tokens in documents, 12 + 4 heads of 80: 78 us both sides, 112 in a launch of each with the same cuts; 1 x 512 tokens, 16 + 8
 // heads of 128 109, of which the products' cycles on the longest block's way are 55. Copying a tile's rows in
 // an order that hid them behind products changed nothing.)
 constexpr int kSharedLds = 128 << 10;

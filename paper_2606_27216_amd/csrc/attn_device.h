@@ -63,7 +63,7 @@ template <GemmStore ST> HM_DEV void mma(f32x16& acc, const Frag<ST>& a, const Fr
 }
 
 // Registers 8 t .. 8 t + 7 of a result as the second operand of the next product. (bf16:
-// rounded to nearest even, at most 2^-9 of each value; sums are taken of the unrounded ones.)
+// rounded to nearest even, by at most 2^-8 of each value; sums are taken of the unrounded ones.)
 template <GemmStore ST> HM_DEV Frag<ST> as_operand(const f32x16& c, int t)
 {
     Frag<ST> f;

@@ -32,10 +32,14 @@ template <bool KEYS> AttnTiles attn_tiles(bool packed, int64_t batch, int64_t le
 }
 
 // A token or some of each sequence against many keys: the waves of a block share the 32 rows that a group of heads
-// has, and take the keys in pieces.
+// has, and take the keys in pieces. One query a sequence, 32 + 8 heads of 128, bf16, us in this form / in the others:
+// 1 x 4096 keys to each of 4 sequences 23 / 71, 512 16 / 14, 128 11.7 / 12.1; 64 sequences with 48 keys 14.9 / 12.2, 128
+// 14.9 / 12.2, 512 28 / 23, 2048 96 / 86 (heads of sequences enough to fill the chip: the others are faster).
 inline bool few_rows(const himuon_attn_t& a) { return !a.q_starts && a.q_len * (a.q_heads / a.k_heads) <= kRows && a.k_len > 64; }
 
-// Blocks that share the keys of a group of heads: as many as fill the chip, one to a CU.
+// Blocks that share the keys of a group of heads: as many as fill the chip, one to a CU. The same calls with 128 / 256 / 512
+// blocks, us: 1 x 32768 keys 45 / 44 / 63, 4 x 4096 27 / 23 / 30, 8 x 4096 42 / 30 / 36, 16 x 4096 84 / 56 / 57, 4 x 32768 159 / 100 / 101,
+// 1 x 8192 23 / 28 / 28. One, two or four tiles to a wave at least: 1 x 2048 19.1 / 16.5 / 16.3, 1 x 8192 28 / 28 / 23.
 inline int64_t few_splits(const himuon_attn_t& a)
 {
     const int64_t es = a.dtype == HIMUON_BF16 ? 2 : 4;

@@ -8,7 +8,7 @@
 // most likely tokens come from a second look at few of them: every lane keeps the largest
 // logit that it saw, the k-th largest of those is a bound that the row's k largest logits reach,
 // and only the shares of lanes whose own reaches it are read again, by all lanes together.
-// (bf16 4096 x 128000 with the top 20: 209 us, 5.0 TB/s; gradient of 8192 x 32000: 195 us, 5.4 TB/s.)
+// (bf16 4096 x 128000 with the top 20: 209 us, 5.0 TB/s; gradient of 8192 x 32000: 176 to 196 us, 5.4 TB/s and more.)
 #include "elementwise8.h"
 #include "train_ops.h"
 
@@ -242,7 +242,9 @@ template <GemmStore ST, int NT, bool TOP> __global__ void __launch_bounds__(NT =
     if (plain && order_of(mine) >= bound) sh.hot[atomicAdd(&sh.hot_count, 1u)] = (uint16_t)lane;  // (in any order: what they hold is ranked)
     group_sync<NT>();
     const int hot = (int)sh.hot_count, chunks = (vocab + 8 * NT - 1) / (8 * NT);
-    if (hot <= (NT == 64 ? 64 : NT / 4)) {  // (more: equal logits everywhere, for the search below)
+    // (more: many lanes' largest logits are equal to the bound, which bf16 logits' are at a top near the limit: of
+    // normal logits two thirds of the rows at 64, 3% at 60, none at 56. The search below takes them.)
+    if (hot <= (NT == 64 ? 64 : NT / 4)) {
         for (int i = lane; i < hot * chunks; i += NT) {
             const int h = i / chunks, at = 8 * (sh.hot[h] + NT * (i - h * chunks));
             if (at >= vocab) continue;
@@ -269,7 +271,7 @@ template <GemmStore ST, int NT, bool TOP> __global__ void __launch_bounds__(NT =
         }
         return;
     }
-    // Many equal logits, few finite ones, NaN: the k largest one after the other.
+    // Equal logits at the bound, few finite ones, NaN: the k largest one after the other.
     uint64_t own = next_key(~0ull);
     for (int i = 0; i < k; ++i) {
         const uint64_t key = group_max<NT>(own, sh, lane);
@@ -390,8 +392,9 @@ template <GemmStore ST> __global__ void __launch_bounds__(kGradThreads) logprob_
     }
 }
 
-// Lanes of a row: a wave's, or a block's of 256 or 512 (4096 x 32000 bf16 with the top 20: 73 us with 256, 87 with 512;
-// 4096 x 128000: 214 with 512, 229 with 1024).
+// Lanes of a row: a wave's, or a block's of 256 or 512. bf16, us: with the top 5 8192 x 1500 18.6 with 64 lanes, 47 with 256, x 2048
+// 15.5 and 45, x 4096 20.7 and 46 (the latter is taken), 256 x 3000 14.3 and 14.1; with the top 20 4096 x 32000 73 with 256,
+// 87 with 512; 4096 x 128000 214 with 512, 229 with 1024.
 int row_lanes(int64_t vocab) { return vocab <= 2048 ? 64 : vocab <= 32768 ? 256 : 512; }
 int64_t row_blocks(int64_t rows, int64_t vocab) { return row_lanes(vocab) == 64 ? ceil_div(rows, 4) : rows; }
 
