@@ -75,13 +75,14 @@ __device__ __forceinline__ float scale_of(double sum, const NormArgs& p) { retur
 
 // r of a row and mean(g_y w h r), from its sums of h^2 and of g_y w h. (h r and that mean are of the gradients'
 // size whatever h's is. An estimate of 2^-23 and a step of Newton's, which takes it to 2^-44: a division and
-// a root of 64 bits would cost the registers of a wave.)
+// a root of 64 bits would cost the registers of a wave. A row with an infinite element has r = 0, and adds nothing to the
+// other columns' dw.)
 struct RowTerms {
     float r, mean;
     __device__ __forceinline__ RowTerms(double s, double t, const NormArgs& p)
     {
         const double x = fma(s, p.inv_width, (double)p.eps), y = __builtin_amdgcn_rsq(x);
-        const double root = y * fma(-0.5 * x * y, y, 1.5);
+        const double root = x > 0.0 && x < INFINITY ? y * fma(-0.5 * x * y, y, 1.5) : y;
         r = (float)root;
         mean = (float)(t * root * p.inv_width);
     }

@@ -50,3 +50,19 @@ def test_large_and_small_rows(scale, eps, width, dtype):
         want = part + (0.0 if up is None else up.double())
         close(dh, want, want.abs() * (e + 2 * U) + size * 12 * U)
         close(dw, (G * H * r).sum(0), (G * H * r).abs().sum(0) * (rows + 4) * U)
+
+
+@pytest.mark.parametrize("width", [100, 2048, 16400])
+def test_a_row_with_an_infinite_element(width):
+    """Its r is zero: it adds nothing to dgain but at that element, where the definition has 0 times infinity."""
+    print("[gpu-case] add_norm infinite element", width, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(width)
+    h, g = (torch.randn(5, width, generator=gen, device="cuda") for _ in range(2))
+    w = torch.ones(width, device="cuda")
+    h[2, 7] = float("inf")
+    rest = [0, 1, 3, 4]
+    dh, dw = hm.add_norm_grad(g, h, w)
+    want_h, want_w = hm.add_norm_grad(g[rest].contiguous(), h[rest].contiguous(), w)
+    assert bool(dw[7].isnan()) and torch.equal(dh[rest], want_h)
+    others = torch.arange(width, device="cuda") != 7
+    assert bool(((dw - want_w)[others].abs() <= 16 * U * (g * h.nan_to_num(0, 0, 0)).abs().sum(0)[others]).all())
