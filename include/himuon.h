@@ -721,8 +721,8 @@ typedef struct himuon_attn {
  * out = softmax(scale * q k^T) v over the keys that each query sees, and lse, the
  * natural logarithm of the sum of the scores' exponentials: [batch, q_len, q_heads] fp32,
  * contiguous. Products of bf16 arrays are exact, the softmax's statistics fp32, its
- * values rounded to bf16 for their product with v (which takes the results' error from 0.0017 to 0.0023 of
- * their size); fp32 arrays are multiplied in fp32, for those who want them unrounded.
+ * values rounded to bf16 for their product with v (results are then off by 0.0021 to 0.0023 of their size,
+ * instead of 0.0017); fp32 arrays are multiplied in fp32, for those who want them unrounded.
  * out must not overlap the inputs.
  * workspace  himuon_attention_workspace_size(args) bytes, 16-byte aligned (0: none is
  *            needed, or the arguments are invalid; NULL will do).
@@ -736,7 +736,7 @@ int himuon_attention(const himuon_attn_t* args, const himuon_heads_t* q, const h
  * Its backward pass: from the gradient g of out, and the inputs and results of the
  * forward call, the gradients dq, dk, dv (summed over the heads that share a key head).
  * They must not overlap the inputs, nor each other. The softmax's values and the scores' gradients are rounded to
- * bf16 for their products if the arrays are (error 0.0025 for 0.0018).
+ * bf16 for their products if the arrays are (errors of 0.0024 to 0.0027 for 0.0017 to 0.0022).
  * workspace  himuon_attention_grad_workspace_size(args) bytes, 16-byte aligned.
  */
 size_t himuon_attention_grad_workspace_size(const himuon_attn_t* args);

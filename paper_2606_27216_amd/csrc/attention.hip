@@ -15,8 +15,8 @@
 // against a cache the memory (one query of each of 4 sequences against their 16384 to 32768 keys, 32 + 8 heads of 128: 99 us).
 //
 // bf16 probabilities are rounded to bf16 for their product with v, as the matrix cores take both operands in one type:
-// results are off by 0.0021 to 0.0023 of their size (root mean square, against 64 bits), 0.0017 if only they are
-// rounded. fp32 arrays keep them in fp32.
+// results are off by 0.0021 to 0.0023 of their size (root mean square, against 64 bits), 0.0016 to 0.0017 if only they
+// are rounded. fp32 arrays keep them in fp32.
 #include "attn_device.h"
 
 #include <algorithm>
